@@ -279,6 +279,103 @@ w8a8_status w8a8_mfma_ceiling(const int8_t *xq, const int8_t *wq, int64_t M, int
 #define W8A8_READ_BLOCKS 2048
 w8a8_status w8a8_read_ceiling(const void *p, int64_t bytes, uint32_t *sums, void *stream);
 
+/* ---- Microscaled operators: 4-bit linears and a quantized key/value cache.
+ *
+ * A microscaled (MX) block (OCP Microscaling Formats v1.0) is 32 neighbouring values v with
+ * one scale byte s, which stands for 2^(s - 127), and 32 elements: e2m1, 4 bits (0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives), or e4m3, 8 bits (up to 448). With a = max |v|,
+ *   s = max(floor(log2(a)) - m + 127, 0), m = 2 (e2m1) or 8 (e4m3);
+ *   element = v / 2^(s - 127) rounded to nearest even, magnitudes above the format's largest
+ *   becoming the largest.
+ * All of it is exact arithmetic, so codes are determined bit by bit; a == 0 gives s = 0. A
+ * block that holds an infinity or a NaN gets s = 255 and zero elements and stands for NaN.
+ *
+ * A 4-bit matrix [R,K] is codes uint8 [R, 16 ceil(K/32)], two elements a byte with the
+ * earlier one in the low half, and scales uint8 [ceil(K/256), R, 8]: the 8 blocks of 256
+ * channels. Elements past K are zero, and so are the scales of blocks past K. Both arrays
+ * are 16-byte aligned (W8A8_ERR_ARG otherwise); bf16 operands may have any alignment. K is
+ * at most W8A8_MX4_MAX_K (W8A8_ERR_K_OVERFLOW). Non-finite inputs are allowed: they give
+ * NaN where the values of their block count. */
+#define W8A8_MX4_MAX_K (1 << 22)
+
+/* x: [R,K] bf16 of activations or weights, quantized as T(x) * col_mul (act and col_mul as in
+ * w8a8_quantize_act_ex). */
+w8a8_status w8a8_mx4_quantize(const uint16_t *x, int64_t R, int64_t K, int act,
+                              const float *col_mul, uint8_t *codes, uint8_t *scales,
+                              void *stream);
+
+/* What codes and scales stand for, as bf16 y [R,K] (every such value is a bf16 value). */
+w8a8_status w8a8_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t R,
+                                int64_t K, uint16_t *y, void *stream);
+
+/* Y [M,N] = bf16(X W^T + b) of two 4-bit matrices X [M,K] and W [N,K], accumulated in
+ * float32; bias: [N] bf16 or NULL. workspace: w8a8_mx4_gemm_workspace_bytes(M,N,K) bytes,
+ * 256-byte aligned (NULL allowed when that is 0). */
+w8a8_status w8a8_mx4_gemm(const uint8_t *xq, const uint8_t *x_scale, const uint8_t *wq,
+                          const uint8_t *w_scale, const uint16_t *bias, uint16_t *y, int64_t M,
+                          int64_t N, int64_t K, void *workspace, size_t workspace_bytes,
+                          void *stream);
+size_t w8a8_mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/* The whole 4-bit linear: x [M,K] bf16 quantized as by w8a8_mx4_quantize, then
+ * w8a8_mx4_gemm. workspace: w8a8_mx4_linear_workspace_bytes(M,N,K) bytes, 256-byte
+ * aligned. */
+w8a8_status w8a8_mx4_linear(const uint16_t *x, int act, const float *col_mul, const uint8_t *wq,
+                            const uint8_t *w_scale, const uint16_t *bias, uint16_t *y, int64_t M,
+                            int64_t N, int64_t K, void *workspace, size_t workspace_bytes,
+                            void *stream);
+size_t w8a8_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/* A key/value cache is uint8 [pages][2][heads][head bytes], 16-byte aligned: for each page,
+ * keys then values, and key/value head, the codes of the page's `page` tokens (dim elements
+ * each, e4m3 for W8A8_KV_FP8, e2m1 for W8A8_KV_FP4), then their scales (dim / 32 bytes each).
+ * page is a multiple of 16 up to W8A8_KV_MAX_PAGE; dim 64, 128, 192 or 256; heads 1 to
+ * W8A8_KV_MAX_HEADS (else W8A8_ERR_ARG). w8a8_kv_page_bytes is the size of a page, all heads,
+ * keys and values, or -1 for arguments out of range. */
+#define W8A8_KV_FP8 0
+#define W8A8_KV_FP4 1
+#define W8A8_KV_MAX_PAGE 4096
+#define W8A8_KV_MAX_HEADS 1024
+int64_t w8a8_kv_page_bytes(int page, int heads, int dim, int fmt);
+
+/* Quantizes keys and values k, v [T, heads, dim] (bf16; strides of token and head in elements,
+ * dim contiguous) into the slots [T] of the cache: slot s is token s % page of page s / page.
+ * Slots below 0 or past the cache are padding and not written. No two tokens of a call may
+ * have the same slot. */
+w8a8_status w8a8_kv_write(uint8_t *cache, int64_t pages, int page, int heads, int dim, int fmt,
+                          const uint16_t *k, int64_t k_token, int64_t k_head, const uint16_t *v,
+                          int64_t v_token, int64_t v_head, const int64_t *slots, int64_t T,
+                          void *stream);
+
+/* What the slots hold, as bf16 k, v [T, heads, dim] (contiguous); zeros for padding. */
+w8a8_status w8a8_kv_read(const uint8_t *cache, int64_t pages, int page, int heads, int dim,
+                         int fmt, const int64_t *slots, int64_t T, uint16_t *k, uint16_t *v,
+                         void *stream);
+
+/* Attention of queries q [T, heads * group, dim] (bf16, strides in elements) over the cache;
+ * query head h reads key/value head h / group. Sequence b of `seqs` has queries q_starts[b] ..
+ * q_starts[b + 1] - 1 (q_starts [seqs + 1] ascending from 0 to T; NULL: T / seqs each) and
+ * kv_lens[b] cached tokens, token j in page table[b * table_stride + j / page]. Its lq queries
+ * belong to its last lq tokens: query i sees the tokens j < kv_lens[b], with causal = 1 those
+ * with j <= kv_lens[b] - lq + i.
+ *   out [T, heads * group, dim] = sum_j p_j v_j / sum_j p_j, p_j = exp(scale * q.k_j - max),
+ * and zeros where a query sees no token. What lies in the cache past kv_lens[b], or is hidden
+ * from a query, has no effect on it, NaN included. Scores and sums are float32; the weights
+ * p_j are rounded to bf16 for the matrix cores.
+ * max_q and max_kv are bounds on a sequence's queries and tokens that the launch is laid out
+ * for; with other values the results are the same (table_pages * page bounds the tokens).
+ * Table entries that are read have to lie inside the cache: others read some page of it.
+ * workspace: w8a8_kv_attention_workspace_bytes(...) bytes, 256-byte aligned. */
+w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
+                              const uint8_t *cache, int64_t pages, int page, int heads, int dim,
+                              int fmt, const int32_t *table, int64_t table_stride,
+                              int table_pages, const int32_t *kv_lens, const int32_t *q_starts,
+                              int64_t T, int seqs, int group, float scale, int causal, int max_q,
+                              int max_kv, uint16_t *out, void *workspace, size_t workspace_bytes,
+                              void *stream);
+size_t w8a8_kv_attention_workspace_bytes(int page, int heads, int dim, int fmt, int group,
+                                         int64_t T, int seqs, int max_q, int max_kv);
+
 /* Static description of a status code. */
 const char *w8a8_status_string(w8a8_status status);
 

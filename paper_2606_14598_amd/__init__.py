@@ -19,7 +19,15 @@ takes col_mul (SmoothQuant's s, folded into W before quantization).
 The method is Section 3 of the paper ("The quantization recipe (reused)", "The fused
 kernel"): per-channel int8 weights, per-token dynamic int8 activations, an int8 x int8
 -> int32 product, and an epilogue that applies sx[m] * sw[n] and the bias off the
-int32 accumulator. If the library is missing, every call raises: there is no fallback.
+int32 accumulator.
+
+Beside the int8 linear there are microscaled operators (mx.py): 4-bit linears, a quantized
+key/value cache and the attention over it:
+
+  mx4_quantize, mx4_dequantize, mx4_gemm, mx4_linear
+  kv_cache, kv_write, kv_read, kv_attention
+
+If the library is missing, every call raises: there is no fallback.
 """
 from __future__ import annotations
 
@@ -94,6 +102,18 @@ def load_library():
         "w8a8_mfma_ceiling_ops": ([I64], I64),
         "w8a8_mfma_ceiling": ([P, P, I64, I64, I64, I64, P, P], INT),
         "w8a8_read_ceiling": ([P, I64, P, P], INT),
+        "w8a8_mx4_quantize": ([P, I64, I64, INT, P, P, P, P], INT),
+        "w8a8_mx4_dequantize": ([P, P, I64, I64, P, P], INT),
+        "w8a8_mx4_gemm": ([P, P, P, P, P, P, I64, I64, I64, P, SZ, P], INT),
+        "w8a8_mx4_gemm_workspace_bytes": ([I64, I64, I64], SZ),
+        "w8a8_mx4_linear": ([P, INT, P, P, P, P, P, I64, I64, I64, P, SZ, P], INT),
+        "w8a8_mx4_linear_workspace_bytes": ([I64, I64, I64], SZ),
+        "w8a8_kv_page_bytes": ([INT, INT, INT, INT], I64),
+        "w8a8_kv_write": ([P, I64, INT, INT, INT, INT, P, I64, I64, P, I64, I64, P, I64, P], INT),
+        "w8a8_kv_read": ([P, I64, INT, INT, INT, INT, P, I64, P, P, P], INT),
+        "w8a8_kv_attention": ([P, I64, I64, P, I64, INT, INT, INT, INT, P, I64, INT, P, P, I64, INT,
+                               INT, ctypes.c_float, INT, INT, INT, P, P, SZ, P], INT),
+        "w8a8_kv_attention_workspace_bytes": ([INT, INT, INT, INT, INT, I64, INT, INT, INT], SZ),
     }
     for name, (args, res) in sigs.items():
         f = getattr(lib, name)
@@ -456,3 +476,10 @@ def read_ceiling(buf: torch.Tensor, *, out=None):
         raise ValueError(f"out needs {READ_BLOCKS} entries on buf's device")
     _launch(buf.device, "w8a8_read_ceiling", _ptr(buf), nbytes, _ptr(sums))
     return sums
+
+
+from .mx import (KV_FORMATS, MX4_MAX_K, kv_attention, kv_cache, kv_read, kv_write,  # noqa: E402
+                 mx4_dequantize, mx4_gemm, mx4_linear, mx4_quantize)
+
+__all__ += ["mx4_quantize", "mx4_dequantize", "mx4_gemm", "mx4_linear", "kv_cache", "kv_write",
+            "kv_read", "kv_attention", "KV_FORMATS", "MX4_MAX_K"]

@@ -30,7 +30,8 @@ FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++20", "-fPIC", "-fvisibility=h
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-command-line-argument"]
 
-SOURCES = ["quant_rows.hip", "gemm_i8.hip", "mfma_ceiling.hip", "w8a8_api.hip"]
+SOURCES = ["quant_rows.hip", "gemm_i8.hip", "mfma_ceiling.hip", "w8a8_api.hip", "mx4_quant.hip",
+           "mx4_gemm.hip", "kv_cache.hip", "kv_attention.hip", "mx_api.hip"]
 
 
 def _compile(src: str, extra: list[str]) -> str:

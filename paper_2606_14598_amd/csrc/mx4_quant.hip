@@ -1,0 +1,164 @@
+// Microscaled 4-bit quantization of a matrix and back.
+//
+// mx4_quantize: v[r][k] = T(x[r][k]) * c[k] (T the identity or GELU, c the SmoothQuant
+// multiplier or absent; float32, or the bf16 inputs themselves where neither is there) in
+// blocks of 32 channels by the rule of mx_math.hpp. Codes [R, 16 ceil(K/32)], scales
+// [ceil(K/256), R, 8]: the scale bytes of 256 channels of neighbouring rows side by side, so
+// that the product reads a tile's scales of one K-panel as one piece of memory.
+//
+// Bound by memory: 2 bytes read and 17/32 written per element.
+#include "gelu.hpp"
+#include "mx_internal.hpp"
+#include "mx_math.hpp"
+
+namespace w8a8 {
+namespace {
+
+using namespace mx;
+
+// A lane holds 8 neighbouring channels, four lanes a block, a wavefront 512 channels (two
+// scale panels) of one row at a time; it takes ROWS rows one below the other, whose scale
+// bytes are neighbours in memory. No value outside a block matters to it, so nothing is
+// exchanged but the block's maximum inside its four lanes.
+constexpr int kRows = 4, kWaves = 4;
+
+// 8 bf16 values of row `row` (K of them) from channel k, zeros behind K. Any alignment.
+__device__ __forceinline__ void load8(const uint16_t *row, int64_t k, int64_t K,
+                                      uint32_t (&w)[4]) {
+    if (k + 8 <= K) {
+        const Bytes16 b = *reinterpret_cast<const Bytes16 *>(row + k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = b.w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = k + 2 * i < K ? row[k + 2 * i] : 0;
+            const uint32_t hi = k + 2 * i + 1 < K ? row[k + 2 * i + 1] : 0;
+            w[i] = lo | hi << 16;
+        }
+    }
+}
+
+// Largest of v over the four lanes of a block.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
+}
+
+template <int ACT, bool CM>
+__global__ void __launch_bounds__(kWaves * 64)
+mx4_quant_kernel(const uint16_t *x, int64_t R, int64_t K, const float *col_mul, uint8_t *codes,
+                 uint8_t *scales, int64_t chunks) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t chunk = blockIdx.x % chunks;                  // 512 channels
+    const int64_t r0 = (blockIdx.x / chunks * kWaves + wave) * kRows;
+    const int64_t k = chunk * 512 + lane * 8;
+    const int64_t row_bytes = (K + 31) / 32 * 16;
+    const int64_t panel = chunk * 2 + (lane >> 5);
+    const bool store_codes = k / 2 < row_bytes, store_scale = panel * 256 < K && lane % 4 == 0;
+    float c[8];
+    if constexpr (CM) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            c[e] = k + e < K ? col_mul[k + e] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t r = r0 + i;
+        if (r >= R)
+            return;
+        uint32_t w[4];
+        load8(x + r * K, k, K, w);
+        uint32_t byte, q;
+        if constexpr (ACT == ACT_NONE && !CM) {
+            uint32_t m = max_halves(max_halves(magnitudes(w[0]), magnitudes(w[1])),
+                                    max_halves(magnitudes(w[2]), magnitudes(w[3])));
+            m = quad_max(max(m & 0xFFFFu, m >> 16));
+            byte = scale_byte<kTop4>(m >> 7);
+            q = encode4_bf16(w, scale_operand(byte));
+        } else {
+            float v[8];
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float f = bf16_to_f32((w[e / 2] >> (16 * (e & 1))) & 0xFFFFu);
+                v[e] = ACT == ACT_GELU ? gelu_f32(f) : f;
+                if constexpr (CM)
+                    v[e] *= c[e];
+                m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+            }
+            m = quad_max(m);
+            byte = scale_byte<kTop4>(m >> 23);
+            q = encode4_f32(v, scale_operand(byte));
+        }
+        if (byte == kNaNScale)
+            q = 0;
+        if (store_codes)
+            *reinterpret_cast<uint32_t *>(codes + r * row_bytes + k / 2) = q;
+        if (store_scale)
+            scales[(panel * R + r) * 8 + (lane >> 2) % 8] = (uint8_t)byte;
+    }
+}
+
+// One lane decodes 8 channels.
+__global__ void __launch_bounds__(256)
+mx4_dequant_kernel(const uint8_t *codes, const uint8_t *scales, int64_t R, int64_t K, uint16_t *y,
+                   int64_t per_row) {
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = t / per_row, k = t % per_row * 8;
+    if (r >= R)
+        return;
+    const uint32_t q = *reinterpret_cast<const uint32_t *>(codes + r * ((K + 31) / 32 * 16) + k / 2);
+    const float s = scale_operand(scales[((k >> 8) * R + r) * 8 + ((k >> 5) & 7)]);
+    const uint32_t w[4] = {decode4<0>(q, s), decode4<1>(q, s), decode4<2>(q, s), decode4<3>(q, s)};
+    uint16_t *o = y + r * K + k;
+    if (k + 8 <= K) {
+        Bytes16 b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            b.w[i] = w[i];
+        *reinterpret_cast<Bytes16 *>(o) = b;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (k + e < K)
+                o[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+    }
+}
+
+}  // namespace
+
+hipError_t launch_mx4_quant(const uint16_t *x, int64_t R, int64_t K, int act,
+                            const float *col_mul, uint8_t *codes, uint8_t *scales,
+                            hipStream_t s) {
+    if (R == 0 || K == 0)
+        return hipSuccess;
+    const int64_t chunks = (K + 511) / 512;
+    const int64_t blocks = chunks * ((R + kWaves * kRows - 1) / (kWaves * kRows));
+    if (blocks > 0x7FFFFFFF)
+        return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks), block(kWaves * 64);
+    const auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, block, 0, s, x, R, K, col_mul, codes, scales, chunks);
+        return hipGetLastError();
+    };
+    if (act == ACT_GELU)
+        return col_mul ? go(mx4_quant_kernel<ACT_GELU, true>) : go(mx4_quant_kernel<ACT_GELU, false>);
+    return col_mul ? go(mx4_quant_kernel<ACT_NONE, true>) : go(mx4_quant_kernel<ACT_NONE, false>);
+}
+
+hipError_t launch_mx4_dequant(const uint8_t *codes, const uint8_t *scales, int64_t R, int64_t K,
+                              uint16_t *y, hipStream_t s) {
+    if (R == 0 || K == 0)
+        return hipSuccess;
+    const int64_t per_row = (K + 7) / 8;
+    const int64_t blocks = (R * per_row + 255) / 256;
+    if (blocks > 0x7FFFFFFF)
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(mx4_dequant_kernel, dim3((unsigned)blocks), dim3(256), 0, s, codes, scales, R,
+                       K, y, per_row);
+    return hipGetLastError();
+}
+
+}  // namespace w8a8
