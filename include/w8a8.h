@@ -336,6 +336,7 @@ size_t w8a8_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 #define W8A8_KV_FP4 1
 #define W8A8_KV_MAX_PAGE 4096
 #define W8A8_KV_MAX_HEADS 1024
+#define W8A8_KV_MAX_TOKENS (1 << 26)   /* of a sequence: table_pages * page */
 int64_t w8a8_kv_page_bytes(int page, int heads, int dim, int fmt);
 
 /* Quantizes keys and values k, v [T, heads, dim] (bf16; strides of token and head in elements,
@@ -363,7 +364,8 @@ w8a8_status w8a8_kv_read(const uint8_t *cache, int64_t pages, int page, int head
  * from a query, has no effect on it, NaN included. Scores and sums are float32; the weights
  * p_j are rounded to bf16 for the matrix cores.
  * max_q and max_kv are bounds on a sequence's queries and tokens that the launch is laid out
- * for; with other values the results are the same (table_pages * page bounds the tokens).
+ * for; with other values the results are the same (table_pages * page bounds the tokens; it is
+ * at most W8A8_KV_MAX_TOKENS, else W8A8_ERR_SHAPE).
  * Table entries that are read have to lie inside the cache: others read some page of it.
  * workspace: w8a8_kv_attention_workspace_bytes(...) bytes, 256-byte aligned. */
 w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head,

@@ -218,7 +218,7 @@ w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head
         return W8A8_ERR_ARG;
     if (T < 0 || seqs < 0 || table_pages < 0 || table_stride < 0 || q_token < 0 || q_head < 0 ||
         max_q < 0 || max_kv < 0 || !product_ok(T, (int64_t)heads * group * dim) ||
-        (int64_t)table_pages * page > 0x7FFFFFFF)
+        (int64_t)table_pages * page > W8A8_KV_MAX_TOKENS)
         return W8A8_ERR_SHAPE;
     if (T == 0 || seqs == 0)
         return T == 0 ? W8A8_OK : W8A8_ERR_SHAPE;
