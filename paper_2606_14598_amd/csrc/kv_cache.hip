@@ -9,17 +9,11 @@
 // Four lanes hold a block, 8 values each; bound by memory.
 #include "mx_internal.hpp"
 #include "mx_math.hpp"
-#include "quant_math.hpp"
 
 namespace w8a8 {
 namespace {
 
 using namespace mx;
-
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
-    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
-}
 
 struct Place {
     int64_t t;        // token of the call

@@ -1,63 +1,626 @@
 // Microscaled 4-bit product: Y[m][n] = bf16(sum_k X[m][k] W[n][k] + b[n]) on the codes and
 // scale bytes of mx4_quant.hip, with float32 accumulation in the scaled matrix instructions.
+//
+// v_mfma_scale_f32_32x32x64 with e2m1 operands takes 16 bytes (a block of 32 elements) of one
+// row and its scale byte from every lane: lane l holds row l % 32 and K-half l / 32. A dot
+// product is unchanged by a permutation of K that both operands share, so inside a K-panel of
+// 256 channels (8 blocks, 128 bytes of codes a row) K-half h takes blocks 4h .. 4h + 3 in
+// steps 0 .. 3: the four scale bytes of a lane are then one word of the scales' layout, and
+// each step selects its byte of that word.
 #include "mx_internal.hpp"
 #include "mx_math.hpp"
+#include "quant_math.hpp"
+
+#include <algorithm>
+#include <utility>
 
 namespace w8a8 {
 namespace {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRsrcWord3 = 0x00020000;     // raw 32-bit buffer
+constexpr int kOOB = 0x7FFFFFF0;           // beyond any buffer: the load gives zero
+constexpr int kPanel = 128;                // bytes of codes of a row in a K-panel
 
 __device__ __forceinline__ i32x8 frag(i32x4 v) {
     return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
 }
 
-// One wavefront per 32 x 32 outputs, operands straight from memory.
-__global__ void __launch_bounds__(256)
-mx4_gemm_simple_kernel(Mx4Args a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t tiles_n = (a.N + 63) / 64;
-    const int64_t m0 = blockIdx.x / tiles_n * 64 + (wave & 1) * 32;
-    const int64_t n0 = blockIdx.x % tiles_n * 64 + (wave >> 1) * 32;
-    const int64_t m = m0 + (lane & 31), n = n0 + (lane & 31);
-    const int64_t mr = min(m, a.M - 1), nr = min(n, a.N - 1);
-    f32x16 acc = {};
-    for (int64_t b = lane >> 5; b - (lane >> 5) < a.nb; b += 2) {
-        i32x4 x = {}, w = {};
-        int sx = 0, sw = 0;
-        if (b < a.nb) {
-            x = *reinterpret_cast<const i32x4 *>(a.xq + (mr * a.nb + b) * 16);
-            w = *reinterpret_cast<const i32x4 *>(a.wq + (nr * a.nb + b) * 16);
-            sx = a.xs[((b >> 3) * a.M + mr) * 8 + (b & 7)];
-            sw = a.ws[((b >> 3) * a.N + nr) * 8 + (b & 7)];
-        }
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(w), frag(x), acc, 4, 4, 0, sw, 0,
-                                                              sx);
-    }
-    if (m >= a.M)
-        return;
+// XOR of the 16-byte chunk index inside an LDS row of 128 bytes: conflict-free both for the
+// direct-to-LDS writes (8 rows of 8 chunks) and for the fragment reads (32 rows, one chunk).
+__device__ __forceinline__ int swz(int row) { return (row & 7) ^ ((row >> 3) & 3); }
+
+__host__ __device__ constexpr int waitcnt_vm(int n) {
+    return (n & 0xF) | ((n >> 4) << 14) | (0x7 << 4) | (0xF << 8);
+}
+
+// Barrier without the fence of __syncthreads(), which would wait for all loads in flight.
+__device__ __forceinline__ void barrier_nofence() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+struct Mx4Params {
+    Mx4Args a;
+    int tiles_m, tiles_n, gm;   // tiles, token tiles per raster group
+    int splits, split_panels;   // K divided among workgroups: panels of each
+    int vec;                    // rows of y 16-byte aligned: N % 8 == 0 and y aligned
+    float *part;                // splits > 1: [splits][M][N]
+};
+
+// Tile (and K-range) of workgroup `bid`: each XCD takes every 8th workgroup and gets a
+// contiguous run of tiles, K-ranges outermost, in groups of gm token tiles.
+__device__ __forceinline__ void tile_of(int bid, const Mx4Params &p, int &tm, int &tn, int &split) {
+    const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.splits;
+    const int xcd = bid & 7, slot = bid >> 3, q = total >> 3, r = total & 7;
+    int t = xcd * q + min(xcd, r) + slot;
+    split = t / tiles;
+    t -= split * tiles;
+    const int per = p.gm * p.tiles_n, first = t / per * p.gm, in = t % per;
+    const int size = min(p.tiles_m - first, p.gm);
+    tm = first + in % size;
+    tn = in / size;
+}
+
+// One workgroup per TM tokens x TN channels; WM x WN wavefronts, S LDS stages of a K-panel:
+// codes of TN weight rows and TM token rows, then their scale words (8 bytes a row). Codes
+// and scales go from memory to LDS directly; what lies past a matrix reads as zero codes and
+// zero scales. Panel k + S - 1 is requested while panel k is multiplied.
+template <int TM, int TN, int WM, int WN, int S>
+__global__ void __launch_bounds__(WM *WN * 64)
+mx4_gemm_kernel(Mx4Params p) {
+    constexpr int NW = WM * WN;
+    constexpr int WTM = TM / WM, WTN = TN / WN, FM = WTM / 32, FN = WTN / 32;
+    constexpr int ROWS = TN + TM;
+    constexpr int CODES = ROWS * kPanel, STAGE = CODES + ROWS * 8;
+    // A wavefront's loads of a panel: 8 rows of codes each, then SR rows of scales each.
+    constexpr int IW = TN / 8 / NW, IX = TM / 8 / NW;
+    constexpr int SB = ROWS * 8 == NW * 1024 ? 16 : 4, SR = 64 * SB / 8, IS = ROWS / SR / NW;
+    constexpr int NV = IW + IX + IS;
+    static_assert(WTM % 32 == 0 && WTN % 32 == 0, "tile");
+    static_assert(TN % (8 * NW) == 0 && TM % (8 * NW) == 0 && NW % 4 == 0, "code loads");
+    static_assert(ROWS % (SR * NW) == 0 && TN % SR == 0, "scale loads");
+    static_assert(S >= 2 && (S - 1) * NV <= 63, "loads in flight");
+    constexpr int RS = 2 * WTN + 16;       // output staging: bytes of a token's row
+    static_assert(NW * 32 * RS + TN * 4 <= S * STAGE && S * STAGE <= 163840, "LDS");
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[S * STAGE];
+
+    const Mx4Args &a = p.a;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+    int tm, tn, split;
+    tile_of(blockIdx.x, p, tm, tn, split);
+    const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * TN;
+    const int rows_x = (int)min(a.M - m0, (int64_t)TM), rows_w = (int)min(a.N - n0, (int64_t)TN);
+    const int row_bytes = (int)a.nb * 16;
+    const int first_panel = split * p.split_panels;
+    const int nk = min((int)((a.nb + 7) / 8) - first_panel, p.split_panels);
+    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(
+        (void *)(a.wq + n0 * row_bytes), (short)0, rows_w * row_bytes, kRsrcWord3);
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
+        (void *)(a.xq + m0 * row_bytes), (short)0, rows_x * row_bytes, kRsrcWord3);
+
+    f32x16 acc[FN][FM];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int64_t c = n0 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-        if (c < a.N) {
-            const float b = a.bias ? __uint_as_float((uint32_t)a.bias[c] << 16) : 0.0f;
-            a.y[m * a.N + c] = __builtin_bit_cast(uint16_t, (__bf16)(acc[i] + b));
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j)
+            acc[i][j] = f32x16{};
+
+    // Codes: load i of this wavefront fills rows 8 (i NW + wave) + lane / 8, physical chunk
+    // lane % 8, and so fetches chunk (lane % 8) ^ swz(row), the same for all i as NW % 4 == 0.
+    const int lrow = wave * 8 + (lane >> 3);
+    const int lchunk = ((lane & 7) ^ swz(lrow)) << 4;
+    // Scales: load i fills SR rows from (i NW + wave) SR of the stage's scale words.
+    const uint8_t *sbase[IS];
+    int64_t sstep[IS];
+    int sbytes[IS];
+#pragma unroll
+    for (int i = 0; i < IS; ++i) {
+        const int row = (i * NW + wave) * SR;
+        const bool w = row < TN;
+        const int left = w ? rows_w - row : rows_x - (row - TN);
+        sstep[i] = (w ? a.N : a.M) * 8;
+        sbase[i] = (w ? a.ws + (n0 + row) * 8 : a.xs + (m0 + row - TN) * 8) + first_panel * sstep[i];
+        sbytes[i] = max(left, 0) * 8;
+    }
+    // Where panel kt's codes start for this lane; beyond the buffers past the last panel and
+    // past the rows' ends.
+    const auto codes_at = [&](int kt) {
+        const int k = (first_panel + kt) * kPanel + lchunk;
+        return kt < nk && k < row_bytes ? lrow * row_bytes + k : kOOB;
+    };
+    const auto issue = [&](auto ic, int kt, int at, int so) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (i < IW + IX) {
+            constexpr int q = i < IW ? i : i - IW;
+            uint8_t *dst = smem + so + (i * NW + wave) * 1024;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                i < IW ? rw : rx, (__attribute__((address_space(3))) void *)dst, 16,
+                at + q * NW * 8 * row_bytes, 0, 0, 0);
+        } else {
+            constexpr int q = i - IW - IX;
+            const bool in = kt < nk;       // past the last panel: an empty buffer
+            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                (void *)(sbase[q] + (in ? kt : 0) * sstep[q]), (short)0, in ? sbytes[q] : 0, kRsrcWord3);
+            uint8_t *dst = smem + so + CODES + (q * NW + wave) * 64 * SB;
+            if constexpr (SB == 16)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    rs, (__attribute__((address_space(3))) void *)dst, 16, lane * 16, 0, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    rs, (__attribute__((address_space(3))) void *)dst, 4, lane * 4, 0, 0, 0);
+        }
+    };
+
+    // Fragment reads: lane (r, h) of step s takes chunk 4h + s of its row.
+    int fofs[4];
+    {
+        const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            fofs[s] = r * kPanel + (((4 * h + s) ^ swz(r)) << 4);
+    }
+    const int sofs = (lane & 31) * 8 + (lane >> 5) * 4;
+    i32x4 fa[2][FN], fb[2][FM];
+    int sa[FN], sb[FM];
+
+    // Step s of the panel at so: its MFMAs, between them the reads of step s + 1 and the
+    // panel's share of the loads of panel kt + S - 1.
+    constexpr int NM = FN * FM, NR = FN + FM;
+    const auto read_frag = [&](int q, int so, int s) __attribute__((always_inline)) {
+        if (q < FN)
+            fa[s & 1][q] = *reinterpret_cast<const i32x4 *>(smem + so + (wn * WTN + q * 32) * kPanel +
+                                                            fofs[s]);
+        else
+            fb[s & 1][q - FN] = *reinterpret_cast<const i32x4 *>(
+                smem + so + (TN + wm * WTM + (q - FN) * 32) * kPanel + fofs[s]);
+    };
+    // With two stages all loads go out in the first step, else a quarter in each.
+    constexpr int VPS = S == 2 ? NV : (NV + 3) / 4;
+    const auto step = [&](auto sc, int so, int kt, int at, int so_load) __attribute__((always_inline)) {
+        constexpr int s = decltype(sc)::value;
+        constexpr int nr = s < 3 ? NR : 0;
+        constexpr int va = s * VPS < NV ? s * VPS : NV, vb = va + VPS < NV ? va + VPS : NV;
+        constexpr int nops = nr + vb - va, steps = NM > nops ? NM : nops;
+        [&]<int... q>(std::integer_sequence<int, q...>) __attribute__((always_inline)) {
+            ([&]() __attribute__((always_inline)) {
+                if constexpr (q < nr)
+                    read_frag(q, so, s + 1);
+                else if constexpr (q < nops)
+                    issue(std::integral_constant<int, va + q - nr>{}, kt, at, so_load);
+                if constexpr (q < NM) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    acc[q / FM][q % FM] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                        frag(fa[s & 1][q / FM]), frag(fb[s & 1][q % FM]), acc[q / FM][q % FM], 4, 4, s,
+                        sa[q / FM], s, sb[q % FM]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }(), ...);
+        }(std::make_integer_sequence<int, steps>{});
+    };
+
+    if (nk > 0) {
+#pragma unroll
+        for (int k = 0; k < S - 1; ++k)
+            [&]<int... i>(std::integer_sequence<int, i...>) __attribute__((always_inline)) {
+                (issue(std::integral_constant<int, i>{}, k, codes_at(k), k * STAGE), ...);
+            }(std::make_integer_sequence<int, NV>{});
+        int st = 0, ld = S - 1;
+        for (int kt = 0; kt < nk; ++kt) {
+            // Panel kt has landed once at most the S - 2 younger ones are in flight; every
+            // wavefront has then read the stage that the next loads go to.
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm((S - 2) * NV));
+            barrier_nofence();
+            const int so = st * STAGE;
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+                sa[i] = *reinterpret_cast<const int *>(smem + so + CODES + (wn * WTN + i * 32) * 8 + sofs);
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+                sb[j] = *reinterpret_cast<const int *>(smem + so + CODES +
+                                                       (TN + wm * WTM + j * 32) * 8 + sofs);
+#pragma unroll
+            for (int q = 0; q < NR; ++q)
+                read_frag(q, so, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            const int kl = kt + S - 1, lo = ld * STAGE, at = codes_at(kl);
+            step(std::integral_constant<int, 0>{}, so, kl, at, lo);
+            step(std::integral_constant<int, 1>{}, so, kl, at, lo);
+            step(std::integral_constant<int, 2>{}, so, kl, at, lo);
+            step(std::integral_constant<int, 3>{}, so, kl, at, lo);
+            st = st + 1 == S ? 0 : st + 1;
+            ld = ld + 1 == S ? 0 : ld + 1;
+        }
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    }
+
+    const int64_t mw = m0 + wm * WTM, nw = n0 + wn * WTN;
+    const int r = lane & 31, h = lane >> 5;
+    if (p.splits > 1) {
+        // Lane (r, h) of fragment (i, j): token 32j + r, channels 32i + 8g + 4h + 0 .. 3.
+        float *out = p.part + (int64_t)split * a.M * a.N;
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+            const int64_t m = mw + j * 32 + r;
+            if (m >= a.M)
+                continue;
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int64_t n = nw + i * 32 + g * 8 + h * 4;
+                    float *o = out + m * a.N + n;
+                    if (n + 4 <= a.N && a.N % 4 == 0) {
+                        *reinterpret_cast<f32x4 *>(o) =
+                            f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                                  acc[i][j][4 * g + 3]};
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (n + e < a.N)
+                                o[e] = acc[i][j][4 * g + e];
+                    }
+                }
+        }
+        return;
+    }
+
+    // Output: 32 tokens at a time through the wavefront's own piece of LDS (free now), so
+    // that stores are whole 16-byte pieces of rows.
+    barrier_nofence();
+    constexpr int CPR = WTN / 8, RPQ = 64 / CPR, NQ = (32 + RPQ - 1) / RPQ;
+    uint8_t *const region = smem + wave * 32 * RS;
+    float *const bias = reinterpret_cast<float *>(smem + NW * 32 * RS);
+    for (int i = threadIdx.x; i < TN; i += NW * 64)
+        bias[i] = a.bias && n0 + i < a.N ? __uint_as_float((uint32_t)a.bias[n0 + i] << 16) : 0.0f;
+    __syncthreads();
+    const int row0 = lane / CPR, ch = lane % CPR;
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 b =
+                    *reinterpret_cast<const f32x4 *>(bias + wn * WTN + i * 32 + g * 8 + h * 4);
+                uint16_t v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = __builtin_bit_cast(uint16_t, (__bf16)(acc[i][j][4 * g + e] + b[e]));
+                *reinterpret_cast<uint2 *>(region + r * RS + (i * 32 + g * 8 + h * 4) * 2) =
+                    make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
+            }
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const int row = row0 + q * RPQ;
+            const int64_t m = mw + j * 32 + row, n = nw + ch * 8;
+            if (row0 >= RPQ || row >= 32 || m >= a.M || n >= a.N)
+                continue;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(region + row * RS + ch * 16);
+            uint16_t *o = a.y + m * a.N + n;
+            if (p.vec) {
+                __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(o));
+            } else if (n + 8 <= a.N) {
+                *reinterpret_cast<Bytes16 *>(o) = __builtin_bit_cast(Bytes16, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (n + e < a.N)
+                        o[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+            }
         }
     }
 }
 
-}  // namespace
+// Sums the K-ranges in order and adds the bias: four outputs a thread where rows allow.
+template <bool VEC>
+__global__ void __launch_bounds__(256)
+mx4_reduce_kernel(Mx4Params p) {
+    const Mx4Args &a = p.a;
+    const int64_t MN = a.M * a.N, t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * (VEC ? 4 : 1);
+    if (t >= MN)
+        return;
+    const int64_t n = t % a.N;
+    if constexpr (VEC) {
+        f32x4 v = *reinterpret_cast<const f32x4 *>(p.part + t);
+        for (int s = 1; s < p.splits; ++s)
+            v += *reinterpret_cast<const f32x4 *>(p.part + s * MN + t);
+        uint16_t y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float b = a.bias ? __uint_as_float((uint32_t)a.bias[n + e] << 16) : 0.0f;
+            y[e] = __builtin_bit_cast(uint16_t, (__bf16)(v[e] + b));
+        }
+        Bytes8 o;
+        o.w[0] = y[0] | (uint32_t)y[1] << 16;
+        o.w[1] = y[2] | (uint32_t)y[3] << 16;
+        *reinterpret_cast<Bytes8 *>(a.y + t) = o;
+    } else {
+        float v = p.part[t];
+        for (int s = 1; s < p.splits; ++s)
+            v += p.part[s * MN + t];
+        const float b = a.bias ? __uint_as_float((uint32_t)a.bias[n] << 16) : 0.0f;
+        a.y[t] = __builtin_bit_cast(uint16_t, (__bf16)(v + b));
+    }
+}
 
-size_t mx4_gemm_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
+// Few tokens: bound by reading W once, so nothing of it is staged. A workgroup owns 16 FNB
+// channels and 16 FMB tokens; its NW wavefronts take K in turn, 512 channels (256 bytes, 16
+// blocks) at a time, with the next 512 channels' loads in flight. v_mfma_scale_f32_16x16x128:
+// lane (r, g) = (lane % 16, lane / 16) holds row r; in step s of four it takes block 4s + g, so
+// that a load instruction reads whole 64-byte pieces of rows, and byte g of a scale word.
+// The wavefronts' sums meet in LDS, added in their order.
+//
+// QX: the tokens are bf16 rows (times col_mul where there is one), and a lane quantizes its
+// block itself before multiplying: blocks need nothing of their row, and a workgroup's
+// wavefronts share no block, so the whole linear is this one launch.
+template <int FMB, int FNB, int NW, bool QX, bool CM>
+__global__ void __launch_bounds__(NW * 64)
+mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul) {
+    using namespace mx;
+    __shared__ f32x4 red[NW][FNB][FMB][64];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int64_t tiles_n = (a.N + 16 * FNB - 1) / (16 * FNB);
+    const int64_t n0 = blockIdx.x % tiles_n * (16 * FNB), m0 = blockIdx.x / tiles_n * (16 * FMB);
+    const int nb = (int)a.nb, panels = (nb + 7) / 8;
 
-hipError_t launch_mx4_gemm(const Mx4Args &a, void *, size_t, hipStream_t s) {
-    const int64_t blocks = ((a.M + 63) / 64) * ((a.N + 63) / 64);
+    // Rows past the matrix repeat the last one; their results are not stored.
+    const uint8_t *wrow[FNB], *wscale[FNB];
+#pragma unroll
+    for (int c = 0; c < FNB; ++c) {
+        const int64_t n = min(n0 + c * 16 + r, a.N - 1);
+        wrow[c] = a.wq + n * nb * 16;
+        wscale[c] = a.ws + n * 8;
+    }
+    const auto word = [&](const uint8_t *scales, int64_t rows, int panel, int s) {
+        return panel < panels
+                   ? *reinterpret_cast<const uint32_t *>(scales + panel * rows * 8 + 4 * (s & 1))
+                   : 0u;
+    };
+    f32x4 acc[FNB][FMB];
+#pragma unroll
+    for (int c = 0; c < FNB; ++c)
+#pragma unroll
+        for (int b = 0; b < FMB; ++b)
+            acc[c][b] = f32x4{};
+
+    i32x4 w[FNB][4];
+    uint32_t sw[FNB][4];
+    const auto load = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < FNB; ++c)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int blk = 16 * j + 4 * s + g;
+                w[c][s] = blk < nb ? *reinterpret_cast<const i32x4 *>(wrow[c] + (int64_t)blk * 16)
+                                   : i32x4{};
+                sw[c][s] = word(wscale[c], a.N, 2 * j + s / 2, s);
+            }
+    };
+    const int steps = (nb + 15) / 16;
+    if (wave < steps)
+        load(wave);
+    for (int j = wave; j < steps; j += NW) {
+        i32x4 fx[FMB][4];
+        int sx[FMB][4];
+#pragma unroll
+        for (int b = 0; b < FMB; ++b) {
+            const int64_t m = m0 + b * 16 + r;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int blk = 16 * j + 4 * s + g;
+                const bool in = m < a.M && blk < nb;
+                fx[b][s] = i32x4{};
+                sx[b][s] = 0;
+                if constexpr (!QX) {
+                    if (in) {
+                        fx[b][s] = *reinterpret_cast<const i32x4 *>(a.xq + (m * nb + blk) * 16);
+                        sx[b][s] = a.xs[((int64_t)(blk >> 3) * a.M + m) * 8 + (blk & 7)];
+                    }
+                } else if (in) {
+                    const uint16_t *src = x + m * K + (int64_t)blk * 32;
+                    const int64_t left = K - (int64_t)blk * 32;
+                    uint32_t v[4][4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        load8(src, 8 * q, left, v[q]);
+                    if constexpr (!CM) {
+                        uint32_t top = 0;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                top = max_halves(top, magnitudes(v[q][e]));
+                        const uint32_t byte = scale_byte<kTop4>(max(top & 0xFFFFu, top >> 16) >> 7);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            fx[b][s][q] = (int)encode4_bf16(v[q], scale_operand(byte));
+                        sx[b][s] = (int)byte;
+                    } else {
+                        float f[4][8];
+                        uint32_t top = 0;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int64_t k = (int64_t)blk * 32 + 8 * q + e;
+                                f[q][e] = qmath::bf16_to_f32((v[q][e / 2] >> (16 * (e & 1))) & 0xFFFFu) *
+                                          (k < K ? col_mul[k] : 0.0f);
+                                top = max(top, __float_as_uint(f[q][e]) & 0x7FFFFFFFu);
+                            }
+                        const uint32_t byte = scale_byte<kTop4>(top >> 23);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            fx[b][s][q] = (int)encode4_f32(f[q], scale_operand(byte));
+                        sx[b][s] = (int)byte;
+                    }
+                }
+            }
+        }
+        i32x4 wc[FNB][4];
+        uint32_t sc[FNB][4];
+#pragma unroll
+        for (int c = 0; c < FNB; ++c)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                wc[c][s] = w[c][s];
+                sc[c][s] = sw[c][s] >> (8 * g);
+            }
+        if (j + NW < steps)
+            load(j + NW);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int c = 0; c < FNB; ++c)
+#pragma unroll
+                for (int b = 0; b < FMB; ++b)
+                    acc[c][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        frag(wc[c][s]), frag(fx[b][s]), acc[c][b], 4, 4, 0, (int)sc[c][s], 0, sx[b][s]);
+    }
+#pragma unroll
+    for (int c = 0; c < FNB; ++c)
+#pragma unroll
+        for (int b = 0; b < FMB; ++b)
+            red[wave][c][b][lane] = acc[c][b];
+    __syncthreads();
+    // Lane (r, g) of a fragment holds token r, channels 4g .. 4g + 3.
+    for (int i = threadIdx.x; i < FNB * FMB * 64; i += NW * 64) {
+        const int l = i & 63, b = (i >> 6) % FMB, c = (i >> 6) / FMB;
+        f32x4 v = red[0][c][b][l];
+#pragma unroll
+        for (int k = 1; k < NW; ++k)
+            v += red[k][c][b][l];
+        const int64_t m = m0 + b * 16 + (l & 15), n = n0 + c * 16 + (l >> 4) * 4;
+        if (m >= a.M)
+            continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < a.N) {
+                const float bias = a.bias ? __uint_as_float((uint32_t)a.bias[n + e] << 16) : 0.0f;
+                a.y[m * a.N + n + e] = __builtin_bit_cast(uint16_t, (__bf16)(v[e] + bias));
+            }
+    }
+}
+
+// ---------------------------------------------------------------- what runs for a shape
+
+enum Tile : int { T256x256, T128x128, T64x64, kTiles };
+struct TileSize {
+    int tm, tn;
+};
+constexpr TileSize kTile[kTiles] = {{256, 256}, {128, 128}, {64, 64}};
+constexpr int kCus = 256;
+constexpr int kStreamTokens = 64;     // the streaming kernel up to here
+
+struct Plan {
+    int tile, splits;
+};
+
+Plan plan_of(int64_t M, int64_t N, int64_t nb) {
+    const int64_t panels = (nb + 7) / 8;
+    Plan best = {T256x256, 1};
+    for (int t = kTiles - 1; t >= 0; --t) {
+        const int64_t tiles = ((M + kTile[t].tm - 1) / kTile[t].tm) * ((N + kTile[t].tn - 1) / kTile[t].tn);
+        if (t == 0 || tiles <= 2 * kCus) {
+            best.tile = t;
+            if (t > 0 && tiles * 2 > kCus)
+                best.splits = 1;
+            else if (t > 0)
+                best.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kCus / tiles, panels / 4, 16}));
+            break;
+        }
+    }
+    return best;
+}
+
+template <int TM, int TN, int WM, int WN, int S>
+hipError_t run_tile(Mx4Params p, hipStream_t s) {
+    p.tiles_m = (int)((p.a.M + TM - 1) / TM);
+    p.tiles_n = (int)((p.a.N + TN - 1) / TN);
+    p.gm = 8;
+    const int64_t blocks = (int64_t)p.tiles_m * p.tiles_n * p.splits;
     if (blocks > 0x7FFFFFFF)
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL(mx4_gemm_simple_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((mx4_gemm_kernel<TM, TN, WM, WN, S>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0,
+                       s, p);
     return hipGetLastError();
+}
+
+template <bool QX, bool CM>
+hipError_t run_stream(const Mx4Args &a, const uint16_t *x, int64_t K, const float *cm, hipStream_t s) {
+    const auto go = [&](auto kernel, int64_t tokens, int64_t channels, int waves) {
+        const int64_t blocks =
+            ((a.M + tokens - 1) / tokens) * ((a.N + channels - 1) / channels);
+        if (blocks > 0x7FFFFFFF)
+            return hipErrorInvalidValue;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), 0, s, a, x, K, cm);
+        return hipGetLastError();
+    };
+    if (a.M <= 16)
+        return a.N >= 8192 ? go(mx4_stream_kernel<1, 2, 8, QX, CM>, 16, 32, 8)
+                           : go(mx4_stream_kernel<1, 1, 8, QX, CM>, 16, 16, 8);
+    if constexpr (!QX) {
+        if (a.M <= 32)
+            return go(mx4_stream_kernel<2, 1, 8, QX, CM>, 32, 16, 8);
+        return go(mx4_stream_kernel<4, 1, 8, QX, CM>, 64, 16, 8);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+size_t mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t nb) {
+    if (M <= kStreamTokens)
+        return 0;
+    const Plan p = plan_of(M, N, nb);
+    return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0;
+}
+
+hipError_t launch_mx4_gemm(const Mx4Args &a, void *ws, hipStream_t s) {
+    if (a.M <= kStreamTokens)
+        return run_stream<false, false>(a, nullptr, 0, nullptr, s);
+    const Plan plan = plan_of(a.M, a.N, a.nb);
+    const int64_t panels = (a.nb + 7) / 8;
+    Mx4Params p;
+    p.a = a;
+    p.split_panels = (int)((panels + plan.splits - 1) / plan.splits);
+    p.splits = p.split_panels > 0 ? (int)((panels + p.split_panels - 1) / p.split_panels) : 1;
+    p.vec = a.N % 8 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
+    p.part = static_cast<float *>(ws);
+    hipError_t e;
+    switch (plan.tile) {
+    case T256x256: e = run_tile<256, 256, 2, 2, 2>(p, s); break;
+    case T128x128: e = run_tile<128, 128, 2, 2, 4>(p, s); break;
+    default: e = run_tile<64, 64, 2, 2, 4>(p, s); break;
+    }
+    if (e != hipSuccess || p.splits <= 1)
+        return e;
+    const bool vec = a.N % 4 == 0;
+    const int64_t blocks = (a.M * a.N / (vec ? 4 : 1) + 255) / 256;
+    if (blocks > 0x7FFFFFFF)
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(vec ? mx4_reduce_kernel<true> : mx4_reduce_kernel<false>, dim3((unsigned)blocks),
+                       dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+bool mx4_linear_one_launch(int64_t M, int act) { return M <= 16 && act == ACT_NONE; }
+
+hipError_t launch_mx4_linear(const Mx4Args &a, const uint16_t *x, int64_t K, const float *col_mul,
+                             hipStream_t s) {
+    return col_mul ? run_stream<true, true>(a, x, K, col_mul, s)
+                   : run_stream<true, false>(a, x, K, col_mul, s);
 }
 
 }  // namespace w8a8

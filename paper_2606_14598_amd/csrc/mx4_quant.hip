@@ -22,30 +22,6 @@ using namespace mx;
 // exchanged but the block's maximum inside its four lanes.
 constexpr int kRows = 4, kWaves = 4;
 
-// 8 bf16 values of row `row` (K of them) from channel k, zeros behind K. Any alignment.
-__device__ __forceinline__ void load8(const uint16_t *row, int64_t k, int64_t K,
-                                      uint32_t (&w)[4]) {
-    if (k + 8 <= K) {
-        const Bytes16 b = *reinterpret_cast<const Bytes16 *>(row + k);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = b.w[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = k + 2 * i < K ? row[k + 2 * i] : 0;
-            const uint32_t hi = k + 2 * i + 1 < K ? row[k + 2 * i + 1] : 0;
-            w[i] = lo | hi << 16;
-        }
-    }
-}
-
-// Largest of v over the four lanes of a block.
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
-    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
-}
-
 template <int ACT, bool CM>
 __global__ void __launch_bounds__(kWaves * 64)
 mx4_quant_kernel(const uint16_t *x, int64_t R, int64_t K, const float *col_mul, uint8_t *codes,

@@ -34,9 +34,8 @@ w8a8_status check_product(int64_t M, int64_t N, int64_t K) {
     return K > W8A8_MX4_MAX_K ? W8A8_ERR_K_OVERFLOW : W8A8_OK;
 }
 
-w8a8_status run_gemm(const uint8_t *xq, const uint8_t *xs, const uint8_t *wq, const uint8_t *ws,
-                     const uint16_t *bias, uint16_t *y, int64_t M, int64_t N, int64_t K,
-                     void *work, size_t work_bytes, hipStream_t s) {
+Mx4Args product(const uint8_t *xq, const uint8_t *xs, const uint8_t *wq, const uint8_t *ws,
+                const uint16_t *bias, uint16_t *y, int64_t M, int64_t N, int64_t K) {
     Mx4Args a;
     a.xq = xq;
     a.xs = xs;
@@ -47,7 +46,7 @@ w8a8_status run_gemm(const uint8_t *xq, const uint8_t *xs, const uint8_t *wq, co
     a.M = M;
     a.N = N;
     a.nb = blocks_of(K);
-    return from_hip(launch_mx4_gemm(a, work, work_bytes, s));
+    return a;
 }
 
 bool cache_shape(KvShape &c, int64_t pages, int page, int heads, int dim, int fmt) {
@@ -118,8 +117,8 @@ w8a8_status w8a8_mx4_gemm(const uint8_t *xq, const uint8_t *x_scale, const uint8
     const size_t need = w8a8_mx4_gemm_workspace_bytes(M, N, K);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
         return W8A8_ERR_WORKSPACE;
-    return run_gemm(xq, x_scale, wq, w_scale, bias, y, M, N, K, workspace, workspace_bytes,
-                    as_stream(stream));
+    return from_hip(launch_mx4_gemm(product(xq, x_scale, wq, w_scale, bias, y, M, N, K), workspace,
+                                    as_stream(stream)));
 }
 
 size_t w8a8_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
@@ -145,13 +144,16 @@ w8a8_status w8a8_mx4_linear(const uint16_t *x, int act, const float *col_mul, co
     const size_t need = w8a8_mx4_linear_workspace_bytes(M, N, K);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
         return W8A8_ERR_WORKSPACE;
+    if (mx4_linear_one_launch(M, act))
+        return from_hip(launch_mx4_linear(product(nullptr, nullptr, wq, w_scale, bias, y, M, N, K), x, K,
+                                          col_mul, as_stream(stream)));
     uint8_t *xq = static_cast<uint8_t *>(workspace);
     uint8_t *xs = xq + align_up(code_bytes(M, K));
     uint8_t *rest = xs + align_up(scale_bytes(M, K));
     if (launch_mx4_quant(x, M, K, act, col_mul, xq, xs, as_stream(stream)) != hipSuccess)
         return W8A8_ERR_HIP;
-    return run_gemm(xq, xs, wq, w_scale, bias, y, M, N, K, rest,
-                    workspace_bytes - (size_t)(rest - xq), as_stream(stream));
+    return from_hip(launch_mx4_gemm(product(xq, xs, wq, w_scale, bias, y, M, N, K), rest,
+                                    as_stream(stream)));
 }
 
 int64_t w8a8_kv_page_bytes(int page, int heads, int dim, int fmt) {

@@ -10,8 +10,7 @@
 // values); the e4m3 one does not saturate, so its inputs are clamped first.
 #pragma once
 
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "quant_math.hpp"
 
 namespace w8a8 {
 namespace mx {
@@ -99,6 +98,30 @@ template <int SEL>
 __device__ __forceinline__ uint32_t decode8(uint32_t codes, float scale) {
     return __builtin_bit_cast(uint32_t,
                               __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, SEL != 0));
+}
+
+// 8 bf16 values of row `row` (K of them) from channel k, zeros behind K. Any alignment.
+__device__ __forceinline__ void load8(const uint16_t *row, int64_t k, int64_t K,
+                                      uint32_t (&w)[4]) {
+    if (k + 8 <= K) {
+        const Bytes16 b = *reinterpret_cast<const Bytes16 *>(row + k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = b.w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = k + 2 * i < K ? row[k + 2 * i] : 0;
+            const uint32_t hi = k + 2 * i + 1 < K ? row[k + 2 * i + 1] : 0;
+            w[i] = lo | hi << 16;
+        }
+    }
+}
+
+// Largest of v over the four lanes of a block.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
 }
 
 }  // namespace mx

@@ -126,7 +126,7 @@ SHAPES = [(1, 1, 1), (1, 16, 32), (2, 33, 100), (3, 128, 256), (16, 257, 520), (
           (31, 100, 2048), (33, 130, 1000), (64, 64, 64), (65, 300, 4096), (77, 512, 544),
           (128, 128, 288), (129, 255, 257), (200, 1001, 800), (256, 256, 256), (257, 640, 1024),
           (300, 513, 2080), (520, 768, 1536), (1, 4096, 8192), (5, 2000, 5000), (40, 96, 16384),
-          (700, 1100, 40), (1, 5, 20000)]
+          (700, 1100, 40), (1, 5, 20000), (2100, 4200, 520), (5000, 1999, 96)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
