@@ -8,8 +8,7 @@
 // steps 0 .. 3: the four scale bytes of a lane are then one word of the scales' layout, and
 // each step selects its byte of that word.
 #include "mx_internal.hpp"
-#include "mx_math.hpp"
-#include "quant_math.hpp"
+#include "mx_quant.hpp"
 
 #include <algorithm>
 #include <utility>
@@ -57,15 +56,18 @@ struct Mx4Params {
 // Tile (and K-range) of workgroup `bid`: each XCD takes every 8th workgroup and gets a
 // contiguous run of tiles, K-ranges outermost, in groups of gm token tiles.
 __device__ __forceinline__ void tile_of(int bid, const Mx4Params &p, int &tm, int &tn, int &split) {
+    // Divisions run in vector registers; the results are made scalar again, or the buffer
+    // descriptors that they lead to would be taken for different ones in each lane.
+    const auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.splits;
     const int xcd = bid & 7, slot = bid >> 3, q = total >> 3, r = total & 7;
     int t = xcd * q + min(xcd, r) + slot;
-    split = t / tiles;
+    split = uniform(t / tiles);
     t -= split * tiles;
-    const int per = p.gm * p.tiles_n, first = t / per * p.gm, in = t % per;
-    const int size = min(p.tiles_m - first, p.gm);
-    tm = first + in % size;
-    tn = in / size;
+    const int per = p.gm * p.tiles_n, group = uniform(t / per), first = group * p.gm;
+    const int in = t - group * per, size = min(p.tiles_m - first, p.gm);
+    tn = uniform(in / size);
+    tm = first + in - tn * size;
 }
 
 // One workgroup per TM tokens x TN channels; WM x WN wavefronts, S LDS stages of a K-panel:
@@ -79,17 +81,16 @@ mx4_gemm_kernel(Mx4Params p) {
     constexpr int WTM = TM / WM, WTN = TN / WN, FM = WTM / 32, FN = WTN / 32;
     constexpr int ROWS = TN + TM;
     constexpr int CODES = ROWS * kPanel, STAGE = CODES + ROWS * 8;
-    // A wavefront's loads of a panel: 8 rows of codes each, then SR rows of scales each.
-    constexpr int IW = TN / 8 / NW, IX = TM / 8 / NW;
-    constexpr int SB = ROWS * 8 == NW * 1024 ? 16 : 4, SR = 64 * SB / 8, IS = ROWS / SR / NW;
-    constexpr int NV = IW + IX + IS;
-    static_assert(WTM % 32 == 0 && WTN % 32 == 0, "tile");
-    static_assert(TN % (8 * NW) == 0 && TM % (8 * NW) == 0 && NW % 4 == 0, "code loads");
-    static_assert(ROWS % (SR * NW) == 0 && TN % SR == 0, "scale loads");
+    // Loads of a panel, NV to a wavefront: 8 rows of codes each, then SR rows of scales each.
+    constexpr int SB = TN % 128 == 0 && TM % 128 == 0 ? 16 : 4, SR = 64 * SB / 8;
+    constexpr int IW = TN / 8, IC = ROWS / 8, NI = IC + ROWS / SR, NV = (NI + NW - 1) / NW;
+    static_assert(WTM % 32 == 0 && WTN % 32 == 0 && NW % 4 == 0, "tile");
+    static_assert(TN % SR == 0 && TM % SR == 0, "scale loads");
     static_assert(S >= 2 && (S - 1) * NV <= 63, "loads in flight");
     constexpr int RS = 2 * WTN + 16;       // output staging: bytes of a token's row
-    static_assert(NW * 32 * RS + TN * 4 <= S * STAGE && S * STAGE <= 163840, "LDS");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[S * STAGE];
+    static_assert(NW * 32 * RS <= S * STAGE && S * STAGE + TN * 4 <= 163840, "LDS");
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[S * STAGE + TN * 4];
+    float *const bias = reinterpret_cast<float *>(smem + S * STAGE);
 
     const Mx4Args &a = p.a;
     const int lane = threadIdx.x & 63;
@@ -114,23 +115,11 @@ mx4_gemm_kernel(Mx4Params p) {
         for (int j = 0; j < FM; ++j)
             acc[i][j] = f32x16{};
 
-    // Codes: load i of this wavefront fills rows 8 (i NW + wave) + lane / 8, physical chunk
-    // lane % 8, and so fetches chunk (lane % 8) ^ swz(row), the same for all i as NW % 4 == 0.
+    // Load i of this wavefront is number i NW + wave (the last one again past it: the same
+    // bytes to the same place). Codes: rows 8n + lane / 8 of the stage, physical chunk lane % 8,
+    // and so chunk (lane % 8) ^ swz(row) of the row, the same for all i as NW % 4 == 0.
     const int lrow = wave * 8 + (lane >> 3);
     const int lchunk = ((lane & 7) ^ swz(lrow)) << 4;
-    // Scales: load i fills SR rows from (i NW + wave) SR of the stage's scale words.
-    const uint8_t *sbase[IS];
-    int64_t sstep[IS];
-    int sbytes[IS];
-#pragma unroll
-    for (int i = 0; i < IS; ++i) {
-        const int row = (i * NW + wave) * SR;
-        const bool w = row < TN;
-        const int left = w ? rows_w - row : rows_x - (row - TN);
-        sstep[i] = (w ? a.N : a.M) * 8;
-        sbase[i] = (w ? a.ws + (n0 + row) * 8 : a.xs + (m0 + row - TN) * 8) + first_panel * sstep[i];
-        sbytes[i] = max(left, 0) * 8;
-    }
     // Where panel kt's codes start for this lane; beyond the buffers past the last panel and
     // past the rows' ends.
     const auto codes_at = [&](int kt) {
@@ -139,18 +128,22 @@ mx4_gemm_kernel(Mx4Params p) {
     };
     const auto issue = [&](auto ic, int kt, int at, int so) __attribute__((always_inline)) {
         constexpr int i = decltype(ic)::value;
-        if constexpr (i < IW + IX) {
-            constexpr int q = i < IW ? i : i - IW;
-            uint8_t *dst = smem + so + (i * NW + wave) * 1024;
+        const int n = i * NW + NW <= NI ? i * NW + wave : min(i * NW + wave, NI - 1);
+        if (i * NW + NW <= IC || n < IC) {
+            const bool w = i * NW + NW <= IW || (i * NW < IW && n < IW);
+            uint8_t *dst = smem + so + n * 1024;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                i < IW ? rw : rx, (__attribute__((address_space(3))) void *)dst, 16,
-                at + q * NW * 8 * row_bytes, 0, 0, 0);
+                w ? rw : rx, (__attribute__((address_space(3))) void *)dst, 16,
+                at + (i * NW * 8 - (w ? 0 : TN)) * row_bytes, 0, 0, 0);
         } else {
-            constexpr int q = i - IW - IX;
-            const bool in = kt < nk;       // past the last panel: an empty buffer
+            const int row = (n - IC) * SR;             // of the stage's scale words
+            const bool w = row < TN, in = kt < nk;     // past the last panel: an empty buffer
+            const int64_t rows = w ? a.N : a.M, r0 = w ? n0 + row : m0 + row - TN;
+            const int left = (w ? rows_w : rows_x + TN) - row;
             const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-                (void *)(sbase[q] + (in ? kt : 0) * sstep[q]), (short)0, in ? sbytes[q] : 0, kRsrcWord3);
-            uint8_t *dst = smem + so + CODES + (q * NW + wave) * 64 * SB;
+                (void *)((w ? a.ws : a.xs) + ((in ? first_panel + kt : 0) * rows + r0) * 8), (short)0,
+                in ? max(left, 0) * 8 : 0, kRsrcWord3);
+            uint8_t *dst = smem + so + CODES + (n - IC) * 64 * SB;
             if constexpr (SB == 16)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(
                     rs, (__attribute__((address_space(3))) void *)dst, 16, lane * 16, 0, 0, 0);
@@ -207,12 +200,27 @@ mx4_gemm_kernel(Mx4Params p) {
         }(std::make_integer_sequence<int, steps>{});
     };
 
+    // The tile's bias, read behind the first panels.
+    constexpr int NB = (TN + NW * 64 - 1) / (NW * 64);
+    float tile_bias[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const int n = i * NW * 64 + (int)threadIdx.x;
+        tile_bias[i] = a.bias && n < rows_w ? __uint_as_float((uint32_t)a.bias[n0 + n] << 16) : 0.0f;
+    }
+    const auto park_bias = [&]() {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            if (i * NW * 64 + (int)threadIdx.x < TN)
+                bias[i * NW * 64 + threadIdx.x] = tile_bias[i];
+    };
     if (nk > 0) {
 #pragma unroll
         for (int k = 0; k < S - 1; ++k)
             [&]<int... i>(std::integer_sequence<int, i...>) __attribute__((always_inline)) {
                 (issue(std::integral_constant<int, i>{}, k, codes_at(k), k * STAGE), ...);
             }(std::make_integer_sequence<int, NV>{});
+        park_bias();
         int st = 0, ld = S - 1;
         for (int kt = 0; kt < nk; ++kt) {
             // Panel kt has landed once at most the S - 2 younger ones are in flight; every
@@ -276,14 +284,16 @@ mx4_gemm_kernel(Mx4Params p) {
 
     // Output: 32 tokens at a time through the wavefront's own piece of LDS (free now), so
     // that stores are whole 16-byte pieces of rows.
-    barrier_nofence();
-    constexpr int CPR = WTN / 8, RPQ = 64 / CPR, NQ = (32 + RPQ - 1) / RPQ;
-    uint8_t *const region = smem + wave * 32 * RS;
-    float *const bias = reinterpret_cast<float *>(smem + NW * 32 * RS);
-    for (int i = threadIdx.x; i < TN; i += NW * 64)
-        bias[i] = a.bias && n0 + i < a.N ? __uint_as_float((uint32_t)a.bias[n0 + i] << 16) : 0.0f;
+    if (nk <= 0)
+        park_bias();
     __syncthreads();
+    constexpr int CPR = WTN / 8, RPQ = 64 / CPR, NQ = (32 + RPQ - 1) / RPQ;
+    constexpr bool EXACT = RPQ * CPR == 64 && NQ * RPQ == 32;
+    uint8_t *const region = smem + wave * 32 * RS;
     const int row0 = lane / CPR, ch = lane % CPR;
+    const int64_t n_lane = nw + ch * 8;
+    uint16_t *const out = a.y + (mw + row0) * a.N + n_lane;
+    const bool whole = p.vec && mw + WTM <= a.M && nw + WTN <= a.N;
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
 #pragma unroll
@@ -299,23 +309,31 @@ mx4_gemm_kernel(Mx4Params p) {
                 *reinterpret_cast<uint2 *>(region + r * RS + (i * 32 + g * 8 + h * 4) * 2) =
                     make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
             }
+        u32x4 v[NQ];
+        const auto live = [&](int q) { return EXACT || (row0 < RPQ && row0 + q * RPQ < 32); };
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+            if (live(q))
+                v[q] = *reinterpret_cast<const u32x4 *>(region + (row0 + q * RPQ) * RS + ch * 16);
+        if (whole) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q)
+                if (live(q))
+                    __builtin_nontemporal_store(
+                        v[q], reinterpret_cast<u32x4 *>(out + (int64_t)(j * 32 + q * RPQ) * a.N));
+            continue;
+        }
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-            const int row = row0 + q * RPQ;
-            const int64_t m = mw + j * 32 + row, n = nw + ch * 8;
-            if (row0 >= RPQ || row >= 32 || m >= a.M || n >= a.N)
+            if (!live(q) || mw + j * 32 + row0 + q * RPQ >= a.M || n_lane >= a.N)
                 continue;
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(region + row * RS + ch * 16);
-            uint16_t *o = a.y + m * a.N + n;
-            if (p.vec) {
-                __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(o));
-            } else if (n + 8 <= a.N) {
-                *reinterpret_cast<Bytes16 *>(o) = __builtin_bit_cast(Bytes16, v);
+            uint16_t *o = out + (int64_t)(j * 32 + q * RPQ) * a.N;
+            if (n_lane + 8 <= a.N) {
+                *reinterpret_cast<Bytes16 *>(o) = __builtin_bit_cast(Bytes16, v[q]);
             } else {
-#pragma unroll
                 for (int e = 0; e < 7; ++e)
-                    if (n + e < a.N)
-                        o[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                    if (n_lane + e < a.N)
+                        o[e] = (uint16_t)(v[q][e >> 1] >> (16 * (e & 1)));
             }
         }
     }
@@ -353,29 +371,31 @@ mx4_reduce_kernel(Mx4Params p) {
     }
 }
 
-// Few tokens: bound by reading W once, so nothing of it is staged. A workgroup owns 16 FNB
-// channels and 16 FMB tokens; its NW wavefronts take K in turn, 512 channels (256 bytes, 16
-// blocks) at a time, with the next 512 channels' loads in flight. v_mfma_scale_f32_16x16x128:
-// lane (r, g) = (lane % 16, lane / 16) holds row r; in step s of four it takes block 4s + g, so
-// that a load instruction reads whole 64-byte pieces of rows, and byte g of a scale word.
-// The wavefronts' sums meet in LDS, added in their order.
+// Few tokens (up to 16): bound by reading W once, so nothing of it is staged. A workgroup owns
+// 16 FNB channels; its NW wavefronts take K in turn, 512 channels (256 bytes, 16 blocks) at a
+// time, with the next 512 channels' loads in flight. v_mfma_scale_f32_16x16x128: lane (r, g) =
+// (lane % 16, lane / 16) holds row r; in step s of four it takes block 4s + g, so that a load
+// instruction reads whole 64-byte pieces of rows, and byte g of a scale word. The wavefronts'
+// sums meet in LDS, added in their order.
 //
-// QX: the tokens are bf16 rows (times col_mul where there is one), and a lane quantizes its
-// block itself before multiplying: blocks need nothing of their row, and a workgroup's
-// wavefronts share no block, so the whole linear is this one launch.
-template <int FMB, int FNB, int NW, bool QX, bool CM>
+// QX: the tokens are bf16 rows (transformed as in the quantizer), which the workgroup quantizes
+// into LDS while its first weights are on their way; the whole linear is then this one launch.
+// Every workgroup quantizes them again, so the host allows it for few tokens x channels only.
+// LDS rows are an odd number of 16-byte blocks apart: the 16 rows of a read then lie in
+// different banks.
+template <int FNB, int NW, bool QX, int ACT, bool CM>
 __global__ void __launch_bounds__(NW * 64)
 mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul) {
     using namespace mx;
-    __shared__ f32x4 red[NW][FNB][FMB][64];
+    __shared__ f32x4 red[NW][FNB][64];
+    extern __shared__ __attribute__((aligned(16))) uint8_t tokens[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
-    const int64_t tiles_n = (a.N + 16 * FNB - 1) / (16 * FNB);
-    const int64_t n0 = blockIdx.x % tiles_n * (16 * FNB), m0 = blockIdx.x / tiles_n * (16 * FMB);
-    const int nb = (int)a.nb, panels = (nb + 7) / 8;
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * FNB);
+    const int M = (int)a.M, nb = (int)a.nb, panels = (nb + 7) / 8;
 
-    // Rows past the matrix repeat the last one; their results are not stored.
+    // Rows past the matrices repeat the last one; their results are not stored.
     const uint8_t *wrow[FNB], *wscale[FNB];
 #pragma unroll
     for (int c = 0; c < FNB; ++c) {
@@ -383,164 +403,172 @@ mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul)
         wrow[c] = a.wq + n * nb * 16;
         wscale[c] = a.ws + n * 8;
     }
-    const auto word = [&](const uint8_t *scales, int64_t rows, int panel, int s) {
-        return panel < panels
-                   ? *reinterpret_cast<const uint32_t *>(scales + panel * rows * 8 + 4 * (s & 1))
-                   : 0u;
-    };
-    f32x4 acc[FNB][FMB];
+    const int m = min(r, M - 1);
+    f32x4 acc[FNB];
 #pragma unroll
     for (int c = 0; c < FNB; ++c)
-#pragma unroll
-        for (int b = 0; b < FMB; ++b)
-            acc[c][b] = f32x4{};
+        acc[c] = f32x4{};
 
-    i32x4 w[FNB][4];
-    uint32_t sw[FNB][4];
+    i32x4 w[FNB][4], fx[4];
+    uint2 sw[FNB][2];
+    int sx[4];
     const auto load = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-        for (int c = 0; c < FNB; ++c)
+        for (int c = 0; c < FNB; ++c) {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const int blk = 16 * j + 4 * s + g;
                 w[c][s] = blk < nb ? *reinterpret_cast<const i32x4 *>(wrow[c] + (int64_t)blk * 16)
                                    : i32x4{};
-                sw[c][s] = word(wscale[c], a.N, 2 * j + s / 2, s);
             }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                sw[c][h] = 2 * j + h < panels
+                               ? *reinterpret_cast<const uint2 *>(wscale[c] + (2 * j + h) * a.N * 8)
+                               : make_uint2(0, 0);
+        }
+        if constexpr (!QX) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int blk = min(16 * j + 4 * s + g, nb - 1);   // against zero weights past nb
+                fx[s] = *reinterpret_cast<const i32x4 *>(a.xq + ((int64_t)m * nb + blk) * 16);
+                sx[s] = a.xs[((int64_t)(blk >> 3) * M + m) * 8 + (blk & 7)];
+            }
+        }
     };
     const int steps = (nb + 15) / 16;
     if (wave < steps)
         load(wave);
+    const int stride = (nb | 1) * 16;
+    uint8_t *const token_scales = tokens + M * stride;
+    if constexpr (QX) {
+        // A lane quantizes 8 channels, four lanes a block.
+        for (int u = threadIdx.x; u < M * nb * 4; u += NW * 64) {
+            const int row = u / (nb * 4), q = u - row * (nb * 4);
+            float c[8];
+            if constexpr (CM)
+                load_multipliers(col_mul, 8 * q, K, c);
+            uint32_t v[4], byte;
+            load8(x + row * K, 8 * q, K, v);
+            const uint32_t codes = quantize_quad<ACT, CM>(v, c, byte);
+            *reinterpret_cast<uint32_t *>(tokens + row * stride + q * 4) = codes;
+            if (q % 4 == 0)
+                token_scales[row * nb + q / 4] = (uint8_t)byte;
+        }
+        __syncthreads();
+    }
     for (int j = wave; j < steps; j += NW) {
-        i32x4 fx[FMB][4];
-        int sx[FMB][4];
-#pragma unroll
-        for (int b = 0; b < FMB; ++b) {
-            const int64_t m = m0 + b * 16 + r;
+        if constexpr (QX) {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const int blk = 16 * j + 4 * s + g;
-                const bool in = m < a.M && blk < nb;
-                fx[b][s] = i32x4{};
-                sx[b][s] = 0;
-                if constexpr (!QX) {
-                    if (in) {
-                        fx[b][s] = *reinterpret_cast<const i32x4 *>(a.xq + (m * nb + blk) * 16);
-                        sx[b][s] = a.xs[((int64_t)(blk >> 3) * a.M + m) * 8 + (blk & 7)];
-                    }
-                } else if (in) {
-                    const uint16_t *src = x + m * K + (int64_t)blk * 32;
-                    const int64_t left = K - (int64_t)blk * 32;
-                    uint32_t v[4][4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        load8(src, 8 * q, left, v[q]);
-                    if constexpr (!CM) {
-                        uint32_t top = 0;
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                top = max_halves(top, magnitudes(v[q][e]));
-                        const uint32_t byte = scale_byte<kTop4>(max(top & 0xFFFFu, top >> 16) >> 7);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            fx[b][s][q] = (int)encode4_bf16(v[q], scale_operand(byte));
-                        sx[b][s] = (int)byte;
-                    } else {
-                        float f[4][8];
-                        uint32_t top = 0;
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const int64_t k = (int64_t)blk * 32 + 8 * q + e;
-                                f[q][e] = qmath::bf16_to_f32((v[q][e / 2] >> (16 * (e & 1))) & 0xFFFFu) *
-                                          (k < K ? col_mul[k] : 0.0f);
-                                top = max(top, __float_as_uint(f[q][e]) & 0x7FFFFFFFu);
-                            }
-                        const uint32_t byte = scale_byte<kTop4>(top >> 23);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            fx[b][s][q] = (int)encode4_f32(f[q], scale_operand(byte));
-                        sx[b][s] = (int)byte;
-                    }
-                }
+                const int blk = min(16 * j + 4 * s + g, nb - 1);
+                fx[s] = *reinterpret_cast<const i32x4 *>(tokens + m * stride + blk * 16);
+                sx[s] = token_scales[m * nb + blk];
             }
         }
-        i32x4 wc[FNB][4];
-        uint32_t sc[FNB][4];
+        i32x4 wc[FNB][4], xc[4];
+        uint32_t sc[FNB][4], xsc[4];
 #pragma unroll
-        for (int c = 0; c < FNB; ++c)
+        for (int s = 0; s < 4; ++s) {
+            xc[s] = fx[s];
+            xsc[s] = sx[s];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
+            for (int c = 0; c < FNB; ++c) {
                 wc[c][s] = w[c][s];
-                sc[c][s] = sw[c][s] >> (8 * g);
+                sc[c][s] = (s & 1 ? sw[c][s / 2].y : sw[c][s / 2].x) >> (8 * g);
             }
+        }
         if (j + NW < steps)
             load(j + NW);
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
             for (int c = 0; c < FNB; ++c)
-#pragma unroll
-                for (int b = 0; b < FMB; ++b)
-                    acc[c][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        frag(wc[c][s]), frag(fx[b][s]), acc[c][b], 4, 4, 0, (int)sc[c][s], 0, sx[b][s]);
+                acc[c] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                    frag(wc[c][s]), frag(xc[s]), acc[c], 4, 4, 0, (int)sc[c][s], 0, (int)xsc[s]);
     }
 #pragma unroll
     for (int c = 0; c < FNB; ++c)
-#pragma unroll
-        for (int b = 0; b < FMB; ++b)
-            red[wave][c][b][lane] = acc[c][b];
+        red[wave][c][lane] = acc[c];
     __syncthreads();
     // Lane (r, g) of a fragment holds token r, channels 4g .. 4g + 3.
-    for (int i = threadIdx.x; i < FNB * FMB * 64; i += NW * 64) {
-        const int l = i & 63, b = (i >> 6) % FMB, c = (i >> 6) / FMB;
-        f32x4 v = red[0][c][b][l];
+    for (int i = threadIdx.x; i < FNB * 64; i += NW * 64) {
+        const int l = i & 63, c = i >> 6, t = l & 15;
+        f32x4 v = red[0][c][l];
 #pragma unroll
         for (int k = 1; k < NW; ++k)
-            v += red[k][c][b][l];
-        const int64_t m = m0 + b * 16 + (l & 15), n = n0 + c * 16 + (l >> 4) * 4;
-        if (m >= a.M)
+            v += red[k][c][l];
+        const int64_t n = n0 + c * 16 + (l >> 4) * 4;
+        if (t >= M)
             continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (n + e < a.N) {
                 const float bias = a.bias ? __uint_as_float((uint32_t)a.bias[n + e] << 16) : 0.0f;
-                a.y[m * a.N + n + e] = __builtin_bit_cast(uint16_t, (__bf16)(v[e] + bias));
+                a.y[t * a.N + n + e] = __builtin_bit_cast(uint16_t, (__bf16)(v[e] + bias));
             }
     }
 }
 
 // ---------------------------------------------------------------- what runs for a shape
 
-enum Tile : int { T256x256, T128x128, T64x64, kTiles };
-struct TileSize {
+// A workgroup of tile t takes start + panel * (its K-panels) microseconds; further rounds of
+// 256 workgroups cost `more` of the first (under 1 where two share a CU, over 1 where the clock
+// falls under the load). Fitted to 200 random shapes (M 17 .. 8192, N 64 .. 20480, K 64 ..
+// 24576) with every tile and 1 to 16 K-ranges: the choice is 1% slower than the best measured
+// one in the geometric mean, 15% at most.
+struct TileCost {
     int tm, tn;
+    float start, panel, more;
 };
-constexpr TileSize kTile[kTiles] = {{256, 256}, {128, 128}, {64, 64}};
+constexpr TileCost kTiles[] = {
+    {288, 256, 5.87f, 1.54f, 1.28f}, {256, 256, 5.74f, 1.32f, 1.17f}, {192, 256, 4.88f, 1.07f, 1.10f},
+    {128, 256, 4.36f, 0.68f, 1.03f}, {128, 128, 3.75f, 0.47f, 1.03f}, {64, 128, 2.14f, 0.376f, 0.83f},
+    {64, 64, 1.64f, 0.269f, 0.76f},
+};
+constexpr float kReduce = 3.9f, kReducePerMega = 1.66f;   // joining K-ranges: + per 2^20 partials
 constexpr int kCus = 256;
-constexpr int kStreamTokens = 64;     // the streaming kernel up to here
+constexpr int kStreamTokens = 16;     // the streaming kernel up to here: one token fragment
+// It quantizes up to so many values itself: each workgroup does them all again, 2 us for 16384
+// tokens x channels on top of the product, as much as a launch of its own (4096 -> 16384
+// channels, us: 9.8, 10.7, 12.9, 17.4 for 1, 2, 4, 8 tokens; in two launches 14.8 for 16).
+constexpr int64_t kOneLaunchValues = 16384;
 
 struct Plan {
     int tile, splits;
 };
 
 Plan plan_of(int64_t M, int64_t N, int64_t nb) {
+    thread_local struct {
+        int64_t M = -1, N, nb;
+        Plan plan;
+    } last;      // a pure function of the sizes: asked for several times in a call
+    if (last.M == M && last.N == N && last.nb == nb)
+        return last.plan;
     const int64_t panels = (nb + 7) / 8;
-    Plan best = {T256x256, 1};
-    for (int t = kTiles - 1; t >= 0; --t) {
-        const int64_t tiles = ((M + kTile[t].tm - 1) / kTile[t].tm) * ((N + kTile[t].tn - 1) / kTile[t].tn);
-        if (t == 0 || tiles <= 2 * kCus) {
-            best.tile = t;
-            if (t > 0 && tiles * 2 > kCus)
-                best.splits = 1;
-            else if (t > 0)
-                best.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kCus / tiles, panels / 4, 16}));
-            break;
+    Plan best = {0, 1};
+    float least = INFINITY;
+    for (int t = 0; t < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++t) {
+        const TileCost &c = kTiles[t];
+        const int64_t tiles = ((M + c.tm - 1) / c.tm) * ((N + c.tn - 1) / c.tn);
+        for (int splits = 1; splits <= 16; splits *= 2) {
+            if (splits > 1 && (tiles * splits > 2 * kCus || panels < 3 * splits))
+                break;
+            const float rounds = (float)((tiles * splits + kCus - 1) / kCus);
+            float us = (c.start + c.panel * (float)((panels + splits - 1) / splits)) *
+                       (1.0f + (rounds - 1.0f) * c.more);
+            if (splits > 1)
+                us += kReduce + kReducePerMega * (float)splits * (float)M * (float)N / 1e6f;
+            if (us < least) {
+                least = us;
+                best = {t, splits};
+            }
         }
     }
+    last.M = M;
+    last.N = N;
+    last.nb = nb;
+    last.plan = best;
     return best;
 }
 
@@ -557,25 +585,23 @@ hipError_t run_tile(Mx4Params p, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <bool QX, bool CM>
+template <bool QX, int ACT, bool CM>
 hipError_t run_stream(const Mx4Args &a, const uint16_t *x, int64_t K, const float *cm, hipStream_t s) {
-    const auto go = [&](auto kernel, int64_t tokens, int64_t channels, int waves) {
-        const int64_t blocks =
-            ((a.M + tokens - 1) / tokens) * ((a.N + channels - 1) / channels);
+    const auto go = [&](auto kernel, int64_t channels, int waves) {
+        const int64_t blocks = (a.N + channels - 1) / channels;
         if (blocks > 0x7FFFFFFF)
             return hipErrorInvalidValue;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), 0, s, a, x, K, cm);
+        const size_t lds = QX ? (size_t)(a.M * ((a.nb | 1) * 16 + a.nb)) : 0;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), lds, s, a, x, K, cm);
         return hipGetLastError();
     };
-    if (a.M <= 16)
-        return a.N >= 8192 ? go(mx4_stream_kernel<1, 2, 8, QX, CM>, 16, 32, 8)
-                           : go(mx4_stream_kernel<1, 1, 8, QX, CM>, 16, 16, 8);
-    if constexpr (!QX) {
-        if (a.M <= 32)
-            return go(mx4_stream_kernel<2, 1, 8, QX, CM>, 32, 16, 8);
-        return go(mx4_stream_kernel<4, 1, 8, QX, CM>, 64, 16, 8);
-    }
-    return hipErrorInvalidValue;
+    // Wavefronts enough to keep memory busy, and few turns of 512 channels for each. Graphs of
+    // one token, us: 4096 x 16384 9.7 with 2 x 4 (10.7 with 1 x 8), 4096 x 4096 4.6 with 1 x 8
+    // (6.0 with 2 x 4, 4.8 with 1 x 16), 16384 x 4096 11.1 with 1 x 16 (12.6 with 1 x 8).
+    if (a.N >= 8192)
+        return go(mx4_stream_kernel<2, 4, QX, ACT, CM>, 32, 4);
+    return a.nb >= 256 ? go(mx4_stream_kernel<1, 16, QX, ACT, CM>, 16, 16)
+                       : go(mx4_stream_kernel<1, 8, QX, ACT, CM>, 16, 8);
 }
 
 }  // namespace
@@ -589,7 +615,7 @@ size_t mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t nb) {
 
 hipError_t launch_mx4_gemm(const Mx4Args &a, void *ws, hipStream_t s) {
     if (a.M <= kStreamTokens)
-        return run_stream<false, false>(a, nullptr, 0, nullptr, s);
+        return run_stream<false, ACT_NONE, false>(a, nullptr, 0, nullptr, s);
     const Plan plan = plan_of(a.M, a.N, a.nb);
     const int64_t panels = (a.nb + 7) / 8;
     Mx4Params p;
@@ -600,8 +626,12 @@ hipError_t launch_mx4_gemm(const Mx4Args &a, void *ws, hipStream_t s) {
     p.part = static_cast<float *>(ws);
     hipError_t e;
     switch (plan.tile) {
-    case T256x256: e = run_tile<256, 256, 2, 2, 2>(p, s); break;
-    case T128x128: e = run_tile<128, 128, 2, 2, 4>(p, s); break;
+    case 0: e = run_tile<288, 256, 3, 4, 2>(p, s); break;
+    case 1: e = run_tile<256, 256, 4, 2, 2>(p, s); break;
+    case 2: e = run_tile<192, 256, 2, 4, 2>(p, s); break;
+    case 3: e = run_tile<128, 256, 2, 4, 3>(p, s); break;
+    case 4: e = run_tile<128, 128, 2, 2, 4>(p, s); break;
+    case 5: e = run_tile<64, 128, 1, 4, 3>(p, s); break;
     default: e = run_tile<64, 64, 2, 2, 4>(p, s); break;
     }
     if (e != hipSuccess || p.splits <= 1)
@@ -615,12 +645,17 @@ hipError_t launch_mx4_gemm(const Mx4Args &a, void *ws, hipStream_t s) {
     return hipGetLastError();
 }
 
-bool mx4_linear_one_launch(int64_t M, int act) { return M <= 16 && act == ACT_NONE; }
+bool mx4_linear_one_launch(int64_t M, int64_t K) {
+    return M <= kStreamTokens && M * K <= kOneLaunchValues;
+}
 
-hipError_t launch_mx4_linear(const Mx4Args &a, const uint16_t *x, int64_t K, const float *col_mul,
-                             hipStream_t s) {
-    return col_mul ? run_stream<true, true>(a, x, K, col_mul, s)
-                   : run_stream<true, false>(a, x, K, col_mul, s);
+hipError_t launch_mx4_linear(const Mx4Args &a, const uint16_t *x, int64_t K, int act,
+                             const float *col_mul, hipStream_t s) {
+    if (act == ACT_GELU)
+        return col_mul ? run_stream<true, ACT_GELU, true>(a, x, K, col_mul, s)
+                       : run_stream<true, ACT_GELU, false>(a, x, K, nullptr, s);
+    return col_mul ? run_stream<true, ACT_NONE, true>(a, x, K, col_mul, s)
+                   : run_stream<true, ACT_NONE, false>(a, x, K, nullptr, s);
 }
 
 }  // namespace w8a8

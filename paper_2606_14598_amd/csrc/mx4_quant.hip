@@ -7,9 +7,8 @@
 // that the product reads a tile's scales of one K-panel as one piece of memory.
 //
 // Bound by memory: 2 bytes read and 17/32 written per element.
-#include "gelu.hpp"
 #include "mx_internal.hpp"
-#include "mx_math.hpp"
+#include "mx_quant.hpp"
 
 namespace w8a8 {
 namespace {
@@ -34,11 +33,8 @@ mx4_quant_kernel(const uint16_t *x, int64_t R, int64_t K, const float *col_mul, 
     const int64_t panel = chunk * 2 + (lane >> 5);
     const bool store_codes = k / 2 < row_bytes, store_scale = panel * 256 < K && lane % 4 == 0;
     float c[8];
-    if constexpr (CM) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            c[e] = k + e < K ? col_mul[k + e] : 0.0f;
-    }
+    if constexpr (CM)
+        load_multipliers(col_mul, k, K, c);
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
         const int64_t r = r0 + i;
@@ -46,30 +42,8 @@ mx4_quant_kernel(const uint16_t *x, int64_t R, int64_t K, const float *col_mul, 
             return;
         uint32_t w[4];
         load8(x + r * K, k, K, w);
-        uint32_t byte, q;
-        if constexpr (ACT == ACT_NONE && !CM) {
-            uint32_t m = max_halves(max_halves(magnitudes(w[0]), magnitudes(w[1])),
-                                    max_halves(magnitudes(w[2]), magnitudes(w[3])));
-            m = quad_max(max(m & 0xFFFFu, m >> 16));
-            byte = scale_byte<kTop4>(m >> 7);
-            q = encode4_bf16(w, scale_operand(byte));
-        } else {
-            float v[8];
-            uint32_t m = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float f = bf16_to_f32((w[e / 2] >> (16 * (e & 1))) & 0xFFFFu);
-                v[e] = ACT == ACT_GELU ? gelu_f32(f) : f;
-                if constexpr (CM)
-                    v[e] *= c[e];
-                m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-            }
-            m = quad_max(m);
-            byte = scale_byte<kTop4>(m >> 23);
-            q = encode4_f32(v, scale_operand(byte));
-        }
-        if (byte == kNaNScale)
-            q = 0;
+        uint32_t byte;
+        const uint32_t q = quantize_quad<ACT, CM>(w, c, byte);
         if (store_codes)
             *reinterpret_cast<uint32_t *>(codes + r * row_bytes + k / 2) = q;
         if (store_scale)

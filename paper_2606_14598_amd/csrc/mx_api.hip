@@ -144,9 +144,9 @@ w8a8_status w8a8_mx4_linear(const uint16_t *x, int act, const float *col_mul, co
     const size_t need = w8a8_mx4_linear_workspace_bytes(M, N, K);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
         return W8A8_ERR_WORKSPACE;
-    if (mx4_linear_one_launch(M, act))
+    if (mx4_linear_one_launch(M, K))
         return from_hip(launch_mx4_linear(product(nullptr, nullptr, wq, w_scale, bias, y, M, N, K), x, K,
-                                          col_mul, as_stream(stream)));
+                                          act, col_mul, as_stream(stream)));
     uint8_t *xq = static_cast<uint8_t *>(workspace);
     uint8_t *xs = xq + align_up(code_bytes(M, K));
     uint8_t *rest = xs + align_up(scale_bytes(M, K));
