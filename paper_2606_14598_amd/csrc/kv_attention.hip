@@ -19,6 +19,8 @@
 #include "mx_math.hpp"
 #include "quant_math.hpp"
 
+#include <algorithm>
+
 namespace w8a8 {
 namespace {
 
@@ -27,6 +29,7 @@ using namespace mx;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -34,11 +37,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // workgroup s of `splits` takes numbers s, s + splits, ...
 struct Split {
     int chunk, splits;
-    float *part;     // splits > 1: [splits][T * q heads][dim + 4]: O, m, l, two unused
+    float *part;     // splits > 1: [splits][T * q heads][dim + 4]: O, m, l; in split 0 the
+                     // number of splits the row has (1: its output is written already)
     uint64_t magic;  // n / (page / 16) = n * magic >> 32 for n < 2^22 (kMaxTokens / 16)
 };
 
-constexpr int kMaxChunk = 8192;
+constexpr int kMaxChunk = 4096;
 constexpr int kSplitRows = 16;
 static_assert(W8A8_KV_MAX_TOKENS / 16 <= 1 << 22 && W8A8_KV_MAX_PAGE / 16 <= 1 << 10, "magic");
 
@@ -123,6 +127,28 @@ struct Unit<8> {
     }
 };
 
+// Where the tokens of a chunk lie, 16 at a time: the first one's place in its page, and the
+// page's keys of the head, from which its codes, scales and values follow.
+struct Places {
+    int64_t page[kMaxChunk / 16];
+    int at[kMaxChunk / 16];
+};
+
+// Fills `count` entries from token j_first on; those past token j_end - 1 repeat its block.
+__device__ __forceinline__ void fill_places(Places &pl, const KvShape &c, const KvAttnArgs &a,
+                                            const Split &sp, int b, int head, int j_first, int j_end,
+                                            int count) {
+    const uint32_t last = (uint32_t)(j_end - 1) / 16;
+    const int32_t *table = a.table + b * a.table_stride;
+    for (int i = threadIdx.x; i < count; i += 256) {
+        const uint32_t blk = min((uint32_t)(j_first / 16 + i), last);
+        const uint32_t entry = (uint32_t)(blk * sp.magic >> 32);
+        const int64_t page = min((int64_t)max(table[entry], 0), c.pages - 1);
+        pl.page[i] = (page * 2 * c.heads + head) * c.head_bytes();
+        pl.at[i] = (int)(blk - entry * (uint32_t)(c.page / 16)) * 16;
+    }
+}
+
 // Few rows (16 a workgroup): the keys are divided among workgroups, and among the four
 // wavefronts of each in tiles of 32 tokens; every wavefront keeps its own m, l and O, joined
 // in LDS at the end. Keys go from memory to the matrix registers as they are: lane (t, g) =
@@ -130,7 +156,7 @@ struct Unit<8> {
 // is loaded in the same order. Values pass through the wavefront's own piece of LDS, decoded,
 // and come back transposed. The next tile's codes are loaded while this one is worked on.
 template <int FMT, int D>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, D <= 128 ? 3 : 2)
 kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
     constexpr int KU = FMT == KV_FP4 && D % 128 == 0 ? 32 : 16;   // elements of a key unit
     constexpr int KB = FMT == KV_FP8 ? KU : KU / 2;               // its bytes
@@ -143,17 +169,22 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                                          // transposing read then lie in different banks
     constexpr int F = D / 16;
     __shared__ __attribute__((aligned(16))) uint8_t lds[4][32 * RS];
-    __shared__ int block_page[kMaxChunk / 16];
+    __shared__ Places places;
     __shared__ float row_m[4][16], row_l[4][16], all_l[16], all_m[16];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x % sp.splits, head = blockIdx.x / sp.splits % c.heads;
-    const int b = blockIdx.x / sp.splits / c.heads;
+    // Heads fastest, splits slowest: every 8th workgroup goes to one XCD, and the last splits
+    // of short sequences are empty; with splits fastest one XCD can get all the full ones.
+    const int pairs = c.heads * a.seqs;
+    const int split = __builtin_amdgcn_readfirstlane(blockIdx.x / pairs);
+    const int pair = blockIdx.x - split * pairs;
+    const int b = __builtin_amdgcn_readfirstlane(pair / c.heads), head = pair - b * c.heads;
     const Seq seq = sequence(c, a, b);
     const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
-    const int64_t head_bytes = c.head_bytes();
+    const int64_t v_offset = c.heads * c.head_bytes();     // from a page's keys to its values
+    const int scales_at = c.page * CB;                     // from codes to scales
     uint8_t *const vt = lds[wave];
 
     for (int rt = blockIdx.y; rt * kSplitRows < rows; rt += gridDim.y) {
@@ -192,59 +223,43 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
             const int j_first = ch * sp.chunk;
             const int j_end = min(j_first + sp.chunk, some_see);
             const int ntile = (j_end - j_first + 31) / 32;
-            __syncthreads();       // the table and the LDS rows of what came before are read
-            {
-                const int n_blocks = (j_end - j_first + 15) / 16;
-                const int32_t *t = a.table + b * a.table_stride;
-                for (int i = threadIdx.x; i < ntile * 2; i += 256) {
-                    const uint32_t blk = (uint32_t)(j_first / 16 + min(i, n_blocks - 1));
-                    const int page = t[blk * sp.magic >> 32];
-                    block_page[i] = (int)min((int64_t)max(page, 0), c.pages - 1);
-                }
-            }
+            __syncthreads();       // the places and the LDS rows of what came before are read
+            fill_places(places, c, a, sp, b, head, j_first, j_end, 2 * ntile);
             __syncthreads();
 
             u32x4 kc[2][NK], vc[NV];
             uint32_t ks[2][NK], vs[NV];
             const auto load = [&](int tile) {
-                const uint8_t *kbase[2], *kscale[2];
-                int64_t vofs[2];
+                const uint8_t *page[2];
                 int at[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int page = __builtin_amdgcn_readfirstlane(block_page[2 * tile + h]);
-                    const uint32_t blk = (uint32_t)(j_first / 16 + 2 * tile + h);
-                    const uint32_t pb = (uint32_t)c.page / 16;
-                    // its place in the page; blocks past the last one repeat it
-                    const uint32_t last = (uint32_t)(j_end - 1) / 16;
-                    const uint32_t bb = min(blk, last);
-                    at[h] = (int)(bb - (uint32_t)(bb * sp.magic >> 32) * pb) * 16;
-                    const int64_t base = ((int64_t)page * 2 * c.heads + head) * head_bytes;
-                    kbase[h] = a.cache + base + (int64_t)at[h] * CB;
-                    kscale[h] = a.cache + base + (int64_t)c.page * CB + at[h] * (D / 32);
-                    vofs[h] = base + c.heads * head_bytes;
+                    const uint64_t p = places.page[2 * tile + h];
+                    page[h] = a.cache + (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)p) +
+                              ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32);
+                    at[h] = __builtin_amdgcn_readfirstlane(places.at[2 * tile + h]);
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int s = 0; s < NK; ++s) {
-                        kc[h][s] = Unit<KB>::load(kbase[h] + (uint32_t)(r16 * CB + (4 * s + g) * KB));
-                        ks[h][s] = kscale[h][(uint32_t)(r16 * (D / 32) + (4 * s + g) * KU / 32)];
+                        kc[h][s] =
+                            Unit<KB>::load(page[h] + (uint32_t)((at[h] + r16) * CB + (4 * s + g) * KB));
+                        ks[h][s] = page[h][(uint32_t)(scales_at + (at[h] + r16) * (D / 32) +
+                                                      (4 * s + g) * KU / 32)];
                     }
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int unit = i * 64 + lane, tok = unit / VT, part = unit % VT;
                     // NV even: an instruction's tokens lie in one half of the tile
-                    const int h = NV % 2 == 0 ? 2 * i / NV : 0;
-                    int64_t base = vofs[h];
-                    int in = at[h] + tok - 16 * h;
-                    if constexpr (NV % 2 != 0) {
-                        base = tok < 16 ? vofs[0] : vofs[1];
-                        in = tok < 16 ? at[0] + tok : at[1] + tok - 16;
-                    }
-                    const uint8_t *p = a.cache + base;
+                    constexpr bool EVEN = NV % 2 == 0;
+                    const int h = EVEN ? 2 * i / NV : 0;
+                    const uint8_t *p = EVEN || tok < 16 ? page[h] : page[1];
+                    const int in = EVEN ? at[h] + tok - 16 * h
+                                        : tok < 16 ? at[0] + tok : at[1] + tok - 16;
+                    p += v_offset;
                     vc[i] = Unit<16>::load(p + (uint32_t)(in * CB + part * 16));
-                    vs[i] = p[(uint32_t)(c.page * CB + in * (D / 32) + part * VU / 32)];
+                    vs[i] = p[(uint32_t)(scales_at + in * (D / 32) + part * VU / 32)];
                 }
             };
 
@@ -327,17 +342,23 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                     }
                 top = fmaxf(max_of_row(top), m);
                 const float base = top == -INFINITY ? 0.0f : top;
-                const float keep = __builtin_amdgcn_exp2f(m - base);   // 0 for the first keys
-                m = top;
-                float ps = 0.0f;
+                if (__any(top > m)) {      // else every factor is 1
+                    const float keep = __builtin_amdgcn_exp2f(m - base);   // 0 for the first keys
+                    l *= keep;
+#pragma unroll
+                    for (int f = 0; f < F; ++f)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            o[f][e] *= keep;
+                    m = top;
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         s[h][e] = __builtin_amdgcn_exp2f(s[h][e] - base);
-                        ps += s[h][e];
+                        l += s[h][e];
                     }
-                l = l * keep + ps;
                 const u32x4 p = {pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]),
                                  pack_bf16(s[1][0], s[1][1]), pack_bf16(s[1][2], s[1][3])};
 #pragma unroll
@@ -348,9 +369,6 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                     const i16x4 hi =
                         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(src + 16 * RS));
                     const u32x2 x = __builtin_bit_cast(u32x2, lo), y = __builtin_bit_cast(u32x2, hi);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        o[f][e] *= keep;
                     o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                         __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]}),
                         __builtin_bit_cast(bf16x8, p), o[f], 0, 0, 0);
@@ -414,94 +432,378 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                     p[D + 1] = all_l[r];
                 }
             }
+            if (d == 0 && split == 0 && sp.splits > 1)
+                sp.part[out_row * (D + 4) + D + 2] = (float)used;
         }
         __syncthreads();           // the next row tile writes the same LDS
     }
 }
 
-// Joins the splits of each row: weights 2^(m_s - max m).
-template <int D>
-__global__ void __launch_bounds__(256)
-kv_attention_join_kernel(KvShape c, KvAttnArgs a, Split sp, int tile_rows) {
-    constexpr int PER = D / 4;                 // lanes that hold a row's outputs
-    constexpr int WAYS = 256 / PER;            // splits read side by side
-    __shared__ float red[WAYS][D + 4];
-    const int q_heads = c.heads * a.group;
-    const int64_t out_row = blockIdx.x;
-    const int64_t t = out_row / q_heads;
-    const int h = (int)(out_row % q_heads);
-    int b;
-    if (a.q_starts) {
-        int lo = 0, hi = a.seqs;               // the last sequence that starts at or before t
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (a.q_starts[mid] <= t)
-                lo = mid;
-            else
-                hi = mid;
-        }
-        b = lo;
-    } else {
-        b = (int)(t / (a.T / a.seqs));
-    }
+// Barrier that orders LDS only: loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// The other half's value beside this one's: lanes l and l ^ 32 hold the same row.
+__device__ __forceinline__ u32x2 both_halves(float v) {
+    return __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+}
+
+constexpr int kTileRows = 128, kTileTokens = 64;
+
+// Many rows (128 a workgroup, 32 a wavefront): 64 tokens at a time are decoded once into LDS
+// for all four wavefronts, the next ones' codes in flight meanwhile; 32x32x16 products with the
+// rows as columns, as above. Keys lie in rows of 2 D + 16 bytes, values in rows of 2 D + 64:
+// the fragment reads (32 keys x 16 bytes; 4 values x 64 bytes) then use every bank alike. O is
+// rescaled only in tiles that raise some row's maximum (otherwise the factor is 1).
+//
+// Workgroup -> problem: every 8th workgroup goes to one XCD; a key/value head of a sequence is
+// given to one XCD with all its row tiles, the last ones (which see the most keys) first.
+template <int FMT, int D>
+__global__ void __launch_bounds__(256, D <= 128 ? 2 : 1)
+kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
+    constexpr int TT = kTileTokens;
+    constexpr int VU = FMT == KV_FP8 ? 16 : 32;        // a unit: 16 bytes of codes
+    constexpr int VT = D / VU, UNITS = TT * VT, NU = (UNITS + 255) / 256;
+    constexpr int CB = FMT == KV_FP8 ? D : D / 2;
+    constexpr int RSK = 2 * D + 16, RSV = 2 * D + 64;
+    constexpr int KS = D / 16, F = D / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t keys[TT * RSK];
+    __shared__ __attribute__((aligned(16))) uint8_t values[TT * RSV];
+    __shared__ Places places;
+    __shared__ uint8_t nan_unit[UNITS];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r32 = lane & 31, h = lane >> 5;
+    const int slot = blockIdx.x >> 3, per = tiles * sp.splits;
+    const int pair = __builtin_amdgcn_readfirstlane(slot / per) * 8 + (blockIdx.x & 7);
+    if (pair >= a.seqs * c.heads)
+        return;
+    const int in = slot % per, split = __builtin_amdgcn_readfirstlane(in % sp.splits);
+    const int b = __builtin_amdgcn_readfirstlane(pair / c.heads), head = pair - b * c.heads;
     const Seq seq = sequence(c, a, b);
-    const int row = (int)(t - seq.q0) * a.group + h % a.group;
-    const int used = min(sp.splits, chunks_of(seq, row / tile_rows, tile_rows, a, sp.chunk));
-    if (used <= 1)
-        return;                                // its workgroup wrote the output
-    const int64_t stride = a.T * q_heads * (D + 4);
-    const float *p = sp.part + out_row * (D + 4);
-    float m = -INFINITY;
-    for (int s = threadIdx.x & 63; s < used; s += 64)
-        m = fmaxf(m, p[s * stride + D]);
+    const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
+    const int64_t v_offset = c.heads * c.head_bytes();
+
+    const int first_rt = __builtin_amdgcn_readfirstlane(tiles - 1 - in / sp.splits);
+    const int last_rt = (rows + kTileRows - 1) / kTileRows - 1;
+    // Row tiles first_rt, first_rt + tiles, ...: more than one only where max_q was too small.
+    for (int rt = first_rt; rt <= last_rt; rt += tiles) {
+        const int nch = chunks_of(seq, rt, kTileRows, a, sp.chunk);
+        const int used = min(sp.splits, nch);
+        if (split >= max(used, 1))
+            continue;
+        const int row = rt * kTileRows + wave * 32 + r32;
+        const bool live = row < rows;
+        const int qi = live ? row / a.group : 0;
+        const int qh = head * a.group + (live ? row - qi * a.group : 0);
+        const int limit = live ? seen(seq, qi, a.causal) : 0;
+        const int all_see = seen(seq, rt * kTileRows / a.group, a.causal);
+        const int some_see =
+            seen(seq, (min(rt * kTileRows + kTileRows, rows) - 1) / a.group, a.causal);
+        // what some row of this wavefront sees
+        const int wave_first = rt * kTileRows + wave * 32;
+        const int wave_sees =
+            wave_first < rows ? seen(seq, (min(wave_first + 32, rows) - 1) / a.group, a.causal) : 0;
+        u32x4 q[KS];
+        {
+            const uint16_t *src = a.q + (seq.q0 + qi) * a.q_token + qh * a.q_head + 8 * h;
 #pragma unroll
-    for (int d = 32; d; d >>= 1)
-        m = fmaxf(m, __shfl_xor(m, d));
-    const float base = m == -INFINITY ? 0.0f : m;
-    const int way = threadIdx.x / PER, d = threadIdx.x % PER * 4;
+            for (int s = 0; s < KS; ++s) {
+                const Bytes16 v = *reinterpret_cast<const Bytes16 *>(src + 16 * s);
+                q[s] = live ? u32x4{v.w[0], v.w[1], v.w[2], v.w[3]} : u32x4{};
+            }
+        }
+        f32x16 o[F];
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+            o[f] = f32x16{};
+        float m = -INFINITY, l = 0.0f;
+        uint32_t row_nan = 0;
+
+        for (int ch = split; ch < nch; ch += sp.splits) {
+            const int j_first = ch * sp.chunk;
+            const int j_end = min(j_first + sp.chunk, some_see);
+            const int ntile = (j_end - j_first + TT - 1) / TT;
+            __syncthreads();
+            fill_places(places, c, a, sp, b, head, j_first, j_end, ntile * (TT / 16));
+            __syncthreads();
+
+            u32x4 kc[NU], vc[NU];
+            uint32_t ks[NU], vs[NU];
+            const auto load = [&](int tile) {
+#pragma unroll
+                for (int i = 0; i < NU; ++i) {
+                    const int unit = min(i * 256 + (int)threadIdx.x, UNITS - 1);
+                    const int tok = unit / VT, part = unit % VT;
+                    const int blk = tile * (TT / 16) + tok / 16;
+                    const int at = places.at[blk] + tok % 16;
+                    const uint8_t *p = a.cache + places.page[blk];
+                    const uint32_t code = at * CB + part * 16;
+                    const uint32_t scale = c.page * CB + at * (D / 32) + part * VU / 32;
+                    kc[i] = Unit<16>::load(p + code);
+                    ks[i] = p[scale];
+                    vc[i] = Unit<16>::load(p + v_offset + code);
+                    vs[i] = p[v_offset + scale];
+                }
+            };
+            const auto decode = [&](uint8_t *dst, const u32x4 &codes, uint32_t byte) {
+                const float sc = scale_operand(byte);
+                u32x4 *d = reinterpret_cast<u32x4 *>(dst);
+                d[0] = decode_part<FMT, 0>(codes, sc);
+                d[1] = decode_part<FMT, 1>(codes, sc);
+                if constexpr (VU == 32) {
+                    d[2] = decode_part<FMT, 2>(codes, sc);
+                    d[3] = decode_part<FMT, 3>(codes, sc);
+                }
+            };
+            load(0);
+            for (int tile = 0; tile < ntile; ++tile) {
+                const int j0 = j_first + tile * TT;
+                const bool part_seen = j0 + TT > all_see;
+                if (tile > 0)
+                    lds_barrier();       // every wavefront has read the last tile
+                bool any_nan = false;
+#pragma unroll
+                for (int i = 0; i < NU; ++i) {
+                    const int unit = i * 256 + threadIdx.x, tok = unit / VT, part = unit % VT;
+                    if (UNITS % 256 != 0 && unit >= UNITS)
+                        break;
+                    if (part_seen) {
+                        // Values past the end, and NaN blocks where only some rows see them,
+                        // become zeros (a zero weight would not silence them).
+                        const bool past = j0 + tok >= seq.kv;
+                        const bool nan = vs[i] == kNaNScale && !past;
+                        any_nan |= nan;
+                        nan_unit[unit] = nan;
+                        if (past || nan) {
+                            vc[i] = u32x4{};
+                            vs[i] = 0;
+                        }
+                    }
+                    decode(keys + tok * RSK + part * VU * 2, kc[i], ks[i]);
+                    decode(values + tok * RSV + part * VU * 2, vc[i], vs[i]);
+                }
+                if (tile + 1 < ntile)
+                    load(tile + 1);
+                if (part_seen) {
+                    if (__syncthreads_or(any_nan))     // rare: who sees the NaN blocks
+                        for (int unit = 0; unit < UNITS; ++unit)
+                            if (nan_unit[unit] && j0 + unit / VT < limit)
+                                row_nan |= 1u << (unit % VT * VU / 32);
+                } else {
+                    lds_barrier();
+                }
+                if (j0 >= wave_sees)
+                    continue;
+
+                // Scores: token 32 t + 8 (i / 4) + 4 h + i % 4 in s[t][i].
+                f32x16 s[2] = {f32x16{}, f32x16{}};
+                const uint8_t *kp = keys + r32 * RSK + h * 16;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            *reinterpret_cast<const bf16x8 *>(kp + t * 32 * RSK + k * 32),
+                            __builtin_bit_cast(bf16x8, q[k]), s[t], 0, 0, 0);
+                float top = -INFINITY;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float v = s[t][i] * a.scale;
+                        if (part_seen)
+                            v = j0 + 32 * t + 8 * (i / 4) + 4 * h + i % 4 < limit ? v : -INFINITY;
+                        s[t][i] = v;
+                        top = fmaxf(top, v);
+                    }
+                const u32x2 tops = both_halves(top);
+                top = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])), m);
+                if (__any(top > m)) {
+                    const float keep = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+                    l *= keep;
+#pragma unroll
+                    for (int f = 0; f < F; ++f)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            o[f][i] *= keep;
+                    m = top;
+                }
+                const float base = m == -INFINITY ? 0.0f : m;
+                u32x4 p[4];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        const float x = __builtin_amdgcn_exp2f(s[t][i] - base);
+                        const float y = __builtin_amdgcn_exp2f(s[t][i + 1] - base);
+                        l += x + y;
+                        p[2 * t + i / 8][i % 8 / 2] = pack_bf16(x, y);
+                    }
+                // Step u of 16 tokens: half h takes tokens 4h + 0 .. 3 and 8 + 4h + 0 .. 3.
+                typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+                const uint8_t *vp = values + (4 * h + ((lane & 15) >> 2)) * RSV +
+                                    ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int f = 0; f < F; ++f) {
+                        const uint8_t *src = vp + 16 * u * RSV + f * 64;
+                        const u32x2 x = __builtin_bit_cast(
+                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)src));
+                        const u32x2 y = __builtin_bit_cast(
+                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(src + 8 * RSV)));
+                        o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]}),
+                            __builtin_bit_cast(bf16x8, p[u]), o[f], 0, 0, 0);
+                    }
+            }
+        }
+
+        const u32x2 ls = both_halves(l);
+        l = __uint_as_float(ls[0]) + __uint_as_float(ls[1]);
+        if (!live)
+            continue;        // the next row tile's barriers are reached all the same
+        const int64_t out_row = (seq.q0 + qi) * q_heads + qh;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        float *const part = sp.part + (split * a.T * q_heads + out_row) * (D + 4);
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+            const bool nan = row_nan >> f & 1;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * f + 2 * i + 4 * h;
+                f32x4 v = {o[f][i], o[f][i + 1], o[f][i + 2], o[f][i + 3]};
+                if (nan)
+                    v = f32x4{NAN, NAN, NAN, NAN};
+                if (used <= 1)
+                    *reinterpret_cast<u32x2 *>(a.out + out_row * D + d) =
+                        u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+                else
+                    *reinterpret_cast<f32x4 *>(part + d) = v;
+            }
+        }
+        if (used > 1 && h == 0) {
+            part[D] = m;
+            part[D + 1] = l;
+        }
+        if (split == 0 && sp.splits > 1 && h == 0)
+            part[D + 2] = (float)used;
+    }
+}
+
+// Joins the splits of each row with weights 2^(m_s - max m): LANES lanes hold 4 outputs each of
+// a row (or of 4 LANES of its outputs), WAYS groups of them take the splits in turn.
+template <int D, int LANES, int WAYS>
+__global__ void __launch_bounds__(256)
+kv_attention_join_kernel(const float *part, int splits, int64_t rows, uint16_t *out) {
+    constexpr int PIECES = D / (4 * LANES), PER = LANES * WAYS, JOBS = 256 / PER;
+    __shared__ f32x4 red[JOBS][WAYS][LANES];
+    __shared__ float red_l[JOBS][WAYS], red_m[JOBS][WAYS];
+    const int job = threadIdx.x / PER, in = threadIdx.x % PER, way = in / LANES;
+    const int64_t id = (int64_t)blockIdx.x * JOBS + job, row = id / PIECES;
+    const int d = (int)(id % PIECES) * (4 * LANES) + in % LANES * 4;
+    const bool live = job < JOBS && row < rows;
+    const float *p = part + (live ? row : 0) * (D + 4);
+    const int64_t stride = rows * (D + 4);
+    const int used = live ? min((int)p[D + 2], splits) : 0;
+    float m = -INFINITY, l = 0.0f;
     f32x4 v = {};
-    float l = 0.0f;
-    if (way < WAYS)
+    if (used > 1) {
         for (int s = way; s < used; s += WAYS) {
-            const float w = __builtin_amdgcn_exp2f(p[s * stride + D] - base);
-            l += w * p[s * stride + D + 1];
+            const float mm = p[s * stride + D], ll = p[s * stride + D + 1];
             const f32x4 x = *reinterpret_cast<const f32x4 *>(p + s * stride + d);
+            const float top = fmaxf(m, mm), base = top == -INFINITY ? 0.0f : top;
+            const float keep = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(mm - base);
+            m = top;
+            l = l * keep + ll * w;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                v[e] = __builtin_fmaf(w, x[e], v[e]);
+                v[e] = v[e] * keep + x[e] * w;
         }
-    if (way < WAYS) {
-        *reinterpret_cast<f32x4 *>(&red[way][d]) = v;
-        if (d == 0)
-            red[way][D] = l;
     }
-    __syncthreads();
-    if (way == 0) {
+    if constexpr (WAYS > 1) {
+        if (live) {
+            red[job][way][in % LANES] = v;
+            if (in % LANES == 0) {
+                red_l[job][way] = l;
+                red_m[job][way] = m;
+            }
+        }
+        __syncthreads();
+        if (way > 0 || used <= 1)
+            return;
+        float top = m;
+#pragma unroll
+        for (int w = 1; w < WAYS; ++w)
+            top = fmaxf(top, red_m[job][w]);
+        const float base = top == -INFINITY ? 0.0f : top, mine = __builtin_amdgcn_exp2f(m - base);
+        l *= mine;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] *= mine;
 #pragma unroll
         for (int w = 1; w < WAYS; ++w) {
-            v += *reinterpret_cast<const f32x4 *>(&red[w][d]);
-            l += red[w][D];
+            const float f = __builtin_amdgcn_exp2f(red_m[job][w] - base);
+            const f32x4 x = red[job][w][in % LANES];
+            l += red_l[job][w] * f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] += x[e] * f;
         }
+    }
+    if (used > 1) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        *reinterpret_cast<u32x2 *>(a.out + out_row * D + d) =
+        *reinterpret_cast<u32x2 *>(out + row * D + d) =
             u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
     }
 }
 
-// Chunks: long enough that a partial result (4 (dim + 4) bytes a row) is little beside the
-// keys and values it stands for, short enough to fill the card.
-Split split_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
-    const int64_t tiles = ((int64_t)max_q * group + kSplitRows - 1) / kSplitRows;
-    const int64_t total = (int64_t)seqs * c.heads * tiles * max_kv;
-    int64_t chunk = (total / 4096 + 127) / 128 * 128;
-    chunk = chunk < 512 ? 512 : chunk > kMaxChunk ? kMaxChunk : chunk;
+template <int D, int LANES, int WAYS>
+hipError_t launch_join(const Split &sp, int64_t rows, uint16_t *out, hipStream_t s) {
+    constexpr int jobs = 256 / (LANES * WAYS), pieces = D / (4 * LANES);
+    const int64_t blocks = (rows * pieces + jobs - 1) / jobs;
+    if (blocks > 0x7FFFFFFF)
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL((kv_attention_join_kernel<D, LANES, WAYS>), dim3((unsigned)blocks), dim3(256), 0, s,
+                       sp.part, sp.splits, rows, out);
+    return hipGetLastError();
+}
+
+// Rows of a sequence and head from which the tile kernel runs. It decodes keys and values once
+// for 128 rows, the other one once for 16.
+constexpr int kManyRows = 48;
+
+bool many_rows(int group, int max_q) { return (int64_t)max_q * group >= kManyRows; }
+
+// How many ways the keys are divided. A partial result is 4 (dim + 4) bytes a row to write and
+// to read, and a workgroup takes some microseconds to start, so only as many as fill the card.
+Split split_of(const KvShape &c, int seqs, int group, int max_q, int max_kv) {
+    const bool many = many_rows(group, max_q);
+    const int tile_rows = many ? kTileRows : kSplitRows;
+    const int64_t tiles = ((int64_t)max_q * group + tile_rows - 1) / tile_rows;
+    const int64_t blocks = (int64_t)seqs * c.heads * tiles;
+    // Few rows: two workgroups a CU for one sequence (8 heads, 200000 tokens of 4 bits: 48 us,
+    // with four a CU 53), eight where several may differ in length, as max_kv bounds them all;
+    // of 512 tokens at least, of 2048 where the heads alone fill the card twice over (64 x 8
+    // heads of 2000 tokens: 52 us, in four parts 60). Many rows: 512 workgroups of 1024 tokens.
+    const int64_t want = many || seqs == 1 ? 512 : 2048;
+    const int64_t least = many ? 1024 : blocks >= 512 ? 2048 : 512;
+    int64_t splits = std::min((want + blocks - 1) / blocks, (max_kv + least - 1) / least);
+    if (many && blocks >= 256)
+        splits = 1;
     Split sp;
-    sp.chunk = (int)chunk;
-    sp.splits = (int)((max_kv + chunk - 1) / chunk);
-    if (sp.splits < 1)
-        sp.splits = 1;
+    sp.splits = (int)std::max<int64_t>(splits, 1);
+    const int64_t chunk = ((max_kv + sp.splits - 1) / sp.splits + 127) / 128 * 128;
+    sp.chunk = (int)std::min<int64_t>(std::max<int64_t>(chunk, 128), kMaxChunk);
+    const uint32_t pb = (uint32_t)c.page / 16;
+    sp.magic = (((uint64_t)1 << 32) + pb - 1) / pb;
     sp.part = nullptr;
-    sp.magic = 0;
     return sp;
 }
 
@@ -509,31 +811,39 @@ Split split_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int 
 
 size_t kv_attention_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_q,
                                     int max_kv) {
-    const Split sp = split_of(c, T, seqs, group, max_q, max_kv);
+    const Split sp = split_of(c, seqs, group, max_q, max_kv);
     return sp.splits == 1 ? 0 : (size_t)sp.splits * T * c.heads * group * (c.dim + 4) * 4;
 }
 
-hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, size_t,
-                               hipStream_t s) {
-    Split sp = split_of(c, a.T, a.seqs, a.group, a.max_q, a.max_kv);
+hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
+    Split sp = split_of(c, a.seqs, a.group, a.max_q, a.max_kv);
     sp.part = static_cast<float *>(ws);
-    const uint32_t pb = (uint32_t)c.page / 16;
-    sp.magic = (((uint64_t)1 << 32) + pb - 1) / pb;
-    const int64_t tiles = ((int64_t)a.max_q * a.group + kSplitRows - 1) / kSplitRows;
-    const int64_t x = (int64_t)sp.splits * c.heads * a.seqs, rows = a.T * c.heads * a.group;
-    if (x > 0x7FFFFFFF || rows > 0x7FFFFFFF)
+    const bool many = many_rows(a.group, a.max_q);
+    const int tile_rows = many ? kTileRows : kSplitRows;
+    const int64_t pairs = (int64_t)c.heads * a.seqs, rows = a.T * c.heads * a.group;
+    const int64_t tiles =
+        std::min<int64_t>(((int64_t)a.max_q * a.group + tile_rows - 1) / tile_rows, 65535);
+    const int64_t blocks = many ? (pairs + 7) / 8 * 8 * tiles * sp.splits : pairs * sp.splits;
+    if (blocks > 0x7FFFFFFF || rows > 0x7FFFFFFF)
         return hipErrorInvalidValue;
-    const dim3 grid((unsigned)x, (unsigned)(tiles > 65535 ? 65535 : tiles));
-    const auto go = [&](auto dim) {
-        constexpr int D = decltype(dim)::value;
-        if (c.fmt == KV_FP8)
-            hipLaunchKernelGGL((kv_attention_split_kernel<KV_FP8, D>), grid, dim3(256), 0, s, c, a, sp);
+    const dim3 grid((unsigned)blocks, many ? 1u : (unsigned)tiles);
+    const auto run = [&](auto dim, auto format) {
+        constexpr int D = decltype(dim)::value, FMT = decltype(format)::value;
+        if (many)
+            hipLaunchKernelGGL((kv_attention_tile_kernel<FMT, D>), grid, dim3(256), 0, s, c, a, sp,
+                               (int)tiles);
         else
-            hipLaunchKernelGGL((kv_attention_split_kernel<KV_FP4, D>), grid, dim3(256), 0, s, c, a, sp);
-        if (sp.splits > 1)
-            hipLaunchKernelGGL((kv_attention_join_kernel<D>), dim3((unsigned)rows), dim3(256), 0, s, c,
-                               a, sp, kSplitRows);
-        return hipGetLastError();
+            hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D>), grid, dim3(256), 0, s, c, a, sp);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || sp.splits == 1)
+            return e;
+        // Few splits: a row by D / 4 lanes. Many: 32 outputs of a row by 32 groups of 8 lanes.
+        return sp.splits <= 16 ? launch_join<D, D / 4, 1>(sp, rows, a.out, s)
+                               : launch_join<D, 8, 32>(sp, rows, a.out, s);
+    };
+    const auto go = [&](auto dim) {
+        return c.fmt == KV_FP8 ? run(dim, std::integral_constant<int, KV_FP8>{})
+                               : run(dim, std::integral_constant<int, KV_FP4>{});
     };
     switch (c.dim) {
     case 64: return go(std::integral_constant<int, 64>{});

@@ -251,7 +251,7 @@ w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head
     const size_t need = kv_attention_workspace_bytes(c, T, seqs, group, a.max_q, max_kv);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
         return W8A8_ERR_WORKSPACE;
-    return from_hip(launch_kv_attention(c, a, workspace, workspace_bytes, as_stream(stream)));
+    return from_hip(launch_kv_attention(c, a, workspace, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -69,7 +69,6 @@ struct KvAttnArgs {
 
 size_t kv_attention_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_q,
                                     int max_kv);
-hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, size_t ws_bytes,
-                               hipStream_t s);
+hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s);
 
 }  // namespace w8a8
