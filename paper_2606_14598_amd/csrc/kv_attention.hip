@@ -42,6 +42,10 @@ struct Split {
     uint64_t magic;  // n / (page / 16) = n * magic >> 32 for n < 2^22 (kMaxTokens / 16)
 };
 
+// The maximum that exponents are taken from may lag behind by this much: O and l are rescaled
+// only when a row's maximum rises further. Weights up to 2^8 instead of 1 lose nothing, as
+// float32 sums and bf16 roundings are relative; a rescaling costs as much as a product.
+constexpr float kSlack = 8.0f;
 constexpr int kMaxChunk = 4096;
 constexpr int kSplitRows = 16;
 static_assert(W8A8_KV_MAX_TOKENS / 16 <= 1 << 22 && W8A8_KV_MAX_PAGE / 16 <= 1 << 10, "magic");
@@ -341,9 +345,9 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                         top = fmaxf(top, v);
                     }
                 top = fmaxf(max_of_row(top), m);
-                const float base = top == -INFINITY ? 0.0f : top;
-                if (__any(top > m)) {      // else every factor is 1
-                    const float keep = __builtin_amdgcn_exp2f(m - base);   // 0 for the first keys
+                if (__any(top > m + kSlack)) {
+                    const float keep =
+                        __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
                     l *= keep;
 #pragma unroll
                     for (int f = 0; f < F; ++f)
@@ -352,6 +356,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                             o[f][e] *= keep;
                     m = top;
                 }
+                const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -457,8 +462,7 @@ constexpr int kTileRows = 128, kTileTokens = 64;
 // Many rows (128 a workgroup, 32 a wavefront): 64 tokens at a time are decoded once into LDS
 // for all four wavefronts, the next ones' codes in flight meanwhile; 32x32x16 products with the
 // rows as columns, as above. Keys lie in rows of 2 D + 16 bytes, values in rows of 2 D + 64:
-// the fragment reads (32 keys x 16 bytes; 4 values x 64 bytes) then use every bank alike. O is
-// rescaled only in tiles that raise some row's maximum (otherwise the factor is 1).
+// the fragment reads (32 keys x 16 bytes; 4 values x 64 bytes) then use every bank alike.
 //
 // Workgroup -> problem: every 8th workgroup goes to one XCD; a key/value head of a sequence is
 // given to one XCD with all its row tiles, the last ones (which see the most keys) first.
@@ -624,8 +628,9 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                     }
                 const u32x2 tops = both_halves(top);
                 top = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])), m);
-                if (__any(top > m)) {
-                    const float keep = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+                if (__any(top > m + kSlack)) {
+                    const float keep =
+                        __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
                     l *= keep;
 #pragma unroll
                     for (int f = 0; f < F; ++f)

@@ -15,117 +15,174 @@ namespace {
 
 using namespace mx;
 
-struct Place {
-    int64_t t;        // token of the call
-    int kv, head, e;  // keys or values, head, first of the lane's 8 elements
-    int64_t codes, scales;   // of the token's element 0 in the cache; codes < 0: padding
+// A wavefront takes one token and up to 64 * kLoads of its units of 8 values, keys then values;
+// where the token lies in the cache is then the same for all lanes, and the divisions that it
+// takes are done once.
+constexpr int kLoads = 4;
+
+struct Token {
+    int64_t t;                 // of the call; past its tokens: nothing to do
+    int64_t keys;              // its page in the cache; below 0 for padding
+    int at;                    // its place in the page
 };
 
-// Lane index g over [T][2][heads][dim / 8].
-__device__ __forceinline__ Place place(int64_t g, const KvShape &c, const int64_t *slots) {
-    Place p;
-    const int per = c.dim / 8;
-    p.e = (int)(g % per) * 8;
-    const int64_t h = g / per;
-    p.head = (int)(h % c.heads);
-    p.kv = (int)(h / c.heads % 2);
-    p.t = h / c.heads / 2;
-    const int64_t slot = slots[p.t];
-    if (slot < 0 || slot >= c.pages * c.page) {
-        p.codes = p.scales = -1;
-        return p;
-    }
-    const int64_t base = ((slot / c.page * 2 + p.kv) * c.heads + p.head) * c.head_bytes();
-    const int at = (int)(slot % c.page);
-    p.codes = base + (int64_t)at * c.code_bytes();
-    p.scales = base + (int64_t)c.page * c.code_bytes() + at * (c.dim / 32);
-    return p;
+__device__ __forceinline__ Token token_of(const KvShape &c, const int64_t *slots, int64_t T) {
+    Token k;
+    k.t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    k.keys = -1;
+    k.at = 0;
+    if (k.t >= T)
+        return k;
+    const int64_t slot = slots[k.t];
+    if (slot < 0 || slot >= c.pages * c.page)
+        return k;
+    const int64_t page = slot >> 31 ? slot / c.page : (uint32_t)slot / (uint32_t)c.page;
+    k.at = (int)(slot - page * c.page);
+    k.keys = page * 2 * c.heads * c.head_bytes();
+    return k;
 }
 
-template <int FMT>
-__global__ void __launch_bounds__(256)
-kv_write_kernel(uint8_t *cache, KvShape c, KvRows k, KvRows v, const int64_t *slots, int64_t n) {
-    const int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (g >= n)          // n is a multiple of the four lanes of a block
-        return;
-    const Place p = place(g, c, slots);
-    if (p.codes < 0)
-        return;
-    const KvRows &src = p.kv ? v : k;
-    const Bytes16 in =
-        *reinterpret_cast<const Bytes16 *>(src.p + p.t * src.token + p.head * src.head + p.e);
-    const uint32_t w[4] = {in.w[0], in.w[1], in.w[2], in.w[3]};
-    uint32_t m = max_halves(max_halves(magnitudes(w[0]), magnitudes(w[1])),
-                            max_halves(magnitudes(w[2]), magnitudes(w[3])));
-    m = quad_max(max(m & 0xFFFFu, m >> 16));
-    const uint32_t byte = scale_byte<FMT == KV_FP8 ? kTop8 : kTop4>(m >> 7);
-    const bool bad = byte == kNaNScale;
-    const float s = scale_operand(byte);
-    if constexpr (FMT == KV_FP8) {
-        uint2 q = make_uint2(encode8_bf16(w[0], w[1], m >> 7, s), encode8_bf16(w[2], w[3], m >> 7, s));
-        if (bad)
-            q = make_uint2(0, 0);
-        *reinterpret_cast<uint2 *>(cache + p.codes + p.e) = q;
-    } else {
-        *reinterpret_cast<uint32_t *>(cache + p.codes + p.e / 2) = bad ? 0 : encode4_bf16(w, s);
+// Unit u of a token: 8 values of keys or values; heads * 2 * D / 8 of them.
+template <int FMT, int D>
+struct Unit8 {
+    static constexpr int CB = FMT == KV_FP8 ? D : D / 2;
+    int head, e;               // head over keys, then values; first of the 8 values
+    int64_t codes, scale;      // in the cache
+    __device__ __forceinline__ Unit8(const KvShape &c, const Token &k, int u) {
+        head = u / (D / 8);
+        e = u % (D / 8) * 8;
+        const int64_t base = k.keys + head * c.head_bytes();
+        codes = base + k.at * CB + (FMT == KV_FP8 ? e : e / 2);
+        scale = base + c.page * CB + k.at * (D / 32) + e / 32;
     }
-    if (p.e % 32 == 0)
-        cache[p.scales + p.e / 32] = (uint8_t)byte;
-}
+};
 
-template <int FMT>
+template <int FMT, int D>
 __global__ void __launch_bounds__(256)
-kv_read_kernel(const uint8_t *cache, KvShape c, KvRows k, KvRows v, const int64_t *slots,
-               int64_t n) {
-    const int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (g >= n)
+kv_write_kernel(uint8_t *cache, KvShape c, KvRows k, KvRows v, const int64_t *slots, int64_t T) {
+    const Token tok = token_of(c, slots, T);
+    if (tok.keys < 0)
         return;
-    const Place p = place(g, c, slots);
-    Bytes16 out = {};
-    if (p.codes >= 0) {
-        const float s = scale_operand(cache[p.scales + p.e / 32]);
+    const int units = 2 * c.heads * (D / 8), u0 = blockIdx.y * (64 * kLoads) + (threadIdx.x & 63);
+    Bytes16 in[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int u = min(u0 + 64 * i, units - 1), head = u / (D / 8), e = u % (D / 8) * 8;
+        const uint16_t *src = head < c.heads ? k.p + tok.t * k.token + head * k.head
+                                             : v.p + tok.t * v.token + (head - c.heads) * v.head;
+        in[i] = *reinterpret_cast<const Bytes16 *>(src + e);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int u = u0 + 64 * i;
+        if (u >= units)        // units is a multiple of the four lanes of a block
+            return;
+        const Unit8<FMT, D> unit(c, tok, u);
+        const uint32_t w[4] = {in[i].w[0], in[i].w[1], in[i].w[2], in[i].w[3]};
+        uint32_t m = max_halves(max_halves(magnitudes(w[0]), magnitudes(w[1])),
+                                max_halves(magnitudes(w[2]), magnitudes(w[3])));
+        m = quad_max(max(m & 0xFFFFu, m >> 16));
+        const uint32_t byte = scale_byte<FMT == KV_FP8 ? kTop8 : kTop4>(m >> 7);
+        const bool bad = byte == kNaNScale;
+        const float s = scale_operand(byte);
         if constexpr (FMT == KV_FP8) {
-            const uint2 q = *reinterpret_cast<const uint2 *>(cache + p.codes + p.e);
-            out.w[0] = decode8<0>(q.x, s);
-            out.w[1] = decode8<1>(q.x, s);
-            out.w[2] = decode8<0>(q.y, s);
-            out.w[3] = decode8<1>(q.y, s);
+            uint2 q = make_uint2(encode8_bf16(w[0], w[1], m >> 7, s), encode8_bf16(w[2], w[3], m >> 7, s));
+            if (bad)
+                q = make_uint2(0, 0);
+            *reinterpret_cast<uint2 *>(cache + unit.codes) = q;
         } else {
-            const uint32_t q = *reinterpret_cast<const uint32_t *>(cache + p.codes + p.e / 2);
-            out.w[0] = decode4<0>(q, s);
-            out.w[1] = decode4<1>(q, s);
-            out.w[2] = decode4<2>(q, s);
-            out.w[3] = decode4<3>(q, s);
+            *reinterpret_cast<uint32_t *>(cache + unit.codes) = bad ? 0 : encode4_bf16(w, s);
+        }
+        if (unit.e % 32 == 0)
+            cache[unit.scale] = (uint8_t)byte;
+    }
+}
+
+template <int FMT, int D>
+__global__ void __launch_bounds__(256)
+kv_read_kernel(const uint8_t *cache, KvShape c, KvRows k, KvRows v, const int64_t *slots, int64_t T) {
+    const Token tok = token_of(c, slots, T);
+    if (tok.t >= T)
+        return;
+    const int units = 2 * c.heads * (D / 8), u0 = blockIdx.y * (64 * kLoads) + (threadIdx.x & 63);
+    uint2 codes[kLoads];
+    uint32_t byte[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        codes[i] = make_uint2(0, 0);
+        byte[i] = 0;
+        if (tok.keys >= 0) {
+            const Unit8<FMT, D> unit(c, tok, min(u0 + 64 * i, units - 1));
+            byte[i] = cache[unit.scale];
+            if constexpr (FMT == KV_FP8)
+                codes[i] = *reinterpret_cast<const uint2 *>(cache + unit.codes);
+            else
+                codes[i].x = *reinterpret_cast<const uint32_t *>(cache + unit.codes);
         }
     }
-    const KvRows &dst = p.kv ? v : k;
-    *reinterpret_cast<Bytes16 *>(dst.p + p.t * dst.token + p.head * dst.head + p.e) = out;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int u = u0 + 64 * i, head = u / (D / 8), e = u % (D / 8) * 8;
+        if (u >= units)
+            return;
+        const float s = scale_operand(byte[i]);
+        Bytes16 out;
+        if constexpr (FMT == KV_FP8) {
+            out.w[0] = decode8<0>(codes[i].x, s);
+            out.w[1] = decode8<1>(codes[i].x, s);
+            out.w[2] = decode8<0>(codes[i].y, s);
+            out.w[3] = decode8<1>(codes[i].y, s);
+        } else {
+            out.w[0] = decode4<0>(codes[i].x, s);
+            out.w[1] = decode4<1>(codes[i].x, s);
+            out.w[2] = decode4<2>(codes[i].x, s);
+            out.w[3] = decode4<3>(codes[i].x, s);
+        }
+        uint16_t *dst = head < c.heads ? k.p + tok.t * k.token + head * k.head
+                                       : v.p + tok.t * v.token + (head - c.heads) * v.head;
+        *reinterpret_cast<Bytes16 *>(dst + e) = out;
+    }
+}
+
+// Calls go(kernel format, head_dim) with both as compile-time constants.
+template <typename F>
+hipError_t by_shape(const KvShape &c, int64_t T, F go) {
+    const int64_t blocks = (T + 3) / 4, pieces = (2 * c.heads * (c.dim / 8) + 64 * kLoads - 1) / (64 * kLoads);
+    if (T == 0)
+        return hipSuccess;
+    if (blocks > 0x7FFFFFFF || pieces > 65535)
+        return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks, (unsigned)pieces);
+    const auto with_dim = [&](auto dim) {
+        return c.fmt == KV_FP8 ? go(std::integral_constant<int, KV_FP8>{}, dim, grid)
+                               : go(std::integral_constant<int, KV_FP4>{}, dim, grid);
+    };
+    switch (c.dim) {
+    case 64: return with_dim(std::integral_constant<int, 64>{});
+    case 128: return with_dim(std::integral_constant<int, 128>{});
+    case 192: return with_dim(std::integral_constant<int, 192>{});
+    default: return with_dim(std::integral_constant<int, 256>{});
+    }
 }
 
 }  // namespace
 
 hipError_t launch_kv_write(uint8_t *cache, const KvShape &c, const KvRows &k, const KvRows &v,
                            const int64_t *slots, int64_t T, hipStream_t s) {
-    const int64_t n = T * 2 * c.heads * (c.dim / 8), blocks = (n + 255) / 256;
-    if (blocks == 0)
-        return hipSuccess;
-    if (blocks > 0x7FFFFFFF)
-        return hipErrorInvalidValue;
-    hipLaunchKernelGGL(c.fmt == KV_FP8 ? kv_write_kernel<KV_FP8> : kv_write_kernel<KV_FP4>,
-                       dim3((unsigned)blocks), dim3(256), 0, s, cache, c, k, v, slots, n);
-    return hipGetLastError();
+    return by_shape(c, T, [&](auto fmt, auto dim, dim3 grid) {
+        hipLaunchKernelGGL((kv_write_kernel<decltype(fmt)::value, decltype(dim)::value>), grid, dim3(256), 0,
+                           s, cache, c, k, v, slots, T);
+        return hipGetLastError();
+    });
 }
 
 hipError_t launch_kv_read(const uint8_t *cache, const KvShape &c, const KvRows &k,
                           const KvRows &v, const int64_t *slots, int64_t T, hipStream_t s) {
-    const int64_t n = T * 2 * c.heads * (c.dim / 8), blocks = (n + 255) / 256;
-    if (blocks == 0)
-        return hipSuccess;
-    if (blocks > 0x7FFFFFFF)
-        return hipErrorInvalidValue;
-    hipLaunchKernelGGL(c.fmt == KV_FP8 ? kv_read_kernel<KV_FP8> : kv_read_kernel<KV_FP4>,
-                       dim3((unsigned)blocks), dim3(256), 0, s, cache, c, k, v, slots, n);
-    return hipGetLastError();
+    return by_shape(c, T, [&](auto fmt, auto dim, dim3 grid) {
+        hipLaunchKernelGGL((kv_read_kernel<decltype(fmt)::value, decltype(dim)::value>), grid, dim3(256), 0,
+                           s, cache, c, k, v, slots, T);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace w8a8

@@ -442,6 +442,12 @@ mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul)
     const int stride = (nb | 1) * 16;
     uint8_t *const token_scales = tokens + M * stride;
     if constexpr (QX) {
+        __shared__ __attribute__((aligned(16))) float gelu[ACT == ACT_GELU ? sizeof(GeluTable) / 4 : 1];
+        if constexpr (ACT == ACT_GELU) {
+            for (int i = threadIdx.x; i < (int)(sizeof(GeluTable) / 16); i += NW * 64)
+                reinterpret_cast<float4 *>(gelu)[i] = reinterpret_cast<const float4 *>(&kGeluTable)[i];
+            __syncthreads();
+        }
         // A lane quantizes 8 channels, four lanes a block.
         for (int u = threadIdx.x; u < M * nb * 4; u += NW * 64) {
             const int row = u / (nb * 4), q = u - row * (nb * 4);
@@ -450,7 +456,7 @@ mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul)
                 load_multipliers(col_mul, 8 * q, K, c);
             uint32_t v[4], byte;
             load8(x + row * K, 8 * q, K, v);
-            const uint32_t codes = quantize_quad<ACT, CM>(v, c, byte);
+            const uint32_t codes = quantize_quad<ACT, CM>(v, c, gelu, byte);
             *reinterpret_cast<uint32_t *>(tokens + row * stride + q * 4) = codes;
             if (q % 4 == 0)
                 token_scales[row * nb + q / 4] = (uint8_t)byte;

@@ -17,33 +17,55 @@ using namespace mx;
 
 // A lane holds 8 neighbouring channels, four lanes a block, a wavefront 512 channels (two
 // scale panels) of one row at a time; it takes ROWS rows one below the other, whose scale
-// bytes are neighbours in memory. No value outside a block matters to it, so nothing is
-// exchanged but the block's maximum inside its four lanes.
-constexpr int kRows = 4, kWaves = 4;
+// bytes are neighbours in memory, and has all their loads in flight at once. No value outside a
+// block matters to it, so nothing is exchanged but the block's maximum inside its four lanes.
+// GELU comes from the table of all bf16 magnitudes, copied to LDS while the rows arrive.
+constexpr int kWaves = 4;
 
-template <int ACT, bool CM>
+template <int ACT, bool CM, int ROWS>
 __global__ void __launch_bounds__(kWaves * 64)
 mx4_quant_kernel(const uint16_t *x, int64_t R, int64_t K, const float *col_mul, uint8_t *codes,
-                 uint8_t *scales, int64_t chunks) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t chunk = blockIdx.x % chunks;                  // 512 channels
-    const int64_t r0 = (blockIdx.x / chunks * kWaves + wave) * kRows;
+                 uint8_t *scales, unsigned chunks) {
+    constexpr bool GELU = ACT == ACT_GELU;
+    __shared__ __attribute__((aligned(16))) float gelu[GELU ? sizeof(GeluTable) / 4 : 1];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned group = blockIdx.x / chunks;
+    const int64_t chunk = blockIdx.x - group * chunks;          // 512 channels
+    const int64_t r0 = ((int64_t)group * kWaves + wave) * ROWS;
     const int64_t k = chunk * 512 + lane * 8;
     const int64_t row_bytes = (K + 31) / 32 * 16;
     const int64_t panel = chunk * 2 + (lane >> 5);
     const bool store_codes = k / 2 < row_bytes, store_scale = panel * 256 < K && lane % 4 == 0;
+    uint32_t w[ROWS][4];
+    if (chunk * 512 + 512 <= K) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const Bytes16 b = *reinterpret_cast<const Bytes16 *>(x + min(r0 + i, R - 1) * K + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[i][e] = b.w[e];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+            load8(x + min(r0 + i, R - 1) * K, k, K, w[i]);
+    }
     float c[8];
     if constexpr (CM)
         load_multipliers(col_mul, k, K, c);
+    if constexpr (GELU) {
+        for (int i = threadIdx.x; i < (int)(sizeof(GeluTable) / 16); i += kWaves * 64)
+            reinterpret_cast<float4 *>(gelu)[i] = reinterpret_cast<const float4 *>(&kGeluTable)[i];
+        __syncthreads();
+    }
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
         const int64_t r = r0 + i;
         if (r >= R)
             return;
-        uint32_t w[4];
-        load8(x + r * K, k, K, w);
         uint32_t byte;
-        const uint32_t q = quantize_quad<ACT, CM>(w, c, byte);
+        const uint32_t q = quantize_quad<ACT, CM>(w[i], c, gelu, byte);
         if (store_codes)
             *reinterpret_cast<uint32_t *>(codes + r * row_bytes + k / 2) = q;
         if (store_scale)
@@ -53,11 +75,10 @@ mx4_quant_kernel(const uint16_t *x, int64_t R, int64_t K, const float *col_mul, 
 
 // One lane decodes 8 channels.
 __global__ void __launch_bounds__(256)
-mx4_dequant_kernel(const uint8_t *codes, const uint8_t *scales, int64_t R, int64_t K, uint16_t *y,
-                   int64_t per_row) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r = t / per_row, k = t % per_row * 8;
-    if (r >= R)
+mx4_dequant_kernel(const uint8_t *codes, const uint8_t *scales, int64_t R, int64_t K, uint16_t *y) {
+    const int64_t r = blockIdx.y + (int64_t)blockIdx.z * 65535;
+    const int64_t k = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (r >= R || k >= K)
         return;
     const uint32_t q = *reinterpret_cast<const uint32_t *>(codes + r * ((K + 31) / 32 * 16) + k / 2);
     const float s = scale_operand(scales[((k >> 8) * R + r) * 8 + ((k >> 5) & 7)]);
@@ -85,29 +106,40 @@ hipError_t launch_mx4_quant(const uint16_t *x, int64_t R, int64_t K, int act,
     if (R == 0 || K == 0)
         return hipSuccess;
     const int64_t chunks = (K + 511) / 512;
-    const int64_t blocks = chunks * ((R + kWaves * kRows - 1) / (kWaves * kRows));
+    // Eight rows a wavefront where that leaves 16 wavefronts a CU (four of its own or fewer
+    // than 4096 in all otherwise: a row each).
+    const int rows = R * chunks >= 8 * 4096 ? 8 : 1;
+    const int64_t blocks = chunks * ((R + kWaves * rows - 1) / (kWaves * rows));
     if (blocks > 0x7FFFFFFF)
         return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(kWaves * 64);
-    const auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, block, 0, s, x, R, K, col_mul, codes, scales, chunks);
+    const auto go = [&](auto act_c, auto cm) {
+        constexpr int A = decltype(act_c)::value;
+        constexpr bool CM = decltype(cm)::value;
+        if (rows == 8)
+            hipLaunchKernelGGL((mx4_quant_kernel<A, CM, 8>), grid, block, 0, s, x, R, K, col_mul, codes,
+                               scales, (unsigned)chunks);
+        else
+            hipLaunchKernelGGL((mx4_quant_kernel<A, CM, 1>), grid, block, 0, s, x, R, K, col_mul, codes,
+                               scales, (unsigned)chunks);
         return hipGetLastError();
     };
-    if (act == ACT_GELU)
-        return col_mul ? go(mx4_quant_kernel<ACT_GELU, true>) : go(mx4_quant_kernel<ACT_GELU, false>);
-    return col_mul ? go(mx4_quant_kernel<ACT_NONE, true>) : go(mx4_quant_kernel<ACT_NONE, false>);
+    const auto with_act = [&](auto act_c) {
+        return col_mul ? go(act_c, std::true_type{}) : go(act_c, std::false_type{});
+    };
+    return act == ACT_GELU ? with_act(std::integral_constant<int, ACT_GELU>{})
+                           : with_act(std::integral_constant<int, ACT_NONE>{});
 }
 
 hipError_t launch_mx4_dequant(const uint8_t *codes, const uint8_t *scales, int64_t R, int64_t K,
                               uint16_t *y, hipStream_t s) {
     if (R == 0 || K == 0)
         return hipSuccess;
-    const int64_t per_row = (K + 7) / 8;
-    const int64_t blocks = (R * per_row + 255) / 256;
-    if (blocks > 0x7FFFFFFF)
+    const int64_t tall = (R + 65534) / 65535;
+    if (tall > 65535)
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL(mx4_dequant_kernel, dim3((unsigned)blocks), dim3(256), 0, s, codes, scales, R,
-                       K, y, per_row);
+    const dim3 grid((unsigned)((K + 2047) / 2048), (unsigned)(R < 65535 ? R : 65535), (unsigned)tall);
+    hipLaunchKernelGGL(mx4_dequant_kernel, grid, dim3(256), 0, s, codes, scales, R, K, y);
     return hipGetLastError();
 }
 

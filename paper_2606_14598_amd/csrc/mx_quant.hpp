@@ -28,10 +28,10 @@ __device__ __forceinline__ void load_multipliers(const float *col_mul, int64_t k
 }
 
 // Codes and scale byte of T(x) * c for a lane's 8 neighbouring bf16 values w; the four lanes of
-// a block (lanes 4i .. 4i + 3) call it together.
+// a block (lanes 4i .. 4i + 3) call it together. gelu: the table, in LDS (ACT_GELU).
 template <int ACT, bool CM>
 __device__ __forceinline__ uint32_t quantize_quad(const uint32_t (&w)[4], const float (&c)[8],
-                                                  uint32_t &byte) {
+                                                  const float *gelu, uint32_t &byte) {
     using namespace mx;
     uint32_t q;
     if constexpr (ACT == ACT_NONE && !CM) {
@@ -45,8 +45,8 @@ __device__ __forceinline__ uint32_t quantize_quad(const uint32_t (&w)[4], const 
         uint32_t m = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float f = bf16_to_f32((w[e / 2] >> (16 * (e & 1))) & 0xFFFFu);
-            v[e] = ACT == ACT_GELU ? gelu_f32(f) : f;
+            const uint32_t h = (w[e / 2] >> (16 * (e & 1))) & 0xFFFFu;
+            v[e] = ACT == ACT_GELU ? gelu_lookup(h, gelu) : bf16_to_f32(h);
             if constexpr (CM)
                 v[e] *= c[e];
             m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
