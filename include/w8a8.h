@@ -318,8 +318,9 @@ w8a8_status w8a8_mx4_gemm(const uint8_t *xq, const uint8_t *x_scale, const uint8
 size_t w8a8_mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 
 /* The whole 4-bit linear: x [M,K] bf16 quantized as by w8a8_mx4_quantize, then
- * w8a8_mx4_gemm. workspace: w8a8_mx4_linear_workspace_bytes(M,N,K) bytes, 256-byte
- * aligned. */
+ * w8a8_mx4_gemm; few tokens run as one launch, which quantizes them itself.
+ * workspace: w8a8_mx4_linear_workspace_bytes(M,N,K) bytes, 256-byte aligned (NULL allowed
+ * when that is 0). */
 w8a8_status w8a8_mx4_linear(const uint16_t *x, int act, const float *col_mul, const uint8_t *wq,
                             const uint8_t *w_scale, const uint16_t *bias, uint16_t *y, int64_t M,
                             int64_t N, int64_t K, void *workspace, size_t workspace_bytes,

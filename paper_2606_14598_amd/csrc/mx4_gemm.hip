@@ -518,21 +518,22 @@ mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul)
 
 // ---------------------------------------------------------------- what runs for a shape
 
-// A workgroup of tile t takes start + panel * (its K-panels) microseconds; further rounds of
-// 256 workgroups cost `more` of the first (under 1 where two share a CU, over 1 where the clock
-// falls under the load). Fitted to 200 random shapes (M 17 .. 8192, N 64 .. 20480, K 64 ..
-// 24576) with every tile and 1 to 16 K-ranges: the choice is 1% slower than the best measured
-// one in the geometric mean, 15% at most.
+// A workgroup of tile t takes start + panel * (its K-panels) microseconds alone. Each full round
+// of 256 workgroups costs `more` of that (under 1 where two share a CU), the last one's share of
+// the CUs `fill` (the clock falls as more of them work). Fitted to 245 random shapes (M 17 ..
+// 8192, N 64 .. 20480, K 64 .. 24576) with every tile and 1 to 16 K-ranges: the choice is 1%
+// slower than the best measured one in the geometric mean, 15% at most.
 struct TileCost {
     int tm, tn;
-    float start, panel, more;
+    float start, panel, more, fill;
 };
 constexpr TileCost kTiles[] = {
-    {288, 256, 5.87f, 1.54f, 1.28f}, {256, 256, 5.74f, 1.32f, 1.17f}, {192, 256, 4.88f, 1.07f, 1.10f},
-    {128, 256, 4.36f, 0.68f, 1.03f}, {128, 128, 3.75f, 0.47f, 1.03f}, {64, 128, 2.14f, 0.376f, 0.83f},
-    {64, 64, 1.64f, 0.269f, 0.76f},
+    {288, 256, 5.36f, 1.48f, 1.30f, 0.35f}, {256, 256, 5.10f, 1.30f, 1.22f, 0.32f},
+    {192, 256, 4.02f, 1.10f, 1.17f, 0.29f}, {128, 256, 3.14f, 0.70f, 1.21f, 0.54f},
+    {128, 128, 2.90f, 0.475f, 1.07f, 0.43f}, {64, 128, 1.52f, 0.367f, 0.87f, 0.46f},
+    {64, 64, 1.19f, 0.26f, 0.79f, 0.39f},
 };
-constexpr float kReduce = 3.9f, kReducePerMega = 1.66f;   // joining K-ranges: + per 2^20 partials
+constexpr float kReduce = 4.4f, kReducePerMega = 1.33f;   // joining K-ranges: + per 10^6 partials
 constexpr int kCus = 256;
 constexpr int kStreamTokens = 16;     // the streaming kernel up to here: one token fragment
 // It quantizes up to so many values itself: each workgroup does them all again, 2 us for 16384
@@ -560,9 +561,10 @@ Plan plan_of(int64_t M, int64_t N, int64_t nb) {
         for (int splits = 1; splits <= 16; splits *= 2) {
             if (splits > 1 && (tiles * splits > 2 * kCus || panels < 3 * splits))
                 break;
-            const float rounds = (float)((tiles * splits + kCus - 1) / kCus);
+            const int64_t blocks = tiles * splits, full = (blocks - 1) / kCus;
+            const float last = (float)(blocks - full * kCus) / (float)kCus;
             float us = (c.start + c.panel * (float)((panels + splits - 1) / splits)) *
-                       (1.0f + (rounds - 1.0f) * c.more);
+                       (1.0f + (float)full * c.more + last * c.fill);
             if (splits > 1)
                 us += kReduce + kReducePerMega * (float)splits * (float)M * (float)N / 1e6f;
             if (us < least) {

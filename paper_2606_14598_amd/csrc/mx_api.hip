@@ -122,7 +122,7 @@ w8a8_status w8a8_mx4_gemm(const uint8_t *xq, const uint8_t *x_scale, const uint8
 }
 
 size_t w8a8_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (check_product(M, N, K) != W8A8_OK || M == 0 || N == 0)
+    if (check_product(M, N, K) != W8A8_OK || M == 0 || N == 0 || mx4_linear_one_launch(M, K))
         return 0;
     return align_up(code_bytes(M, K)) + align_up(scale_bytes(M, K)) +
            mx4_gemm_workspace_bytes(M, N, blocks_of(K));

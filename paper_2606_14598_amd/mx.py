@@ -14,9 +14,15 @@ formats and rules); imported by the package, whose conventions hold here too.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import (_act, _check, _check_out, _col_mul, _launch, _ptr, _same_device, _size, _workspace)
+
+# Sizes of workspaces and caches, pure functions of a call's sizes, by the sizes asked last: a
+# call's host time is what a small one costs.
+_bytes = functools.lru_cache(maxsize=4096)(_size)
 
 __all__ = ["mx4_quantize", "mx4_dequantize", "mx4_gemm", "mx4_linear", "kv_cache", "kv_write",
            "kv_read", "kv_attention", "KV_FORMATS", "MX4_MAX_K"]
@@ -86,7 +92,7 @@ def mx4_gemm(xq, x_scale, wq, w_scale, bias=None, *, out=None, workspace=None):
     if out is not None:
         _check_out(out, torch.bfloat16, (M, N), xq.device)
     y = out if out is not None else torch.empty((M, N), dtype=torch.bfloat16, device=xq.device)
-    ws = _workspace(_size("w8a8_mx4_gemm_workspace_bytes", M, N, 32 * nb), xq.device, workspace)
+    ws = _workspace(_bytes("w8a8_mx4_gemm_workspace_bytes", M, N, 32 * nb), xq.device, workspace)
     _launch(xq.device, "w8a8_mx4_gemm", _ptr(xq), _ptr(x_scale), _ptr(wq), _ptr(w_scale),
             _ptr(bias), _ptr(y), M, N, 32 * nb, _ptr(ws), 0 if ws is None else ws.nbytes)
     return y
@@ -113,7 +119,7 @@ def mx4_linear(x, wq, w_scale, bias=None, *, act: str = "none", col_mul=None, ou
     if out is not None:
         _check_out(out, torch.bfloat16, (M, N), x.device)
     y = out if out is not None else torch.empty((M, N), dtype=torch.bfloat16, device=x.device)
-    ws = _workspace(_size("w8a8_mx4_linear_workspace_bytes", M, N, K), x.device, workspace)
+    ws = _workspace(_bytes("w8a8_mx4_linear_workspace_bytes", M, N, K), x.device, workspace)
     _launch(x.device, "w8a8_mx4_linear", _ptr(x2), a, _ptr(cm), _ptr(wq), _ptr(w_scale),
             _ptr(bias), _ptr(y), M, N, K, _ptr(ws), 0 if ws is None else ws.nbytes)
     return y if x.dim() == 2 else y.reshape(*lead, N)
@@ -139,17 +145,22 @@ def kv_cache(pages: int, heads: int, head_dim: int, page_size: int = 64, *, fmt:
     return torch.zeros((pages, 2, heads, n // (2 * heads)), dtype=torch.uint8, device=device)
 
 
-def _check_cache(cache, head_dim: int, fmt: str):
+@functools.lru_cache(maxsize=1024)
+def _cache_shape(shape, head_dim: int, fmt: str):
     """(pages, page size, heads, head_dim, format): the C ABI's description of a cache."""
     f = _format(fmt)
-    _check(cache, torch.uint8, 4, "cache")
-    pages, two, heads, n = cache.shape
+    pages, two, heads, n = shape
     token = (head_dim if f == 0 else head_dim // 2) + head_dim // 32
     page = n // token if token else 0
     if two != 2 or heads < 1 or page * token != n or _size("w8a8_kv_page_bytes", page, heads,
                                                            head_dim, f) != 2 * heads * n:
-        raise ValueError(f"cache {tuple(cache.shape)} is no {fmt} cache of heads of {head_dim}")
+        raise ValueError(f"cache {tuple(shape)} is no {fmt} cache of heads of {head_dim}")
     return pages, page, heads, head_dim, f
+
+
+def _check_cache(cache, head_dim: int, fmt: str):
+    _check(cache, torch.uint8, 4, "cache")
+    return _cache_shape(cache.shape, head_dim, fmt)
 
 
 def _check_slots(slots, T, device):
@@ -244,7 +255,7 @@ def kv_attention(q, cache, block_table, kv_lens, *, fmt: str = "fp8", q_starts=N
     if T == 0:
         return y
     group = q_heads // heads
-    nws = _size("w8a8_kv_attention_workspace_bytes", page, heads, dim, f, group, T, B,
+    nws = _bytes("w8a8_kv_attention_workspace_bytes", page, heads, dim, f, group, T, B,
                 max(1, int(max_q)), max_kv)
     ws = _workspace(nws, device, workspace)
     _launch(device, "w8a8_kv_attention", _ptr(q), q.stride(0), q.stride(1), _ptr(cache), pages,
