@@ -213,7 +213,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 for (int e = 0; e < KU / 8; ++e) {
                     const Bytes16 v =
                         *reinterpret_cast<const Bytes16 *>(src + (4 * s + g) * KU + 8 * e);
-                    q[s][e] = live ? u32x4{v.w[0], v.w[1], v.w[2], v.w[3]} : u32x4{};
+                    q[s][e] = live ? u32x4{v.w[0], v.w[1], v.w[2], v.w[3]} ^ a.q_sign : u32x4{};
                 }
         }
         f32x4 o[F];
@@ -338,13 +338,11 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float v = s[h][e] * a.scale;
                         if (part_seen)
-                            v = j0 + 16 * h + 4 * g + e < limit ? v : -INFINITY;
-                        s[h][e] = v;
-                        top = fmaxf(top, v);
+                            s[h][e] = j0 + 16 * h + 4 * g + e < limit ? s[h][e] : -INFINITY;
+                        top = fmaxf(top, s[h][e]);
                     }
-                top = fmaxf(max_of_row(top), m);
+                top = fmaxf(max_of_row(top) * a.scale, m);
                 if (__any(top > m + kSlack)) {
                     const float keep =
                         __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
@@ -361,7 +359,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[h][e] = __builtin_amdgcn_exp2f(s[h][e] - base);
+                        s[h][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][e], a.scale, -base));
                         l += s[h][e];
                     }
                 const u32x4 p = {pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]),
@@ -460,7 +458,7 @@ __device__ __forceinline__ u32x2 both_halves(float v) {
 constexpr int kTileRows = 128, kTileTokens = 64;
 
 // Many rows (128 a workgroup, 32 a wavefront): 64 tokens at a time are decoded once into LDS
-// for all four wavefronts, the next ones' codes in flight meanwhile; 32x32x16 products with the
+// for all four wavefronts, between the products of the 64 before; 32x32x16 products with the
 // rows as columns, as above. Keys lie in rows of 2 D + 16 bytes, values in rows of 2 D + 64:
 // the fragment reads (32 keys x 16 bytes; 4 values x 64 bytes) then use every bank alike.
 //
@@ -475,10 +473,12 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     constexpr int CB = FMT == KV_FP8 ? D : D / 2;
     constexpr int RSK = 2 * D + 16, RSV = 2 * D + 64;
     constexpr int KS = D / 16, F = D / 32;
-    __shared__ __attribute__((aligned(16))) uint8_t keys[TT * RSK];
-    __shared__ __attribute__((aligned(16))) uint8_t values[TT * RSV];
+    // Two stages: a tile is staged while the one before it is multiplied.
+    __shared__ __attribute__((aligned(16))) uint8_t keys[2][TT * RSK];
+    __shared__ __attribute__((aligned(16))) uint8_t values[2][TT * RSV];
     __shared__ Places places;
-    __shared__ uint8_t nan_unit[UNITS];
+    __shared__ uint8_t nan_unit[2][UNITS];
+    __shared__ int nan_any;
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -519,7 +519,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const Bytes16 v = *reinterpret_cast<const Bytes16 *>(src + 16 * s);
-                q[s] = live ? u32x4{v.w[0], v.w[1], v.w[2], v.w[3]} : u32x4{};
+                q[s] = live ? u32x4{v.w[0], v.w[1], v.w[2], v.w[3]} ^ a.q_sign : u32x4{};
             }
         }
         f32x16 o[F];
@@ -534,12 +534,14 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
             const int j_end = min(j_first + sp.chunk, some_see);
             const int ntile = (j_end - j_first + TT - 1) / TT;
             __syncthreads();
+            if (threadIdx.x == 0)
+                nan_any = 0;
             fill_places(places, c, a, sp, b, head, j_first, j_end, ntile * (TT / 16));
             __syncthreads();
 
             u32x4 kc[NU], vc[NU];
             uint32_t ks[NU], vs[NU];
-            const auto load = [&](int tile) {
+            const auto load = [&](int tile) __attribute__((always_inline)) {
 #pragma unroll
                 for (int i = 0; i < NU; ++i) {
                     const int unit = min(i * 256 + (int)threadIdx.x, UNITS - 1);
@@ -555,9 +557,33 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                     vs[i] = p[v_offset + scale];
                 }
             };
-            const auto decode = [&](uint8_t *dst, const u32x4 &codes, uint32_t byte) {
-                const float sc = scale_operand(byte);
-                u32x4 *d = reinterpret_cast<u32x4 *>(dst);
+            // Values past the end, and NaN blocks in tiles that only some rows see whole, become
+            // zeros before they are staged (a zero weight would not silence them).
+            const auto mark = [&](int j0, int st) {
+#pragma unroll
+                for (int i = 0; i < NU; ++i) {
+                    const int unit = min(i * 256 + (int)threadIdx.x, UNITS - 1);
+                    const bool past = j0 + unit / VT >= seq.kv;
+                    const bool nan = vs[i] == kNaNScale && !past;
+                    nan_unit[st][unit] = nan;
+                    if (nan)
+                        nan_any = 1;
+                    if (past || nan) {
+                        vc[i] = u32x4{};
+                        vs[i] = 0;
+                    }
+                }
+            };
+            // Unit z of 2 NU into stage st: keys, then values.
+            const auto stage = [&](auto zc, int st) __attribute__((always_inline)) {
+                constexpr int z = decltype(zc)::value, i = z % NU;
+                const int unit = i * 256 + threadIdx.x, tok = unit / VT, part = unit % VT;
+                if (UNITS % 256 != 0 && unit >= UNITS)
+                    return;
+                const u32x4 codes = z < NU ? kc[i] : vc[i];
+                const float sc = scale_operand(z < NU ? ks[i] : vs[i]);
+                u32x4 *d = reinterpret_cast<u32x4 *>(
+                    (z < NU ? keys[st] + tok * RSK : values[st] + tok * RSV) + part * VU * 2);
                 d[0] = decode_part<FMT, 0>(codes, sc);
                 d[1] = decode_part<FMT, 1>(codes, sc);
                 if constexpr (VU == 32) {
@@ -565,69 +591,68 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                     d[3] = decode_part<FMT, 3>(codes, sc);
                 }
             };
+            const auto partly_seen = [&](int j0) { return j0 + TT > all_see; };
             load(0);
+            if (partly_seen(j_first))
+                mark(j_first, 0);
+            [&]<int... z>(std::integer_sequence<int, z...>) __attribute__((always_inline)) {
+                (stage(std::integral_constant<int, z>{}, 0), ...);
+            }(std::make_integer_sequence<int, 2 * NU>{});
+            load(min(1, ntile - 1));
             for (int tile = 0; tile < ntile; ++tile) {
-                const int j0 = j_first + tile * TT;
-                const bool part_seen = j0 + TT > all_see;
-                if (tile > 0)
-                    lds_barrier();       // every wavefront has read the last tile
-                bool any_nan = false;
-#pragma unroll
-                for (int i = 0; i < NU; ++i) {
-                    const int unit = i * 256 + threadIdx.x, tok = unit / VT, part = unit % VT;
-                    if (UNITS % 256 != 0 && unit >= UNITS)
-                        break;
-                    if (part_seen) {
-                        // Values past the end, and NaN blocks where only some rows see them,
-                        // become zeros (a zero weight would not silence them).
-                        const bool past = j0 + tok >= seq.kv;
-                        const bool nan = vs[i] == kNaNScale && !past;
-                        any_nan |= nan;
-                        nan_unit[unit] = nan;
-                        if (past || nan) {
-                            vc[i] = u32x4{};
-                            vs[i] = 0;
-                        }
-                    }
-                    decode(keys + tok * RSK + part * VU * 2, kc[i], ks[i]);
-                    decode(values + tok * RSV + part * VU * 2, vc[i], vs[i]);
-                }
-                if (tile + 1 < ntile)
-                    load(tile + 1);
-                if (part_seen) {
-                    if (__syncthreads_or(any_nan))     // rare: who sees the NaN blocks
-                        for (int unit = 0; unit < UNITS; ++unit)
-                            if (nan_unit[unit] && j0 + unit / VT < limit)
-                                row_nan |= 1u << (unit % VT * VU / 32);
-                } else {
-                    lds_barrier();
-                }
+                const int j0 = j_first + tile * TT, st = tile & 1;
+                const bool part_seen = partly_seen(j0);
+                lds_barrier();       // this tile is staged, the other stage's last one is read
+                if (partly_seen(j0 + TT) && tile + 1 < ntile)
+                    mark(j0 + TT, st ^ 1);
+                if (part_seen && nan_any)      // rare: which rows see a NaN block
+                    for (int unit = 0; unit < UNITS; ++unit)
+                        if (nan_unit[st][unit] && j0 + unit / VT < limit)
+                            row_nan |= 1u << (unit % VT * VU / 32);
+                // Scores: token 32 t + 8 (i / 4) + 4 h + i % 4 in s[t][i]. Between the products
+                // the next tile is staged (after the last tile: itself again, unread).
+                f32x16 s[2] = {f32x16{}, f32x16{}};
+                const uint8_t *kp = keys[st] + r32 * RSK + h * 16;
+                bf16x8 fk[2][2];
+                const auto read_keys = [&](int k) __attribute__((always_inline)) {
+                    fk[k & 1][0] = *reinterpret_cast<const bf16x8 *>(kp + k * 32);
+                    fk[k & 1][1] = *reinterpret_cast<const bf16x8 *>(kp + 32 * RSK + k * 32);
+                };
+                read_keys(0);
+                [&]<int... k>(std::integer_sequence<int, k...>) __attribute__((always_inline)) {
+                    ([&]() __attribute__((always_inline)) {
+                        if constexpr (k + 1 < KS)
+                            read_keys(k + 1);
+                        constexpr int z0 = k * 2 * NU / KS, z1 = (k + 1) * 2 * NU / KS;
+                        if constexpr (z0 < z1)
+                            stage(std::integral_constant<int, z0>{}, st ^ 1);
+                        if constexpr (z0 + 1 < z1)
+                            stage(std::integral_constant<int, z0 + 1>{}, st ^ 1);
+                        static_assert(z1 - z0 <= 2, "units of a step");
+                        __builtin_amdgcn_sched_barrier(0);
+                        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            fk[k & 1][0], __builtin_bit_cast(bf16x8, q[k]), s[0], 0, 0, 0);
+                        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            fk[k & 1][1], __builtin_bit_cast(bf16x8, q[k]), s[1], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }(), ...);
+                }(std::make_integer_sequence<int, KS>{});
+                load(min(tile + 2, ntile - 1));
                 if (j0 >= wave_sees)
                     continue;
 
-                // Scores: token 32 t + 8 (i / 4) + 4 h + i % 4 in s[t][i].
-                f32x16 s[2] = {f32x16{}, f32x16{}};
-                const uint8_t *kp = keys + r32 * RSK + h * 16;
-#pragma unroll
-                for (int k = 0; k < KS; ++k)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            *reinterpret_cast<const bf16x8 *>(kp + t * 32 * RSK + k * 32),
-                            __builtin_bit_cast(bf16x8, q[k]), s[t], 0, 0, 0);
                 float top = -INFINITY;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        float v = s[t][i] * a.scale;
                         if (part_seen)
-                            v = j0 + 32 * t + 8 * (i / 4) + 4 * h + i % 4 < limit ? v : -INFINITY;
-                        s[t][i] = v;
-                        top = fmaxf(top, v);
+                            s[t][i] = j0 + 32 * t + 8 * (i / 4) + 4 * h + i % 4 < limit ? s[t][i]
+                                                                                       : -INFINITY;
+                        top = fmaxf(top, s[t][i]);
                     }
                 const u32x2 tops = both_halves(top);
-                top = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])), m);
+                top = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])) * a.scale, m);
                 if (__any(top > m + kSlack)) {
                     const float keep =
                         __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
@@ -640,33 +665,54 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                     m = top;
                 }
                 const float base = m == -INFINITY ? 0.0f : m;
-                u32x4 p[4];
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float x = __builtin_amdgcn_exp2f(s[t][i] - base);
-                        const float y = __builtin_amdgcn_exp2f(s[t][i + 1] - base);
-                        l += x + y;
-                        p[2 * t + i / 8][i % 8 / 2] = pack_bf16(x, y);
-                    }
-                // Step u of 16 tokens: half h takes tokens 4h + 0 .. 3 and 8 + 4h + 0 .. 3.
+                // Values: step u of 16 tokens, half h takes tokens 4h + 0 .. 3 and 8 + 4h +
+                // 0 .. 3. The weights of step u + 1 are computed between the products of step u.
                 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-                const uint8_t *vp = values + (4 * h + ((lane & 15) >> 2)) * RSV +
+                const uint8_t *vp = values[st] + (4 * h + ((lane & 15) >> 2)) * RSV +
                                     ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int f = 0; f < F; ++f) {
-                        const uint8_t *src = vp + 16 * u * RSV + f * 64;
-                        const u32x2 x = __builtin_bit_cast(
-                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)src));
-                        const u32x2 y = __builtin_bit_cast(
-                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(src + 8 * RSV)));
+                u32x2 fv[2][2];
+                const auto read_values = [&](int z) __attribute__((always_inline)) {
+                    const uint8_t *src = vp + 16 * (z / F) * RSV + z % F * 64;
+                    fv[z & 1][0] = __builtin_bit_cast(
+                        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)src));
+                    fv[z & 1][1] = __builtin_bit_cast(
+                        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(src + 8 * RSV)));
+                };
+                u32x4 p[4];
+                const auto weight = [&](auto qc) __attribute__((always_inline)) {
+                    constexpr int w = decltype(qc)::value;     // of 16 pairs
+                    const float x = __builtin_amdgcn_exp2f(
+                        __builtin_fmaf(s[w / 8][w % 8 * 2], a.scale, -base));
+                    const float y = __builtin_amdgcn_exp2f(
+                        __builtin_fmaf(s[w / 8][w % 8 * 2 + 1], a.scale, -base));
+                    l += x + y;
+                    p[w / 4][w % 4] = pack_bf16(x, y);
+                };
+                weight(std::integral_constant<int, 0>{});
+                weight(std::integral_constant<int, 1>{});
+                weight(std::integral_constant<int, 2>{});
+                weight(std::integral_constant<int, 3>{});
+                read_values(0);
+                [&]<int... z>(std::integer_sequence<int, z...>) __attribute__((always_inline)) {
+                    ([&]() __attribute__((always_inline)) {
+                        constexpr int u = z / F, f = z % F;
+                        if constexpr (z + 1 < 4 * F)
+                            read_values(z + 1);
+                        if constexpr (u < 3) {
+                            constexpr int w0 = 4 * (u + 1) + f * 4 / F, w1 = 4 * (u + 1) + (f + 1) * 4 / F;
+                            if constexpr (w0 < w1)
+                                weight(std::integral_constant<int, w0>{});
+                            if constexpr (w0 + 1 < w1)
+                                weight(std::integral_constant<int, w0 + 1>{});
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
                         o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]}),
+                            __builtin_bit_cast(bf16x8, u32x4{fv[z & 1][0][0], fv[z & 1][0][1],
+                                                             fv[z & 1][1][0], fv[z & 1][1][1]}),
                             __builtin_bit_cast(bf16x8, p[u]), o[f], 0, 0, 0);
-                    }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }(), ...);
+                }(std::make_integer_sequence<int, 4 * F>{});
             }
         }
 

@@ -247,7 +247,12 @@ w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head
     a.causal = causal;
     a.max_q = max_q > 1 ? max_q : 1;
     a.max_kv = max_kv;
-    a.scale = scale * 1.44269504088896341f;
+    // The kernels scale a maximum instead of every score, and mask with minus infinity: a
+    // positive factor. A zero becomes so small a one that all weights are 1.
+    a.q_sign = scale < 0.0f ? 0x80008000u : 0u;
+    a.scale = __builtin_fabsf(scale) * 1.44269504088896341f;
+    if (a.scale < 0x1p-126f)
+        a.scale = 0x1p-126f;
     const size_t need = kv_attention_workspace_bytes(c, T, seqs, group, a.max_q, max_kv);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
         return W8A8_ERR_WORKSPACE;

@@ -227,6 +227,14 @@ def test_nan_tokens_reach_only_the_queries_that_see_them(fmt, qs, kvs, nan_at):
                 assert (np.abs(y[:first, h] - want) <= mag * 2.0 ** -7).all()
 
 
+def test_scales():
+    """Negative, zero and large scales, in both kernels."""
+    for qs, kvs in (([1, 2], [300, 40]), ([60], [130])):
+        c = Case("fp8", 128, 1, 2, 16, qs, kvs, seed=13)
+        for scale in (-0.2, 0.0, 1e-6, 3.0):
+            c.check(c.run(scale=scale), scale=scale)
+
+
 def test_extreme_scores():
     """Rows whose scores differ by hundreds: one key takes all the weight, sums stay finite."""
     c = Case("fp8", 128, 1, 1, 16, [1, 1], [100, 37], seed=9)
