@@ -99,6 +99,9 @@ __device__ __forceinline__ float sum_of_row(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// In a branch that few tiles take: without it the compiler computes both sides in every tile.
+__device__ __forceinline__ void keep_branch() { asm volatile(""); }
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
 }
@@ -299,6 +302,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 for (int i = 0; i < NV; ++i) {
                     const int unit = i * 64 + lane, tok = unit / VT, part = unit % VT;
                     if (part_seen) {
+                        keep_branch();
                         const bool past = j0 + tok >= seq.kv;
                         const bool nan = vs[i] == kNaNScale && !past;
                         any_nan |= nan;
@@ -333,17 +337,24 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 if (tile + 4 < ntile)
                     load(tile + 4);
 
+                if (part_seen) {
+                    const int left = limit - j0 - 4 * g;
+                    keep_branch();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[h][e] = 16 * h + e < left ? s[h][e] : -INFINITY;
+                }
                 float top = -INFINITY;
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (part_seen)
-                            s[h][e] = j0 + 16 * h + 4 * g + e < limit ? s[h][e] : -INFINITY;
+                    for (int e = 0; e < 4; ++e)
                         top = fmaxf(top, s[h][e]);
-                    }
                 top = fmaxf(max_of_row(top) * a.scale, m);
                 if (__any(top > m + kSlack)) {
+                    keep_branch();
                     const float keep =
                         __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
                     l *= keep;
@@ -641,19 +652,25 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                 if (j0 >= wave_sees)
                     continue;
 
+                if (part_seen) {
+                    const int left = limit - j0 - 4 * h;
+                    keep_branch();
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            s[t][i] = 32 * t + 8 * (i / 4) + i % 4 < left ? s[t][i] : -INFINITY;
+                }
                 float top = -INFINITY;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (part_seen)
-                            s[t][i] = j0 + 32 * t + 8 * (i / 4) + 4 * h + i % 4 < limit ? s[t][i]
-                                                                                       : -INFINITY;
+                    for (int i = 0; i < 16; ++i)
                         top = fmaxf(top, s[t][i]);
-                    }
                 const u32x2 tops = both_halves(top);
                 top = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])) * a.scale, m);
                 if (__any(top > m + kSlack)) {
+                    keep_branch();
                     const float keep =
                         __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
                     l *= keep;
