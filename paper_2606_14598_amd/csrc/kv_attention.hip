@@ -473,8 +473,12 @@ constexpr int kTileRows = 128, kTileTokens = 64;
 // rows as columns, as above. Keys lie in rows of 2 D + 16 bytes, values in rows of 2 D + 64:
 // the fragment reads (32 keys x 16 bytes; 4 values x 64 bytes) then use every bank alike.
 //
-// Workgroup -> problem: every 8th workgroup goes to one XCD; a key/value head of a sequence is
-// given to one XCD with all its row tiles, the last ones (which see the most keys) first.
+// Workgroup -> problem: every 8th workgroup goes to one XCD; a split of a key/value head of a
+// sequence is given to one XCD with all its row tiles, the last ones (which see the most keys)
+// first, so that its L2 holds the keys. Fewer than kSpreadUnits of them would leave XCDs idle:
+// their row tiles go to all XCDs.
+constexpr int kSpreadUnits = 32;
+
 template <int FMT, int D>
 __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1)
 kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
@@ -494,17 +498,26 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r32 = lane & 31, h = lane >> 5;
-    const int slot = blockIdx.x >> 3, per = tiles * sp.splits;
-    const int pair = __builtin_amdgcn_readfirstlane(slot / per) * 8 + (blockIdx.x & 7);
-    if (pair >= a.seqs * c.heads)
-        return;
-    const int in = slot % per, split = __builtin_amdgcn_readfirstlane(in % sp.splits);
+    const int pairs = a.seqs * c.heads, units = pairs * sp.splits;
+    int unit, in;                          // head of a sequence and split; row tile from the end
+    if (units >= kSpreadUnits) {
+        const int slot = blockIdx.x >> 3;
+        unit = __builtin_amdgcn_readfirstlane(slot / tiles);
+        in = slot - unit * tiles;
+        unit = unit * 8 + (blockIdx.x & 7);
+        if (unit >= units)
+            return;
+    } else {
+        unit = __builtin_amdgcn_readfirstlane(blockIdx.x / tiles);
+        in = blockIdx.x - unit * tiles;
+    }
+    const int split = __builtin_amdgcn_readfirstlane(unit / pairs), pair = unit - split * pairs;
     const int b = __builtin_amdgcn_readfirstlane(pair / c.heads), head = pair - b * c.heads;
     const Seq seq = sequence(c, a, b);
     const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
     const int64_t v_offset = c.heads * c.head_bytes();
 
-    const int first_rt = __builtin_amdgcn_readfirstlane(tiles - 1 - in / sp.splits);
+    const int first_rt = tiles - 1 - in;
     const int last_rt = (rows + kTileRows - 1) / kTileRows - 1;
     // Row tiles first_rt, first_rt + tiles, ...: more than one only where max_q was too small.
     for (int rt = first_rt; rt <= last_rt; rt += tiles) {
@@ -851,20 +864,25 @@ bool many_rows(int group, int max_q) { return (int64_t)max_q * group >= kManyRow
 
 // How many ways the keys are divided. A partial result is 4 (dim + 4) bytes a row to write and
 // to read, and a workgroup takes some microseconds to start, so only as many as fill the card.
-Split split_of(const KvShape &c, int seqs, int group, int max_q, int max_kv) {
+Split split_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
     const bool many = many_rows(group, max_q);
     const int tile_rows = many ? kTileRows : kSplitRows;
-    const int64_t tiles = ((int64_t)max_q * group + tile_rows - 1) / tile_rows;
-    const int64_t blocks = (int64_t)seqs * c.heads * tiles;
+    // Row tiles: of max_q queries each, and no more than T queries in all make.
+    const int64_t tiles = std::min(seqs * (((int64_t)max_q * group + tile_rows - 1) / tile_rows),
+                                   T * group / tile_rows + seqs);
+    const int64_t blocks = c.heads * tiles;
     // Few rows: two workgroups a CU for one sequence (8 heads, 200000 tokens of 4 bits: 48 us,
     // with four a CU 53), eight where several may differ in length, as max_kv bounds them all;
     // of 512 tokens at least, of 2048 where the heads alone fill the card twice over (64 x 8
-    // heads of 2000 tokens: 52 us, in four parts 60). Many rows: 512 workgroups of 1024 tokens.
-    const int64_t want = many || seqs == 1 ? 512 : 2048;
-    const int64_t least = many ? 1024 : blocks >= 512 ? 2048 : 512;
-    int64_t splits = std::min((want + blocks - 1) / blocks, (max_kv + least - 1) / least);
-    if (many && blocks >= 256)
-        splits = 1;
+    // heads of 2000 tokens: 52 us, in four parts 60). Many rows, whose partial results are large:
+    // only while they leave a third of the CUs idle (2 heads, 2 x 700 queries on 20000 keys of
+    // 256: 770 us, in five parts 393; 18 heads, 1000 on 6000: 241, in two parts 257).
+    int64_t splits;
+    if (many)
+        splits = std::min<int64_t>(400 / blocks, (max_kv + 1023) / 1024);
+    else
+        splits = std::min<int64_t>(((seqs == 1 ? 512 : 2048) + blocks - 1) / blocks,
+                                   (max_kv + (blocks >= 512 ? 2047 : 511)) / (blocks >= 512 ? 2048 : 512));
     Split sp;
     sp.splits = (int)std::max<int64_t>(splits, 1);
     const int64_t chunk = ((max_kv + sp.splits - 1) / sp.splits + 127) / 128 * 128;
@@ -879,19 +897,20 @@ Split split_of(const KvShape &c, int seqs, int group, int max_q, int max_kv) {
 
 size_t kv_attention_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_q,
                                     int max_kv) {
-    const Split sp = split_of(c, seqs, group, max_q, max_kv);
+    const Split sp = split_of(c, T, seqs, group, max_q, max_kv);
     return sp.splits == 1 ? 0 : (size_t)sp.splits * T * c.heads * group * (c.dim + 4) * 4;
 }
 
 hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
-    Split sp = split_of(c, a.seqs, a.group, a.max_q, a.max_kv);
+    Split sp = split_of(c, a.T, a.seqs, a.group, a.max_q, a.max_kv);
     sp.part = static_cast<float *>(ws);
     const bool many = many_rows(a.group, a.max_q);
     const int tile_rows = many ? kTileRows : kSplitRows;
     const int64_t pairs = (int64_t)c.heads * a.seqs, rows = a.T * c.heads * a.group;
     const int64_t tiles =
         std::min<int64_t>(((int64_t)a.max_q * a.group + tile_rows - 1) / tile_rows, 65535);
-    const int64_t blocks = many ? (pairs + 7) / 8 * 8 * tiles * sp.splits : pairs * sp.splits;
+    const int64_t units = pairs * sp.splits;
+    const int64_t blocks = many ? (units >= kSpreadUnits ? (units + 7) / 8 * 8 : units) * tiles : units;
     if (blocks > 0x7FFFFFFF || rows > 0x7FFFFFFF)
         return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks, many ? 1u : (unsigned)tiles);
