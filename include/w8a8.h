@@ -363,7 +363,7 @@ w8a8_status w8a8_kv_read(const uint8_t *cache, int64_t pages, int page, int head
  *   out [T, heads * group, dim] = sum_j p_j v_j / sum_j p_j, p_j = exp(scale * q.k_j - max),
  * and zeros where a query sees no token. What lies in the cache past kv_lens[b], or is hidden
  * from a query, has no effect on it, NaN included. Scores and sums are float32; the weights
- * p_j are rounded to bf16 for the matrix cores.
+ * p_j are rounded to one or two bf16 terms for the matrix cores.
  * max_q and max_kv are bounds on a sequence's queries and tokens that the launch is laid out
  * for; with other values the results are the same (table_pages * page bounds the tokens; it is
  * at most W8A8_KV_MAX_TOKENS, else W8A8_ERR_SHAPE).

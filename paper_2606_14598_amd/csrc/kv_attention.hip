@@ -12,8 +12,8 @@
 // holds one row, so maxima, sums and the rescaling of O stay inside a lane but for one
 // exchange of the maximum between the lanes that share a row, and the weights P^T come out of
 // S^T in the layout the second product takes them in. Codes decode to bf16 exactly; the
-// weights are rounded to bf16 for the second product (2^-9 of each weight; their sum is taken
-// before).
+// weights are rounded for the second product, to one bf16 term (2^-8 of each at most) where
+// there are many rows and products bind, to two (2^-16) where there are few.
 #include "../../include/w8a8.h"
 #include "mx_internal.hpp"
 #include "mx_math.hpp"
@@ -90,13 +90,9 @@ __device__ __forceinline__ float max_of_row(float v) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-__device__ __forceinline__ float sum_of_row(float v) {
-    u32x2 r = __builtin_bit_cast(
-        u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
-    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_bit_cast(
-        u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+// An operand of ones: products with it sum the weights on the matrix cores.
+__device__ __forceinline__ bf16x8 ones() {
+    return __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
 }
 
 // In a branch that few tiles take: without it the compiler computes both sides in every tile.
@@ -223,7 +219,8 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x4{};
-        float m = -INFINITY, l = 0.0f;
+        float m = -INFINITY;
+        f32x4 sums = {};           // in each element: the sum of a row's weights
         uint32_t row_nan = 0;      // blocks of the row's output that a seen NaN value reaches
 
         for (int ch = split; ch < nch; ch += sp.splits) {
@@ -357,7 +354,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                     keep_branch();
                     const float keep =
                         __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
-                    l *= keep;
+                    sums[0] *= keep;           // the only one that is used
 #pragma unroll
                     for (int f = 0; f < F; ++f)
 #pragma unroll
@@ -369,12 +366,21 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                    for (int e = 0; e < 4; ++e)
                         s[h][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][e], a.scale, -base));
-                        l += s[h][e];
-                    }
-                const u32x4 p = {pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]),
-                                 pack_bf16(s[1][0], s[1][1]), pack_bf16(s[1][2], s[1][3])};
+                // The weights in two bf16 terms, 16 bits in all: the products are few here.
+                u32x4 p, p2;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = s[i / 2][i % 2 * 2], y = s[i / 2][i % 2 * 2 + 1];
+                    p[i] = pack_bf16(x, y);
+                    p2[i] = pack_bf16(x - __uint_as_float(p[i] << 16),
+                                      y - __uint_as_float(p[i] & 0xFFFF0000u));
+                }
+                sums = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    ones(), __builtin_bit_cast(bf16x8, p), sums, 0, 0, 0);
+                sums = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    ones(), __builtin_bit_cast(bf16x8, p2), sums, 0, 0, 0);
 #pragma unroll
                 for (int f = 0; f < F; ++f) {
                     typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
@@ -383,15 +389,17 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                     const i16x4 hi =
                         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(src + 16 * RS));
                     const u32x2 x = __builtin_bit_cast(u32x2, lo), y = __builtin_bit_cast(u32x2, hi);
-                    o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]}),
-                        __builtin_bit_cast(bf16x8, p), o[f], 0, 0, 0);
+                    const bf16x8 v = __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
+                    o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, p), o[f],
+                                                                   0, 0, 0);
+                    o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, p2), o[f],
+                                                                   0, 0, 0);
                 }
             }
         }
 
         // Join the four wavefronts: row r16, outputs 16 f + 4 g + e.
-        l = sum_of_row(l);
+        const float l = sums[0];
         if (g == 0) {
             row_m[wave][r16] = m;
             row_l[wave][r16] = l;
@@ -879,7 +887,7 @@ Split split_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int 
     // 256: 770 us, in five parts 393; 18 heads, 1000 on 6000: 241, in two parts 257).
     int64_t splits;
     if (many)
-        splits = std::min<int64_t>(400 / blocks, (max_kv + 1023) / 1024);
+        splits = std::min<int64_t>(384 / blocks, (max_kv + 1023) / 1024);
     else
         splits = std::min<int64_t>(((seqs == 1 ? 512 : 2048) + blocks - 1) / blocks,
                                    (max_kv + (blocks >= 512 ? 2047 : 511)) / (blocks >= 512 ? 2048 : 512));

@@ -138,8 +138,8 @@ class Case:
                                  self.kv_lens, fmt=self.fmt, **kw)
 
     def check(self, y, scale=None, causal=True):
-        """Within the rounding of the weights and of the output to bf16 (2^-9 of the weighted
-        mean of |v| each) and float32 sums: 2^-7 of that mean."""
+        """Within the rounding of the weights and of the output to bf16 (2^-8 of the weighted
+        mean of |v| each): 2^-7 of that mean."""
         scale = self.dim ** -0.5 if scale is None else scale
         y, q = f64(y), f64(self.q)
         assert np.isfinite(y).all()
