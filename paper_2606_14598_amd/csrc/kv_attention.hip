@@ -573,21 +573,24 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 
             u32x4 kc[NU], vc[NU];
             uint32_t ks[NU], vs[NU];
-            const auto load = [&](int tile) __attribute__((always_inline)) {
-#pragma unroll
-                for (int i = 0; i < NU; ++i) {
-                    const int unit = min(i * 256 + (int)threadIdx.x, UNITS - 1);
-                    const int tok = unit / VT, part = unit % VT;
-                    const int blk = tile * (TT / 16) + tok / 16;
-                    const int at = places.at[blk] + tok % 16;
-                    const uint8_t *p = a.cache + places.page[blk];
-                    const uint32_t code = at * CB + part * 16;
-                    const uint32_t scale = c.page * CB + at * (D / 32) + part * VU / 32;
-                    kc[i] = Unit<16>::load(p + code);
-                    ks[i] = p[scale];
-                    vc[i] = Unit<16>::load(p + v_offset + code);
-                    vs[i] = p[v_offset + scale];
-                }
+            const auto load = [&](auto ic, int tile) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                const int unit = min(i * 256 + (int)threadIdx.x, UNITS - 1);
+                const int tok = unit / VT, part = unit % VT;
+                const int blk = tile * (TT / 16) + tok / 16;
+                const int at = places.at[blk] + tok % 16;
+                const uint8_t *p = a.cache + places.page[blk];
+                const uint32_t code = at * CB + part * 16;
+                const uint32_t scale = c.page * CB + at * (D / 32) + part * VU / 32;
+                kc[i] = Unit<16>::load(p + code);
+                ks[i] = p[scale];
+                vc[i] = Unit<16>::load(p + v_offset + code);
+                vs[i] = p[v_offset + scale];
+            };
+            const auto load_all = [&](int tile) {
+                [&]<int... i>(std::integer_sequence<int, i...>) __attribute__((always_inline)) {
+                    (load(std::integral_constant<int, i>{}, tile), ...);
+                }(std::make_integer_sequence<int, NU>{});
             };
             // Values past the end, and NaN blocks in tiles that only some rows see whole, become
             // zeros before they are staged (a zero weight would not silence them).
@@ -606,9 +609,9 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                     }
                 }
             };
-            // Unit z of 2 NU into stage st: keys, then values.
+            // Half z of 4 NU half units into stage st: keys, then values.
             const auto stage = [&](auto zc, int st) __attribute__((always_inline)) {
-                constexpr int z = decltype(zc)::value, i = z % NU;
+                constexpr int z = decltype(zc)::value / 2, half = decltype(zc)::value % 2, i = z % NU;
                 const int unit = i * 256 + threadIdx.x, tok = unit / VT, part = unit % VT;
                 if (UNITS % 256 != 0 && unit >= UNITS)
                     return;
@@ -616,21 +619,21 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                 const float sc = scale_operand(z < NU ? ks[i] : vs[i]);
                 u32x4 *d = reinterpret_cast<u32x4 *>(
                     (z < NU ? keys[st] + tok * RSK : values[st] + tok * RSV) + part * VU * 2);
-                d[0] = decode_part<FMT, 0>(codes, sc);
-                d[1] = decode_part<FMT, 1>(codes, sc);
-                if constexpr (VU == 32) {
-                    d[2] = decode_part<FMT, 2>(codes, sc);
-                    d[3] = decode_part<FMT, 3>(codes, sc);
+                if constexpr (VU == 16) {
+                    d[half] = decode_part<FMT, half>(codes, sc);
+                } else {
+                    d[2 * half] = decode_part<FMT, 2 * half>(codes, sc);
+                    d[2 * half + 1] = decode_part<FMT, 2 * half + 1>(codes, sc);
                 }
             };
             const auto partly_seen = [&](int j0) { return j0 + TT > all_see; };
-            load(0);
+            load_all(0);
             if (partly_seen(j_first))
                 mark(j_first, 0);
             [&]<int... z>(std::integer_sequence<int, z...>) __attribute__((always_inline)) {
                 (stage(std::integral_constant<int, z>{}, 0), ...);
-            }(std::make_integer_sequence<int, 2 * NU>{});
-            load(min(1, ntile - 1));
+            }(std::make_integer_sequence<int, 4 * NU>{});
+            load_all(min(1, ntile - 1));
             for (int tile = 0; tile < ntile; ++tile) {
                 const int j0 = j_first + tile * TT, st = tile & 1;
                 const bool part_seen = partly_seen(j0);
@@ -655,12 +658,10 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                     ([&]() __attribute__((always_inline)) {
                         if constexpr (k + 1 < KS)
                             read_keys(k + 1);
-                        constexpr int z0 = k * 2 * NU / KS, z1 = (k + 1) * 2 * NU / KS;
+                        constexpr int z0 = k * 4 * NU / KS, z1 = (k + 1) * 4 * NU / KS;
                         if constexpr (z0 < z1)
                             stage(std::integral_constant<int, z0>{}, st ^ 1);
-                        if constexpr (z0 + 1 < z1)
-                            stage(std::integral_constant<int, z0 + 1>{}, st ^ 1);
-                        static_assert(z1 - z0 <= 2, "units of a step");
+                        static_assert(z1 - z0 <= 1, "half units of a step");
                         __builtin_amdgcn_sched_barrier(0);
                         s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                             fk[k & 1][0], __builtin_bit_cast(bf16x8, q[k]), s[0], 0, 0, 0);
@@ -669,9 +670,11 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                         __builtin_amdgcn_sched_barrier(0);
                     }(), ...);
                 }(std::make_integer_sequence<int, KS>{});
-                load(min(tile + 2, ntile - 1));
-                if (j0 >= wave_sees)
+                // The next loads go out between the products with the values.
+                if (j0 >= wave_sees) {
+                    load_all(min(tile + 2, ntile - 1));
                     continue;
+                }
 
                 if (part_seen) {
                     const int left = limit - j0 - 4 * h;
@@ -743,6 +746,9 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                             if constexpr (w0 + 1 < w1)
                                 weight(std::integral_constant<int, w0 + 1>{});
                         }
+                        if constexpr (z < 2 * NU && z % 2 == 1)
+                            load(std::integral_constant<int, z / 2>{}, min(tile + 2, ntile - 1));
+                        static_assert(2 * NU <= 4 * F, "loads between the products");
                         __builtin_amdgcn_sched_barrier(0);
                         o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                             __builtin_bit_cast(bf16x8, u32x4{fv[z & 1][0][0], fv[z & 1][0][1],
