@@ -7,6 +7,11 @@
 // 256 channels (8 blocks, 128 bytes of codes a row) K-half h takes blocks 4h .. 4h + 3 in
 // steps 0 .. 3: the four scale bytes of a lane are then one word of the scales' layout, and
 // each step selects its byte of that word.
+//
+// Many tokens: bound by the matrix cores at the clock that their power leaves (1.6 GHz on
+// random codes, 6.4 PFLOP/s from registers; 2.3 GHz and 9.1 on zeros) and by waits for panels.
+// 4608 x 4096 x 16384 runs at 3.8 PFLOP/s, 4608 x 16384 x 4096 in one round of tiles at 4.5. Few
+// tokens: bound by reading W; 1 x 4096 x 16384 takes 9.8 us (3.7 TB/s) with its quantizer.
 #include "mx_internal.hpp"
 #include "mx_quant.hpp"
 
@@ -74,6 +79,11 @@ __device__ __forceinline__ void tile_of(int bid, const Mx4Params &p, int &tm, in
 // codes of TN weight rows and TM token rows, then their scale words (8 bytes a row). Codes
 // and scales go from memory to LDS directly; what lies past a matrix reads as zero codes and
 // zero scales. Panel k + S - 1 is requested while panel k is multiplied.
+//
+// Eight to twelve wavefronts on the large tiles: a product's operands are two LDS reads, and
+// with one wavefront a SIMD their latencies show (256 x 256 by 4 wavefronts 183 us at 4608 x
+// 4096 x 16384, by 8 159). Fragments of half panels read a step ahead across four stages, for
+// four wavefronts, were slower yet (214), as were two workgroups a CU (128 x 128 tiles, 180).
 template <int TM, int TN, int WM, int WN, int S>
 __global__ void __launch_bounds__(WM *WN * 64)
 mx4_gemm_kernel(Mx4Params p) {
@@ -371,7 +381,7 @@ mx4_reduce_kernel(Mx4Params p) {
     }
 }
 
-// Few tokens (up to 16): bound by reading W once, so nothing of it is staged. A workgroup owns
+// Few tokens (16 FMB): bound by reading W once, so nothing of it is staged. A workgroup owns
 // 16 FNB channels; its NW wavefronts take K in turn, 512 channels (256 bytes, 16 blocks) at a
 // time, with the next 512 channels' loads in flight. v_mfma_scale_f32_16x16x128: lane (r, g) =
 // (lane % 16, lane / 16) holds row r; in step s of four it takes block 4s + g, so that a load
@@ -383,11 +393,12 @@ mx4_reduce_kernel(Mx4Params p) {
 // Every workgroup quantizes them again, so the host allows it for few tokens x channels only.
 // LDS rows are an odd number of 16-byte blocks apart: the 16 rows of a read then lie in
 // different banks.
-template <int FNB, int NW, bool QX, int ACT, bool CM>
+template <int FMB, int FNB, int NW, bool QX, int ACT, bool CM>
 __global__ void __launch_bounds__(NW * 64)
 mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul) {
     using namespace mx;
-    __shared__ f32x4 red[NW][FNB][64];
+    static_assert(!QX || FMB == 1);
+    __shared__ f32x4 red[NW][FNB * FMB][64];
     extern __shared__ __attribute__((aligned(16))) uint8_t tokens[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -403,15 +414,16 @@ mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul)
         wrow[c] = a.wq + n * nb * 16;
         wscale[c] = a.ws + n * 8;
     }
-    const int m = min(r, M - 1);
-    f32x4 acc[FNB];
+    f32x4 acc[FNB][FMB];
 #pragma unroll
     for (int c = 0; c < FNB; ++c)
-        acc[c] = f32x4{};
+#pragma unroll
+        for (int f = 0; f < FMB; ++f)
+            acc[c][f] = f32x4{};
 
-    i32x4 w[FNB][4], fx[4];
-    uint2 sw[FNB][2];
-    int sx[4];
+    i32x4 w[FNB][4], fx[FMB][4];
+    uint2 sw[FNB][2], sx[FMB][2];
+    int token_scale[4];
     const auto load = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < FNB; ++c) {
@@ -429,10 +441,18 @@ mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul)
         }
         if constexpr (!QX) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int blk = min(16 * j + 4 * s + g, nb - 1);   // against zero weights past nb
-                fx[s] = *reinterpret_cast<const i32x4 *>(a.xq + ((int64_t)m * nb + blk) * 16);
-                sx[s] = a.xs[((int64_t)(blk >> 3) * M + m) * 8 + (blk & 7)];
+            for (int f = 0; f < FMB; ++f) {
+                const int m = min(f * 16 + r, M - 1);
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int blk = min(16 * j + 4 * s + g, nb - 1);   // against zero weights past nb
+                    fx[f][s] = *reinterpret_cast<const i32x4 *>(a.xq + ((int64_t)m * nb + blk) * 16);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    sx[f][h] = 2 * j + h < panels ? *reinterpret_cast<const uint2 *>(
+                                                        a.xs + ((int64_t)(2 * j + h) * M + m) * 8)
+                                                  : make_uint2(0, 0);
             }
         }
     };
@@ -465,23 +485,27 @@ mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul)
     }
     for (int j = wave; j < steps; j += NW) {
         if constexpr (QX) {
+            const int m = min(r, M - 1);
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const int blk = min(16 * j + 4 * s + g, nb - 1);
-                fx[s] = *reinterpret_cast<const i32x4 *>(tokens + m * stride + blk * 16);
-                sx[s] = token_scales[m * nb + blk];
+                fx[0][s] = *reinterpret_cast<const i32x4 *>(tokens + m * stride + blk * 16);
+                token_scale[s] = token_scales[m * nb + blk];
             }
         }
-        i32x4 wc[FNB][4], xc[4];
-        uint32_t sc[FNB][4], xsc[4];
+        i32x4 wc[FNB][4], xc[FMB][4];
+        int sc[FNB][4], xsc[FMB][4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            xc[s] = fx[s];
-            xsc[s] = sx[s];
+#pragma unroll
+            for (int f = 0; f < FMB; ++f) {
+                xc[f][s] = fx[f][s];
+                xsc[f][s] = QX ? token_scale[s] : (int)((s & 1 ? sx[f][s / 2].y : sx[f][s / 2].x) >> (8 * g));
+            }
 #pragma unroll
             for (int c = 0; c < FNB; ++c) {
                 wc[c][s] = w[c][s];
-                sc[c][s] = (s & 1 ? sw[c][s / 2].y : sw[c][s / 2].x) >> (8 * g);
+                sc[c][s] = (int)((s & 1 ? sw[c][s / 2].y : sw[c][s / 2].x) >> (8 * g));
             }
         }
         if (j + NW < steps)
@@ -489,21 +513,25 @@ mx4_stream_kernel(Mx4Args a, const uint16_t *x, int64_t K, const float *col_mul)
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
-            for (int c = 0; c < FNB; ++c)
-                acc[c] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                    frag(wc[c][s]), frag(xc[s]), acc[c], 4, 4, 0, (int)sc[c][s], 0, (int)xsc[s]);
+            for (int f = 0; f < FMB; ++f)
+#pragma unroll
+                for (int c = 0; c < FNB; ++c)
+                    acc[c][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        frag(wc[c][s]), frag(xc[f][s]), acc[c][f], 4, 4, 0, sc[c][s], 0, xsc[f][s]);
     }
 #pragma unroll
     for (int c = 0; c < FNB; ++c)
-        red[wave][c][lane] = acc[c];
+#pragma unroll
+        for (int f = 0; f < FMB; ++f)
+            red[wave][f * FNB + c][lane] = acc[c][f];
     __syncthreads();
     // Lane (r, g) of a fragment holds token r, channels 4g .. 4g + 3.
-    for (int i = threadIdx.x; i < FNB * 64; i += NW * 64) {
-        const int l = i & 63, c = i >> 6, t = l & 15;
-        f32x4 v = red[0][c][l];
+    for (int i = threadIdx.x; i < FNB * FMB * 64; i += NW * 64) {
+        const int l = i & 63, c = (i >> 6) % FNB, t = i / (FNB * 64) * 16 + (l & 15);
+        f32x4 v = red[0][i >> 6][l];
 #pragma unroll
         for (int k = 1; k < NW; ++k)
-            v += red[k][c][l];
+            v += red[k][i >> 6][l];
         const int64_t n = n0 + c * 16 + (l >> 4) * 4;
         if (t >= M)
             continue;
@@ -535,11 +563,18 @@ constexpr TileCost kTiles[] = {
 };
 constexpr float kReduce = 4.4f, kReducePerMega = 1.33f;   // joining K-ranges: + per 10^6 partials
 constexpr int kCus = 256;
-constexpr int kStreamTokens = 16;     // the streaming kernel up to here: one token fragment
-// It quantizes up to so many values itself: each workgroup does them all again, 2 us for 16384
-// tokens x channels on top of the product, as much as a launch of its own (4096 -> 16384
-// channels, us: 9.8, 10.7, 12.9, 17.4 for 1, 2, 4, 8 tokens; in two launches 14.8 for 16).
-constexpr int64_t kOneLaunchValues = 16384;
+
+// Fragments of 16 tokens for the streaming kernel, 0: a tile. It has no workgroups' partial sums
+// to join, but reads every token from the L2 in each workgroup: it wins where one round of
+// workgroups covers N, and where K is short for the second fragment. us, streaming and the best
+// tile, K x N: 16 tokens 4096 x 4096 5.4, 7.7; 4096 x 8192 about 6.6, 8.0; 8192 x 8192 11.9,
+// 15.2; 4096 x 16384 10.3, 9.4. 32 tokens 4096 x 4096 6.5, 7.8; 8192 x 1024 9.1, 8.1; 4096 x
+// 6144 8.5, 8.2; 48 tokens 4096 x 4096 8.0, 8.1.
+int stream_fragments(int64_t M, int64_t N, int64_t nb) {
+    if (M <= 16)
+        return N <= 8192 ? 1 : 0;
+    return M <= 32 && N <= 4096 && nb <= 128 ? 2 : 0;
+}
 
 struct Plan {
     int tile, splits;
@@ -593,7 +628,7 @@ hipError_t run_tile(Mx4Params p, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <bool QX, int ACT, bool CM>
+template <int FMB, bool QX, int ACT, bool CM>
 hipError_t run_stream(const Mx4Args &a, const uint16_t *x, int64_t K, const float *cm, hipStream_t s) {
     const auto go = [&](auto kernel, int64_t channels, int waves) {
         const int64_t blocks = (a.N + channels - 1) / channels;
@@ -603,27 +638,34 @@ hipError_t run_stream(const Mx4Args &a, const uint16_t *x, int64_t K, const floa
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), lds, s, a, x, K, cm);
         return hipGetLastError();
     };
-    // Wavefronts enough to keep memory busy, and few turns of 512 channels for each. Graphs of
-    // one token, us: 4096 x 16384 9.7 with 2 x 4 (10.7 with 1 x 8), 4096 x 4096 4.6 with 1 x 8
-    // (6.0 with 2 x 4, 4.8 with 1 x 16), 16384 x 4096 11.1 with 1 x 16 (12.6 with 1 x 8).
-    if (a.N >= 8192)
-        return go(mx4_stream_kernel<2, 4, QX, ACT, CM>, 32, 4);
-    return a.nb >= 256 ? go(mx4_stream_kernel<1, 16, QX, ACT, CM>, 16, 16)
-                       : go(mx4_stream_kernel<1, 8, QX, ACT, CM>, 16, 8);
+    // A workgroup a CU. us for 16 tokens, K x N: 4096 x 4096 5.4 by 16 channels (32: 6.2), 4096 x
+    // 6144 6.6 by 32 (7.6 by 16); one token through 4096 x 16384 9.9 with 4 wavefronts (8: 10.7).
+    if (a.N <= 4096)
+        return go(mx4_stream_kernel<FMB, 1, 8, QX, ACT, CM>, 16, 8);
+    if constexpr (FMB == 1) {
+        if (a.N <= 8192)
+            return go(mx4_stream_kernel<1, 2, 8, QX, ACT, CM>, 32, 8);
+        if constexpr (QX)
+            return go(mx4_stream_kernel<1, 2, 4, QX, ACT, CM>, 32, 4);
+    }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 size_t mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t nb) {
-    if (M <= kStreamTokens)
+    if (stream_fragments(M, N, nb) != 0)
         return 0;
     const Plan p = plan_of(M, N, nb);
     return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0;
 }
 
 hipError_t launch_mx4_gemm(const Mx4Args &a, void *ws, hipStream_t s) {
-    if (a.M <= kStreamTokens)
-        return run_stream<false, ACT_NONE, false>(a, nullptr, 0, nullptr, s);
+    switch (stream_fragments(a.M, a.N, a.nb)) {
+    case 1: return run_stream<1, false, ACT_NONE, false>(a, nullptr, 0, nullptr, s);
+    case 2: return run_stream<2, false, ACT_NONE, false>(a, nullptr, 0, nullptr, s);
+    default: break;
+    }
     const Plan plan = plan_of(a.M, a.N, a.nb);
     const int64_t panels = (a.nb + 7) / 8;
     Mx4Params p;
@@ -653,17 +695,21 @@ hipError_t launch_mx4_gemm(const Mx4Args &a, void *ws, hipStream_t s) {
     return hipGetLastError();
 }
 
-bool mx4_linear_one_launch(int64_t M, int64_t K) {
-    return M <= kStreamTokens && M * K <= kOneLaunchValues;
+// The streaming kernel's workgroups each quantize all tokens again, 2 us for 16384 values on top
+// of the product, as much as a launch of its own; past 8192 channels they do so in two rounds. us
+// in one launch and in two, tokens x K x N: 4 x 4096 x 4096 6.0, 7.0; 6 x 4096 x 4096 7.0, 7.1;
+// 6 x 2048 x 8192 6.3, 6.7; 2 x 4096 x 16384 10.7, 11.5; 4 x 4096 x 16384 12.2, 11.5.
+bool mx4_linear_one_launch(int64_t M, int64_t N, int64_t K) {
+    return M <= 16 && M * K <= (N <= 8192 ? 16384 : 8192);
 }
 
 hipError_t launch_mx4_linear(const Mx4Args &a, const uint16_t *x, int64_t K, int act,
                              const float *col_mul, hipStream_t s) {
     if (act == ACT_GELU)
-        return col_mul ? run_stream<true, ACT_GELU, true>(a, x, K, col_mul, s)
-                       : run_stream<true, ACT_GELU, false>(a, x, K, nullptr, s);
-    return col_mul ? run_stream<true, ACT_NONE, true>(a, x, K, col_mul, s)
-                   : run_stream<true, ACT_NONE, false>(a, x, K, nullptr, s);
+        return col_mul ? run_stream<1, true, ACT_GELU, true>(a, x, K, col_mul, s)
+                       : run_stream<1, true, ACT_GELU, false>(a, x, K, nullptr, s);
+    return col_mul ? run_stream<1, true, ACT_NONE, true>(a, x, K, col_mul, s)
+                   : run_stream<1, true, ACT_NONE, false>(a, x, K, nullptr, s);
 }
 
 }  // namespace w8a8

@@ -122,7 +122,7 @@ w8a8_status w8a8_mx4_gemm(const uint8_t *xq, const uint8_t *x_scale, const uint8
 }
 
 size_t w8a8_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (check_product(M, N, K) != W8A8_OK || M == 0 || N == 0 || mx4_linear_one_launch(M, K))
+    if (check_product(M, N, K) != W8A8_OK || M == 0 || N == 0 || mx4_linear_one_launch(M, N, K))
         return 0;
     return align_up(code_bytes(M, K)) + align_up(scale_bytes(M, K)) +
            mx4_gemm_workspace_bytes(M, N, blocks_of(K));
@@ -144,7 +144,7 @@ w8a8_status w8a8_mx4_linear(const uint16_t *x, int act, const float *col_mul, co
     const size_t need = w8a8_mx4_linear_workspace_bytes(M, N, K);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
         return W8A8_ERR_WORKSPACE;
-    if (mx4_linear_one_launch(M, K))
+    if (mx4_linear_one_launch(M, N, K))
         return from_hip(launch_mx4_linear(product(nullptr, nullptr, wq, w_scale, bias, y, M, N, K), x, K,
                                           act, col_mul, as_stream(stream)));
     uint8_t *xq = static_cast<uint8_t *>(workspace);

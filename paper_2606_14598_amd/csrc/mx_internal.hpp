@@ -26,7 +26,7 @@ hipError_t launch_mx4_gemm(const Mx4Args &a, void *ws, hipStream_t s);
 
 // Whether the linear runs as one launch, which quantizes the tokens as it multiplies (a.xq and
 // a.xs unused then).
-bool mx4_linear_one_launch(int64_t M, int64_t K);
+bool mx4_linear_one_launch(int64_t M, int64_t N, int64_t K);
 hipError_t launch_mx4_linear(const Mx4Args &a, const uint16_t *x, int64_t K, int act,
                              const float *col_mul, hipStream_t s);
 

@@ -18,7 +18,6 @@ namespace mx {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kBlock = 32;
 constexpr int kTop4 = 2, kTop8 = 8;         // exponents of 6 and 448
 constexpr uint32_t kNaNScale = 255;
 

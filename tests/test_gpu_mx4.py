@@ -146,6 +146,15 @@ def test_product_and_linear(M, N, K):
             assert (err <= tol).all(), (err / tol).max()
 
 
+# Either side of the streaming kernel's limits: 16 and 32 tokens, 4096 and 8192 channels, and
+# of the sizes up to which the linear is one launch.
+@pytest.mark.parametrize("M,N,K", [(1, 8193, 520), (2, 9000, 4096), (3, 8200, 4096), (16, 8192, 33),
+                                   (12, 5001, 1100), (16, 4097, 1024), (17, 4096, 4096), (32, 4000, 600),
+                                   (25, 4097, 300), (20, 600, 4128), (33, 4096, 512), (16, 8208, 300)])
+def test_few_tokens(M, N, K):
+    test_product_and_linear(M, N, K)
+
+
 @pytest.mark.parametrize("M", [3, 40, 300])
 def test_linear_with_transforms_is_quantizer_and_product(M):
     N, K = 200, 1000
