@@ -33,10 +33,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// How the keys of a launch are divided: chunks of `chunk` tokens (a multiple of 128), of which
-// workgroup s of `splits` takes numbers s, s + splits, ...
+// How the keys of a launch are divided: a workgroup's share is `share` tokens (a multiple of
+// 128), or what the lengths make of `target` if that is more, or what divides a sequence's tokens
+// among `splits` workgroups, the most that a head and row tile of it can have, if that is more.
 struct Split {
-    int chunk, splits;
+    int share, splits;
+    int target;      // workgroups that the tokens of all sequences are spread over, 0: share holds
     float *part;     // splits > 1: [splits][T * q heads][dim + 4]: O, m, l; in split 0 the
                      // number of splits the row has (1: its output is written already)
     uint64_t magic;  // n / (page / 16) = n * magic >> 32 for n < 2^22 (kMaxTokens / 16)
@@ -47,7 +49,7 @@ struct Split {
 // float32 sums and bf16 roundings are relative; a rescaling costs as much as a product.
 constexpr float kSlack = 8.0f;
 constexpr int kMaxChunk = 4096;
-constexpr int kSplitRows = 16;
+constexpr int kSplitRows = 16, kTileRows = 128, kTileTokens = 64;
 static_assert(W8A8_KV_MAX_TOKENS / 16 <= 1 << 22 && W8A8_KV_MAX_PAGE / 16 <= 1 << 10, "magic");
 
 struct Seq {
@@ -73,11 +75,28 @@ __device__ __forceinline__ int seen(const Seq &s, int i, int causal) {
     return max(0, causal ? min(s.kv, s.kv - s.lq + i + 1) : s.kv);
 }
 
-// Chunks with a token that some row of row tile rt (of `rows` rows) sees.
-__device__ __forceinline__ int chunks_of(const Seq &s, int rt, int rows, const KvAttnArgs &a,
-                                         int chunk) {
-    const int last = min(rt * rows + rows, s.lq * a.group) - 1;
-    return (seen(s, last / a.group, a.causal) + chunk - 1) / chunk;
+// The share for this call's lengths: their tokens (once a head and row tile) spread evenly,
+// whatever each sequence has of them. A wavefront sums them by itself, in the same order in
+// every workgroup.
+__device__ __forceinline__ int share_of(const KvShape &c, const KvAttnArgs &a, const Split &sp, int rows) {
+    if (sp.target == 0)
+        return sp.share;
+    float sum = 0.0f;
+    for (int i = threadIdx.x & 63; i < a.seqs; i += 64) {
+        const Seq s = sequence(c, a, i);
+        sum += (float)max(s.kv, 0) * (float)((max(s.lq, 0) * a.group + rows - 1) / rows);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2)
+        sum += __shfl_xor(sum, d);
+    const float even = fminf(sum * (float)c.heads / (float)sp.target, (float)W8A8_KV_MAX_TOKENS);
+    return __builtin_amdgcn_readfirstlane(max(((int)even + 127) & ~127, sp.share));
+}
+
+// Its equal pieces, for which Places has room.
+__device__ __forceinline__ int chunk_of(int share) {
+    const int pieces = (share + kMaxChunk - 1) / kMaxChunk;
+    return ((share + pieces - 1) / pieces + 127) & ~127;
 }
 
 __device__ __forceinline__ float max_of_row(float v) {
@@ -162,7 +181,7 @@ __device__ __forceinline__ void fill_places(Places &pl, const KvShape &c, const 
 // Bound by reading the cache: 4 sequences of 100000 tokens (8 heads of 128, e4m3, 4 queries a
 // head) at 5.4 TB/s, 16 of 8000 with 18 heads of 256 at 5.6; one of 200000 in e2m1, 8 queries a
 // head, at 4.6 (about 370 instructions for 32 tokens of 4.3 KB); 48 sequences of very different
-// lengths at 4.1, as the CUs with the longest finish last.
+// lengths at 4.0 (unequal shares, more workgroups that start).
 template <int FMT, int D>
 __global__ void __launch_bounds__(256, D <= 128 ? 3 : 2)
 kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
@@ -190,24 +209,28 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
     const int pair = blockIdx.x - split * pairs;
     const int b = __builtin_amdgcn_readfirstlane(pair / c.heads), head = pair - b * c.heads;
     const Seq seq = sequence(c, a, b);
+    if (split > 0 && (int64_t)split * sp.share >= seq.kv)
+        return;                            // shares are this long or longer
+    const int even = share_of(c, a, sp, kSplitRows);
     const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
     const int64_t v_offset = c.heads * c.head_bytes();     // from a page's keys to its values
     const int scales_at = c.page * CB;                     // from codes to scales
     uint8_t *const vt = lds[wave];
 
     for (int rt = blockIdx.y; rt * kSplitRows < rows; rt += gridDim.y) {
-        const int nch = chunks_of(seq, rt, kSplitRows, a, sp.chunk);
-        const int used = min(sp.splits, nch);
+        const int some_see =
+            seen(seq, (min(rt * kSplitRows + kSplitRows, rows) - 1) / a.group, a.causal);   // some row
+        const int share = max(even, ((some_see + sp.splits - 1) / sp.splits + 127) & ~127);
+        const int used = (some_see + share - 1) / share;
         if (split >= max(used, 1))
             continue;
+        const int chunk = chunk_of(share), nch = (some_see + chunk - 1) / chunk;
         const int row = rt * kSplitRows + r16;
         const bool live = row < rows;
         const int qi = live ? row / a.group : 0;
         const int qh = head * a.group + (live ? row % a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
         const int all_see = seen(seq, rt * kSplitRows / a.group, a.causal);   // every live row
-        const int some_see =
-            seen(seq, (min(rt * kSplitRows + kSplitRows, rows) - 1) / a.group, a.causal);
         u32x4 q[NK][KU / 8];
         {
             const uint16_t *src = a.q + (seq.q0 + qi) * a.q_token + qh * a.q_head;
@@ -228,9 +251,9 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
         f32x4 sums = {};           // in each element: the sum of a row's weights
         uint32_t row_nan = 0;      // blocks of the row's output that a seen NaN value reaches
 
-        for (int ch = split; ch < nch; ch += sp.splits) {
-            const int j_first = ch * sp.chunk;
-            const int j_end = min(j_first + sp.chunk, some_see);
+        for (int ch = split; ch < nch; ch += used) {
+            const int j_first = ch * chunk;
+            const int j_end = min(j_first + chunk, some_see);
             const int ntile = (j_end - j_first + 31) / 32;
             __syncthreads();       // the places and the LDS rows of what came before are read
             fill_places(places, c, a, sp, b, head, j_first, j_end, 2 * ntile);
@@ -479,8 +502,6 @@ __device__ __forceinline__ u32x2 both_halves(float v) {
         u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
 }
 
-constexpr int kTileRows = 128, kTileTokens = 64;
-
 // Many rows (128 a workgroup, 32 a wavefront): 64 tokens at a time are decoded once into LDS
 // for all four wavefronts, between the products of the 64 before; 32x32x16 products with the
 // rows as columns, as above. Keys lie in rows of 2 D + 16 bytes, values in rows of 2 D + 64:
@@ -489,8 +510,8 @@ constexpr int kTileRows = 128, kTileTokens = 64;
 // Bound by instructions: per row and 64 tokens 64 exponentials and some 350 other vector
 // instructions a wavefront beside 64 (heads of 256) or 32 (128) products, two wavefronts a SIMD
 // for heads of up to 128, one above (O and Q alone take 192 registers). 4 x 1000 queries on
-// 6000 keys, causal: 32 heads of 128 at 980 TFLOP/s, 18 heads of 256 at 620; 8 x 512 on 4000,
-// 32 heads of 64 at 730. Staging whole tiles between barriers, before it was spread over the
+// 6000 keys, causal: 32 heads of 128 at 950 TFLOP/s, 18 heads of 256 at 610; 8 x 512 on 4000,
+// 32 heads of 64 at 720. Staging whole tiles between barriers, before it was spread over the
 // products, cost a third of the time at heads of 256.
 //
 // Workgroup -> problem: every 8th workgroup goes to one XCD; a split of a key/value head of a
@@ -534,6 +555,9 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     const int split = __builtin_amdgcn_readfirstlane(unit / pairs), pair = unit - split * pairs;
     const int b = __builtin_amdgcn_readfirstlane(pair / c.heads), head = pair - b * c.heads;
     const Seq seq = sequence(c, a, b);
+    if (split > 0 && (int64_t)split * sp.share >= seq.kv)
+        return;                            // shares are this long or longer
+    const int even = share_of(c, a, sp, kTileRows);
     const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
     const int64_t v_offset = c.heads * c.head_bytes();
 
@@ -541,18 +565,19 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     const int last_rt = (rows + kTileRows - 1) / kTileRows - 1;
     // Row tiles first_rt, first_rt + tiles, ...: more than one only where max_q was too small.
     for (int rt = first_rt; rt <= last_rt; rt += tiles) {
-        const int nch = chunks_of(seq, rt, kTileRows, a, sp.chunk);
-        const int used = min(sp.splits, nch);
+        const int some_see =
+            seen(seq, (min(rt * kTileRows + kTileRows, rows) - 1) / a.group, a.causal);   // some row
+        const int share = max(even, ((some_see + sp.splits - 1) / sp.splits + 127) & ~127);
+        const int used = (some_see + share - 1) / share;
         if (split >= max(used, 1))
             continue;
+        const int chunk = chunk_of(share), nch = (some_see + chunk - 1) / chunk;
         const int row = rt * kTileRows + wave * 32 + r32;
         const bool live = row < rows;
         const int qi = live ? row / a.group : 0;
         const int qh = head * a.group + (live ? row - qi * a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
         const int all_see = seen(seq, rt * kTileRows / a.group, a.causal);
-        const int some_see =
-            seen(seq, (min(rt * kTileRows + kTileRows, rows) - 1) / a.group, a.causal);
         // what some row of this wavefront sees
         const int wave_first = rt * kTileRows + wave * 32;
         const int wave_sees =
@@ -573,9 +598,9 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
         float m = -INFINITY, l = 0.0f;
         uint32_t row_nan = 0;
 
-        for (int ch = split; ch < nch; ch += sp.splits) {
-            const int j_first = ch * sp.chunk;
-            const int j_end = min(j_first + sp.chunk, some_see);
+        for (int ch = split; ch < nch; ch += used) {
+            const int j_first = ch * chunk;
+            const int j_end = min(j_first + chunk, some_see);
             const int ntile = (j_end - j_first + TT - 1) / TT;
             __syncthreads();
             if (threadIdx.x == 0)
@@ -882,37 +907,49 @@ hipError_t launch_join(const Split &sp, int64_t rows, uint16_t *out, hipStream_t
     return hipGetLastError();
 }
 
-// Rows of a sequence and head from which the tile kernel runs. It decodes keys and values once
-// for 128 rows, the other one once for 16.
-constexpr int kManyRows = 48;
+// Whether the tile kernel runs: it decodes keys and values once for 128 rows, the other one once
+// for 16, where 4-bit codes are fewer bytes to read again. Time of the other one by its time, 1800
+// random shapes of 17 to 64 rows of a sequence and head, e4m3 and e2m1: 17 to 32 rows 0.86, 0.75;
+// 33 to 48 0.96, 0.82; 49 to 64 1.04, 0.94.
+// Where heads and sequences alone give half the CUs work, its instructions bound the other one and
+// 16 rows fewer are many: 32 x 8 heads of 128, 16000 keys, e4m3, 48 rows 489 us, by the tile
+// kernel 288; e2m1, 56 rows 345, 259.
+bool many_rows(const KvShape &c, int seqs, int group, int max_q) {
+    const int few = (c.fmt == KV_FP8 ? 48 : 64) - ((int64_t)seqs * c.heads >= 128 ? 16 : 0);
+    return (int64_t)max_q * group > few;
+}
 
-bool many_rows(int group, int max_q) { return (int64_t)max_q * group >= kManyRows; }
+// Up to here one workgroup takes all keys: a second launch costs as much. us divided and whole, 8
+// heads of 128, 4 queries a head: 300 keys 9.7, 8.6; 500 9.8, 9.8; 700 10.0, 11.9.
+constexpr int kWholeTokens = 512;
+// Sequences whose lengths a wavefront sums, 64 at a time, at the start of every workgroup.
+constexpr int kSummed = 512;
 
-// How many ways the keys are divided. A partial result is 4 (dim + 4) bytes a row to write and
-// to read, and a workgroup takes some microseconds to start, so only as many as fill the card.
+// How the keys are divided. A partial result is 4 (dim + 4) bytes a row to write and to read, and
+// a workgroup takes some microseconds to start, so only as many as fill the card: 512 workgroups
+// of few rows, one of many rows a CU (1.5 up to 128 wide heads, where two share one); on 1055
+// random shapes of many rows and 3077 of few, twice as many took 4% and 1% longer, half as many 4%
+// and none. With several sequences the kernels spread the tokens that there are over them, and a
+// long sequence may take 1.5 and 8 times its part of the workgroups. With twice its part 48
+// sequences of up to 16384 tokens, a quarter of that in the mean, took 128 us, with 4 times 104,
+// 8 times 98; many rows, in whose launches empty and small workgroups cost more, take as long
+// with 2 and with 4 times on average, and 216 row tiles of 256 wide heads had better stay whole
+// (227 us, in two parts 250).
 Split split_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
-    const bool many = many_rows(group, max_q);
+    const bool many = many_rows(c, seqs, group, max_q);
     const int tile_rows = many ? kTileRows : kSplitRows;
     // Row tiles: of max_q queries each, and no more than T queries in all make.
     const int64_t tiles = std::min(seqs * (((int64_t)max_q * group + tile_rows - 1) / tile_rows),
                                    T * group / tile_rows + seqs);
     const int64_t blocks = c.heads * tiles;
-    // Few rows: two workgroups a CU for one sequence (8 heads, 200000 tokens of 4 bits: 48 us,
-    // with four a CU 53), eight where several may differ in length, as max_kv bounds them all;
-    // of 512 tokens at least, of 2048 where the heads alone fill the card twice over (64 x 8
-    // heads of 2000 tokens: 52 us, in four parts 60). Many rows, whose partial results are large:
-    // only while they leave a third of the CUs idle (2 heads, 2 x 700 queries on 20000 keys of
-    // 256: 770 us, in five parts 393; 18 heads, 1000 on 6000: 241, in two parts 257).
-    int64_t splits;
-    if (many)
-        splits = std::min<int64_t>(384 / blocks, (max_kv + 1023) / 1024);
-    else
-        splits = std::min<int64_t>(((seqs == 1 ? 512 : 2048) + blocks - 1) / blocks,
-                                   (max_kv + (blocks >= 512 ? 2047 : 511)) / (blocks >= 512 ? 2048 : 512));
     Split sp;
+    const int64_t target = many ? (c.dim <= 128 ? 384 : 256) : 512;
+    const int64_t most = target * (seqs == 1 ? 2 : many ? 3 : 16) / 2 / blocks;
+    const int64_t least = blocks <= 16 ? 256 : blocks < 512 ? 512 : 1024;
+    const int64_t splits = max_kv <= kWholeTokens ? 1 : std::min(most, (max_kv + least - 1) / least);
     sp.splits = (int)std::max<int64_t>(splits, 1);
-    const int64_t chunk = ((max_kv + sp.splits - 1) / sp.splits + 127) / 128 * 128;
-    sp.chunk = (int)std::min<int64_t>(std::max<int64_t>(chunk, 128), kMaxChunk);
+    sp.target = seqs == 1 || seqs > kSummed || sp.splits == 1 ? 0 : (int)target;
+    sp.share = (int)(sp.target ? least : std::max<int64_t>((max_kv + sp.splits - 1) / sp.splits, 1) + 127) / 128 * 128;
     const uint32_t pb = (uint32_t)c.page / 16;
     sp.magic = (((uint64_t)1 << 32) + pb - 1) / pb;
     sp.part = nullptr;
@@ -930,7 +967,7 @@ size_t kv_attention_workspace_bytes(const KvShape &c, int64_t T, int seqs, int g
 hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
     Split sp = split_of(c, a.T, a.seqs, a.group, a.max_q, a.max_kv);
     sp.part = static_cast<float *>(ws);
-    const bool many = many_rows(a.group, a.max_q);
+    const bool many = many_rows(c, a.seqs, a.group, a.max_q);
     const int tile_rows = many ? kTileRows : kSplitRows;
     const int64_t pairs = (int64_t)c.heads * a.seqs, rows = a.T * c.heads * a.group;
     const int64_t tiles =
@@ -951,7 +988,7 @@ hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, 
         if (e != hipSuccess || sp.splits == 1)
             return e;
         // Few splits: a row by D / 4 lanes. Many: 32 outputs of a row by 32 groups of 8 lanes.
-        return sp.splits <= 16 ? launch_join<D, D / 4, 1>(sp, rows, a.out, s)
+        return sp.splits <= 16 || rows * (D / 4) >= 65536 ? launch_join<D, D / 4, 1>(sp, rows, a.out, s)
                                : launch_join<D, 8, 32>(sp, rows, a.out, s);
     };
     const auto go = [&](auto dim) {

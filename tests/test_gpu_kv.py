@@ -187,6 +187,31 @@ def test_attention(fmt, case):
     c.check(c.run(scale=0.3), scale=0.3)
 
 
+# Sequences of very different lengths: shares that the kernels take from the sum of all lengths,
+# of a few sequences, of more than a wavefront sums at once, and of more than it sums at all.
+UNEQUAL = [
+    (128, 1, 4, 16, [1, 3, 1, 2], [9000, 700, 0, 5000]),
+    (64, 2, 1, 16, [1] * 70, [20000, 30000, 0, 1] + [1500] * 66),
+    (64, 1, 2, 16, [1] * 600, [9000] + [i % 40 for i in range(599)]),
+    (128, 1, 2, 64, [70, 1, 130], [2000, 1500, 900]),
+    (256, 2, 1, 64, [128, 40, 0, 129], [6000, 40, 0, 700]),
+    (64, 18, 2, 16, [17] * 9, [1300, 17, 20, 400, 17, 33, 100, 19, 600]),
+]
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("case", range(len(UNEQUAL)))
+def test_unequal_lengths(fmt, case):
+    dim, heads, group, page, qs, kvs = UNEQUAL[case]
+    say(f"attention, unequal lengths {fmt} {UNEQUAL[case][:4]}")
+    c = Case(fmt, dim, heads, group, page, qs, kvs, seed=case)
+    first = c.run()
+    c.check(first)
+    assert torch.equal(first, c.run())
+    c.check(c.run(max_q=max(qs), max_kv=max(kvs)))
+    c.check(c.run(causal=False), causal=False)
+
+
 @pytest.mark.parametrize("fmt", ["fp8", "fp4"])
 def test_decoding_without_starts_and_strided_queries(fmt):
     c = Case(fmt, 128, 2, 4, 16, [1, 1, 1], [20, 0, 333], seed=5)
