@@ -299,7 +299,7 @@ w8a8_status w8a8_read_ceiling(const void *p, int64_t bytes, uint32_t *sums, void
 #define W8A8_MX4_MAX_K (1 << 22)
 
 /* x: [R,K] bf16 of activations or weights, quantized as T(x) * col_mul (act and col_mul as in
- * w8a8_quantize_act_ex). */
+ * w8a8_quantize_act_ex; GELU takes Phi from the table at every K). */
 w8a8_status w8a8_mx4_quantize(const uint16_t *x, int64_t R, int64_t K, int act,
                               const float *col_mul, uint8_t *codes, uint8_t *scales,
                               void *stream);

@@ -46,7 +46,8 @@ struct Split {
 
 // The maximum that exponents are taken from may lag behind by this much: O and l are rescaled
 // only when a row's maximum rises further. Weights up to 2^8 instead of 1 lose nothing, as
-// float32 sums and bf16 roundings are relative; a rescaling costs as much as a product.
+// float32 sums and bf16 roundings are relative; a rescaling costs as much as a product. 4 x 1000
+// queries on 6000 keys, 18 heads of 256: 783 us rescaling at every rise, 670 so.
 constexpr float kSlack = 8.0f;
 constexpr int kMaxChunk = 4096;
 constexpr int kSplitRows = 16, kTileRows = 128, kTileTokens = 64;
@@ -517,7 +518,9 @@ __device__ __forceinline__ u32x2 both_halves(float v) {
 // Workgroup -> problem: every 8th workgroup goes to one XCD; a split of a key/value head of a
 // sequence is given to one XCD with all its row tiles, the last ones (which see the most keys)
 // first, so that its L2 holds the keys. Fewer than kSpreadUnits of them would leave XCDs idle:
-// their row tiles go to all XCDs.
+// their row tiles go to all XCDs. 4 x 1000 queries on 6000 keys take 713 us at 18 heads of 256
+// and 405 at 8 of 128 (4 queries a head) where neighbours in the grid are neighbouring row
+// tiles, 670 and 382 so.
 constexpr int kSpreadUnits = 32;
 
 template <int FMT, int D>

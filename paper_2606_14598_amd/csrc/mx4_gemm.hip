@@ -81,9 +81,9 @@ __device__ __forceinline__ void tile_of(int bid, const Mx4Params &p, int &tm, in
 // zero scales. Panel k + S - 1 is requested while panel k is multiplied.
 //
 // Eight to twelve wavefronts on the large tiles: a product's operands are two LDS reads, and
-// with one wavefront a SIMD their latencies show (256 x 256 by 4 wavefronts 183 us at 4608 x
-// 4096 x 16384, by 8 159). Fragments of half panels read a step ahead across four stages, for
-// four wavefronts, were slower yet (214), as were two workgroups a CU (128 x 128 tiles, 180).
+// with one wavefront a SIMD their latencies show. 256 x 256 by four, whose fragments were read a
+// step ahead across four stages of half panels, took 214 us at 4608 x 4096 x 16384 (288 x 256
+// by twelve: 160) and 258 at 4608 x 16384 x 4096 (138).
 template <int TM, int TN, int WM, int WN, int S>
 __global__ void __launch_bounds__(WM *WN * 64)
 mx4_gemm_kernel(Mx4Params p) {

@@ -110,7 +110,9 @@ hipError_t launch_mx4_quant(const uint16_t *x, int64_t R, int64_t K, int act,
         return hipSuccess;
     const int64_t chunks = (K + 511) / 512;
     // Eight rows a wavefront where that leaves 4096 wavefronts, 16 a CU; else a row each, as a
-    // short call's time is one row's latency (64 x 256: 2.8 us, with four rows 3.4).
+    // short call's time is one row's latency. us by one and by eight, calls in a graph: 64 x 256
+    // 2.4, 5.0; 1024 x 4096 with GELU and multiplier 4.7, 5.9; 2048 x 4096 4.5, 4.3; 1152 x 16384
+    // and 4608 x 16384 with both 16.0, 15.2 and 52.7, 40.1.
     const int rows = R * chunks >= 8 * 4096 ? 8 : 1;
     const int64_t blocks = chunks * ((R + kWaves * rows - 1) / (kWaves * rows));
     if (blocks > 0x7FFFFFFF)
