@@ -903,7 +903,7 @@ template <int D, int LANES, int WAYS>
 hipError_t launch_join(const Split &sp, int64_t rows, uint16_t *out, hipStream_t s) {
     constexpr int jobs = 256 / (LANES * WAYS), pieces = D / (4 * LANES);
     const int64_t blocks = (rows * pieces + jobs - 1) / jobs;
-    if (blocks > 0x7FFFFFFF)
+    if (!launchable(blocks, 256))
         return hipErrorInvalidValue;
     hipLaunchKernelGGL((kv_attention_join_kernel<D, LANES, WAYS>), dim3((unsigned)blocks), dim3(256), 0, s,
                        sp.part, sp.splits, rows, out);
@@ -925,6 +925,8 @@ bool many_rows(const KvShape &c, int seqs, int group, int max_q) {
 // Up to here one workgroup takes all keys: a second launch costs as much. us divided and whole, 8
 // heads of 128, 4 queries a head: 300 keys 9.7, 8.6; 500 9.8, 9.8; 700 10.0, 11.9.
 constexpr int kWholeTokens = 512;
+// Workgroups of a launch of many rows: more than this many with work in them gain nothing.
+constexpr int64_t kMostGroups = 1 << 20;
 // Sequences whose lengths a wavefront sums, 64 at a time, at the start of every workgroup.
 constexpr int kSummed = 512;
 
@@ -973,11 +975,15 @@ hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, 
     const bool many = many_rows(c, a.seqs, a.group, a.max_q);
     const int tile_rows = many ? kTileRows : kSplitRows;
     const int64_t pairs = (int64_t)c.heads * a.seqs, rows = a.T * c.heads * a.group;
-    const int64_t tiles =
-        std::min<int64_t>(((int64_t)a.max_q * a.group + tile_rows - 1) / tile_rows, 65535);
     const int64_t units = pairs * sp.splits;
-    const int64_t blocks = many ? (units >= kSpreadUnits ? (units + 7) / 8 * 8 : units) * tiles : units;
-    if (blocks > 0x7FFFFFFF || rows > 0x7FFFFFFF)
+    const int64_t columns = many && units >= kSpreadUnits ? (units + 7) / 8 * 8 : units;
+    // A workgroup goes on to every tiles-th row tile, so that a loose max_q costs empty workgroups
+    // but never more than kMostGroups of them.
+    int64_t tiles = (std::min<int64_t>(a.max_q, a.T) * a.group + tile_rows - 1) / tile_rows;
+    if (many)
+        tiles = std::min(tiles, std::max<int64_t>(kMostGroups / columns, 1));
+    const int64_t blocks = many ? columns * tiles : units;
+    if (!launchable(blocks, 256) || rows > 0x7FFFFFFF)
         return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks, many ? 1u : (unsigned)tiles);
     const auto run = [&](auto dim, auto format) {

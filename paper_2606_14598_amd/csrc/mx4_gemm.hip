@@ -621,7 +621,7 @@ hipError_t run_tile(Mx4Params p, hipStream_t s) {
     p.tiles_n = (int)((p.a.N + TN - 1) / TN);
     p.gm = 8;
     const int64_t blocks = (int64_t)p.tiles_m * p.tiles_n * p.splits;
-    if (blocks > 0x7FFFFFFF)
+    if (!launchable(blocks, WM * WN * 64))
         return hipErrorInvalidValue;
     hipLaunchKernelGGL((mx4_gemm_kernel<TM, TN, WM, WN, S>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0,
                        s, p);
@@ -632,7 +632,7 @@ template <int FMB, bool QX, int ACT, bool CM>
 hipError_t run_stream(const Mx4Args &a, const uint16_t *x, int64_t K, const float *cm, hipStream_t s) {
     const auto go = [&](auto kernel, int64_t channels, int waves) {
         const int64_t blocks = (a.N + channels - 1) / channels;
-        if (blocks > 0x7FFFFFFF)
+        if (!launchable(blocks, waves * 64))
             return hipErrorInvalidValue;
         const size_t lds = QX ? (size_t)(a.M * ((a.nb | 1) * 16 + a.nb)) : 0;
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), lds, s, a, x, K, cm);
@@ -688,7 +688,7 @@ hipError_t launch_mx4_gemm(const Mx4Args &a, void *ws, hipStream_t s) {
         return e;
     const bool vec = a.N % 4 == 0;
     const int64_t blocks = (a.M * a.N / (vec ? 4 : 1) + 255) / 256;
-    if (blocks > 0x7FFFFFFF)
+    if (!launchable(blocks, 256))
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(vec ? mx4_reduce_kernel<true> : mx4_reduce_kernel<false>, dim3((unsigned)blocks),
                        dim3(256), 0, s, p);

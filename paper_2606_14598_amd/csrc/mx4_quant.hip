@@ -115,7 +115,7 @@ hipError_t launch_mx4_quant(const uint16_t *x, int64_t R, int64_t K, int act,
     // and 4608 x 16384 with both 16.0, 15.2 and 52.7, 40.1.
     const int rows = R * chunks >= 8 * 4096 ? 8 : 1;
     const int64_t blocks = chunks * ((R + kWaves * rows - 1) / (kWaves * rows));
-    if (blocks > 0x7FFFFFFF)
+    if (!launchable(blocks, kWaves * 64))
         return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(kWaves * 64);
     const auto go = [&](auto act_c, auto cm) {

@@ -6,6 +6,12 @@
 
 namespace w8a8 {
 
+// A dimension of a grid holds fewer than 2^32 threads. With more the launch reports nothing and
+// runs the remainder of 2^32, so every grid whose size follows from a call's is checked first.
+constexpr bool launchable(int64_t blocks, int threads) {
+    return blocks <= (int64_t)UINT32_MAX / threads;
+}
+
 // ---------------------------------------------------------------- matrices
 hipError_t launch_mx4_quant(const uint16_t *x, int64_t R, int64_t K, int act,
                             const float *col_mul, uint8_t *codes, uint8_t *scales,
