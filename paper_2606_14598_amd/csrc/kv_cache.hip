@@ -145,18 +145,27 @@ kv_read_kernel(const uint8_t *cache, KvShape c, KvRows k, KvRows v, const int64_
     }
 }
 
-// Calls go(kernel format, head_dim) with both as compile-time constants.
+// Calls go(kernel format, head_dim, grid, first token, tokens), the first two as compile-time
+// constants, for up to kTokens of the T tokens at a time: four make a workgroup of 256 threads.
+constexpr int64_t kTokens = 1 << 25;
+static_assert(launchable(kTokens / 4, 256));
+
 template <typename F>
 hipError_t by_shape(const KvShape &c, int64_t T, F go) {
-    const int64_t blocks = (T + 3) / 4, pieces = (2 * c.heads * (c.dim / 8) + 64 * kLoads - 1) / (64 * kLoads);
-    if (T == 0)
+    const int64_t pieces = (2 * c.heads * (c.dim / 8) + 64 * kLoads - 1) / (64 * kLoads);
+    const auto run = [&](auto fmt, auto dim) {
+        for (int64_t t0 = 0; t0 < T; t0 += kTokens) {
+            const int64_t n = T - t0 < kTokens ? T - t0 : kTokens;
+            go(fmt, dim, dim3((unsigned)((n + 3) / 4), (unsigned)pieces), t0, n);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess)
+                return e;
+        }
         return hipSuccess;
-    if (blocks > 0x7FFFFFFF || pieces > 65535)
-        return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks, (unsigned)pieces);
+    };
     const auto with_dim = [&](auto dim) {
-        return c.fmt == KV_FP8 ? go(std::integral_constant<int, KV_FP8>{}, dim, grid)
-                               : go(std::integral_constant<int, KV_FP4>{}, dim, grid);
+        return c.fmt == KV_FP8 ? run(std::integral_constant<int, KV_FP8>{}, dim)
+                               : run(std::integral_constant<int, KV_FP4>{}, dim);
     };
     switch (c.dim) {
     case 64: return with_dim(std::integral_constant<int, 64>{});
@@ -166,23 +175,23 @@ hipError_t by_shape(const KvShape &c, int64_t T, F go) {
     }
 }
 
+KvRows rows_from(const KvRows &r, int64_t t0) { return {r.p + t0 * r.token, r.token, r.head}; }
+
 }  // namespace
 
 hipError_t launch_kv_write(uint8_t *cache, const KvShape &c, const KvRows &k, const KvRows &v,
                            const int64_t *slots, int64_t T, hipStream_t s) {
-    return by_shape(c, T, [&](auto fmt, auto dim, dim3 grid) {
+    return by_shape(c, T, [&](auto fmt, auto dim, dim3 grid, int64_t t0, int64_t n) {
         hipLaunchKernelGGL((kv_write_kernel<decltype(fmt)::value, decltype(dim)::value>), grid, dim3(256), 0,
-                           s, cache, c, k, v, slots, T);
-        return hipGetLastError();
+                           s, cache, c, rows_from(k, t0), rows_from(v, t0), slots + t0, n);
     });
 }
 
 hipError_t launch_kv_read(const uint8_t *cache, const KvShape &c, const KvRows &k,
                           const KvRows &v, const int64_t *slots, int64_t T, hipStream_t s) {
-    return by_shape(c, T, [&](auto fmt, auto dim, dim3 grid) {
+    return by_shape(c, T, [&](auto fmt, auto dim, dim3 grid, int64_t t0, int64_t n) {
         hipLaunchKernelGGL((kv_read_kernel<decltype(fmt)::value, decltype(dim)::value>), grid, dim3(256), 0,
-                           s, cache, c, k, v, slots, T);
-        return hipGetLastError();
+                           s, cache, c, rows_from(k, t0), rows_from(v, t0), slots + t0, n);
     });
 }
 

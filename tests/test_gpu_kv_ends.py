@@ -36,3 +36,24 @@ def test_many_sequences_without_bounds():
     say("6000 sequences, max_q left out")
     assert torch.equal(w8a8.kv_attention(q, cache, table, lens, q_starts=starts), want)
     assert torch.equal(w8a8.kv_attention(q, cache, table, lens, q_starts=starts, max_q=1), want)
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+def test_more_tokens_than_a_grid_holds(fmt):
+    """2^26 + 5 tokens in one call, padding but for the first two and the last three."""
+    T, dim = (1 << 26) + 5, 64
+    live = torch.tensor([0, 1, (1 << 25) + 7, T - 3, T - 2, T - 1]).cuda()
+    slots = torch.full((T,), -1, dtype=torch.int64, device="cuda")
+    slots[live] = torch.tensor([3, 17, 9, 31, 0, 22]).cuda()
+    kv = _kv(1, 1, dim, 27).cuda()
+    cache = w8a8.kv_cache(2, 1, dim, 16, fmt=fmt)
+    say(f"{T} tokens {fmt}")
+    w8a8.kv_write(cache, kv[:, 0].expand(T, 1, dim), kv[:, 1].expand(T, 1, dim), slots, fmt=fmt)
+    one = w8a8.kv_cache(1, 1, dim, 16, fmt=fmt)
+    zero = torch.zeros(1, dtype=torch.int64, device="cuda")
+    w8a8.kv_write(one, kv[:, 0], kv[:, 1], zero, fmt=fmt)
+    k, v = w8a8.kv_read(cache, slots, dim, fmt=fmt)
+    for got, want in zip((k, v), w8a8.kv_read(one, zero, dim, fmt=fmt)):
+        assert torch.equal(got[live], want.expand(6, 1, dim))
+        for at in (2, 1 << 25, (1 << 26) - 3, T - 10):
+            assert (got[at:at + 5] == 0).all()
