@@ -100,6 +100,15 @@ __device__ __forceinline__ int chunk_of(int share) {
     return ((share + pieces - 1) / pieces + 127) & ~127;
 }
 
+// A row's maximum before its first key: minus infinity where it sees none, else the least finite
+// number. A sum of zero then tells a row without keys (zeros) from one all of whose scores are
+// minus infinity, as a query with an infinity has them (NaN, as exp(-inf - -inf) is).
+__device__ __forceinline__ float start_of(int limit) { return limit > 0 ? -__FLT_MAX__ : -INFINITY; }
+
+__device__ __forceinline__ float inverse(float l, float m) {
+    return l == 0.0f ? (m == -INFINITY ? 0.0f : NAN) : 1.0f / l;
+}
+
 __device__ __forceinline__ float max_of_row(float v) {
     // lanes l, l ^ 16, l ^ 32, l ^ 48 hold the same row
     u32x2 r = __builtin_bit_cast(
@@ -248,7 +257,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x4{};
-        float m = -INFINITY;
+        float m = start_of(limit);
         f32x4 sums = {};           // in each element: the sum of a row's weights
         uint32_t row_nan = 0;      // blocks of the row's output that a seen NaN value reaches
 
@@ -472,7 +481,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
             const int64_t out_row =
                 (seq.q0 + rr / a.group) * q_heads + head * a.group + rr % a.group;
             if (used <= 1) {
-                const float inv = all_l[r] == 0.0f ? 0.0f : 1.0f / all_l[r];
+                const float inv = inverse(all_l[r], all_m[r]);
                 *reinterpret_cast<u32x2 *>(a.out + out_row * D + d) =
                     u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
             } else {
@@ -598,7 +607,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x16{};
-        float m = -INFINITY, l = 0.0f;
+        float m = start_of(limit), l = 0.0f;
         uint32_t row_nan = 0;
 
         for (int ch = split; ch < nch; ch += used) {
@@ -805,7 +814,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
         if (!live)
             continue;        // the next row tile's barriers are reached all the same
         const int64_t out_row = (seq.q0 + qi) * q_heads + qh;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const float inv = inverse(l, m);
         float *const part = sp.part + (split * a.T * q_heads + out_row) * (D + 4);
 #pragma unroll
         for (int f = 0; f < F; ++f) {
@@ -893,7 +902,7 @@ kv_attention_join_kernel(const float *part, int splits, int64_t rows, uint16_t *
         }
     }
     if (used > 1) {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const float inv = inverse(l, m);
         *reinterpret_cast<u32x2 *>(out + row * D + d) =
             u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
     }

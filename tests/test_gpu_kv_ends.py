@@ -1,10 +1,12 @@
 """The quantized cache and the attention over it at the ends of their ranges."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2606_14598_amd as w8a8
 from _helpers import say
-from test_gpu_kv import _kv
+from _mx_ref import attention, f64
+from test_gpu_kv import Case, _kv
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +59,51 @@ def test_more_tokens_than_a_grid_holds(fmt):
         assert torch.equal(got[live], want.expand(6, 1, dim))
         for at in (2, 1 << 25, (1 << 26) - 3, T - 10):
             assert (got[at:at + 5] == 0).all()
+
+
+# ---------------------------------------------------------------- scores without a finite one
+
+def _slots(c):
+    return [int(c.table[b, j // c.page]) * c.page + j % c.page
+            for b, n in enumerate(c.kvs) for j in range(n)]
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("qs,kvs", [([3], [40]), ([1], [3000]), ([200], [150]), ([150], [5000])])
+def test_infinite_queries_give_nan(fmt, qs, kvs):
+    """An infinity in a query makes all its scores infinite. exp(score - max) is then NaN whatever
+    the sign; a query that sees no key still gives zeros."""
+    c = Case(fmt, 64, 1, 2, 16, qs, kvs, seed=21)
+    kv = _kv(sum(kvs), 1, 64, 22)
+    kv[:, 0, 0, 5] = 2.0 ** 6
+    c.write(kv, _slots(c))
+    lq, lk = qs[0], kvs[0]
+    c.q[::2, 0, 5], c.q[1::2, 0, 5] = -float("inf"), float("inf")
+    c.q[::2, 1, 5] = float("inf")
+    y = f64(c.run())
+    sees = np.array([lk - lq + i >= 0 for i in range(lq)])
+    assert (y[~sees] == 0).all()
+    assert np.isnan(y[sees, 0]).all() and np.isnan(y[sees & (np.arange(lq) % 2 == 0), 1]).all()
+    odd = sees & (np.arange(lq) % 2 == 1)
+    assert np.isfinite(y[odd, 1]).all()
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("qs,kvs", [([2], [60]), ([1], [4000]), ([100], [4000])])
+def test_scores_that_overflow_take_no_weight(fmt, qs, kvs):
+    """Finite queries and keys whose products pass float32's least number: those keys' weights are
+    zero, in a part of the keys that holds nothing else too."""
+    c = Case(fmt, 64, 1, 1, 16, qs, kvs, seed=23)
+    kv = _kv(sum(kvs), 1, 64, 24)
+    n = kvs[0] // 2
+    kv[:, 0, 0, :32] = 0.0
+    kv[:n, 0, 0, 5] = 8.0
+    c.write(kv, _slots(c))
+    c.q[:, 0, 5] = -3e38
+    y, at = f64(c.run()), kvs[0] - qs[0]
+    q = f64(c.q)[:, 0]
+    q[:, 5] = 0.0
+    for i in range(qs[0]):
+        v = c.values[n:at + i + 1, :, 0]
+        want, mag = attention(q[i:i + 1], v[:, 0], v[:, 1], 64 ** -0.5, False)
+        assert (np.abs(y[i, 0] - want[0]) <= mag[0] * 2.0 ** -7 + 1e-30).all()
