@@ -362,11 +362,12 @@ w8a8_status w8a8_kv_read(const uint8_t *cache, int64_t pages, int page, int head
  * with j <= kv_lens[b] - lq + i.
  *   out [T, heads * group, dim] = sum_j p_j v_j / sum_j p_j, p_j = exp(scale * q.k_j - max),
  * and zeros where a query sees no token. What lies in the cache past kv_lens[b], or is hidden
- * from a query, has no effect on it, NaN included. Scores and sums are float32; the weights
- * p_j are rounded to one or two bf16 terms for the matrix cores.
+ * from a query, has no effect on it, NaN included. Scores and sums are float32. The weights p_j
+ * are rounded for the matrix cores, to two bf16 terms (2^-16 of each) in every sequence with
+ * lq * group <= 64, whatever else the call holds; in others one term (2^-8) may be all.
  * max_q and max_kv are bounds on a sequence's queries and tokens that the launch is laid out
- * for; with other values the results are the same (table_pages * page bounds the tokens; it is
- * at most W8A8_KV_MAX_TOKENS, else W8A8_ERR_SHAPE).
+ * for; with other values the results are the same but for such rounding (table_pages * page
+ * bounds the tokens; it is at most W8A8_KV_MAX_TOKENS, else W8A8_ERR_SHAPE).
  * Table entries that are read have to lie inside the cache: others read some page of it.
  * workspace: w8a8_kv_attention_workspace_bytes(...) bytes, 256-byte aligned. */
 w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head,

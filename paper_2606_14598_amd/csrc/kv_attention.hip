@@ -12,8 +12,8 @@
 // holds one row, so maxima, sums and the rescaling of O stay inside a lane but for one
 // exchange of the maximum between the lanes that share a row, and the weights P^T come out of
 // S^T in the layout the second product takes them in. Codes decode to bf16 exactly; the
-// weights are rounded for the second product, to one bf16 term (2^-8 of each at most) where
-// there are many rows and products bind, to two (2^-16) where there are few.
+// weights are rounded for the second product: to two bf16 terms (2^-16 of each at most), or to one
+// (2^-8) in the tile kernel for sequences of more than kTwoTermRows rows, whose products bind.
 #include "../../include/w8a8.h"
 #include "mx_internal.hpp"
 #include "mx_math.hpp"
@@ -49,6 +49,10 @@ struct Split {
 // float32 sums and bf16 roundings are relative; a rescaling costs as much as a product. 4 x 1000
 // queries on 6000 keys, 18 heads of 256: 783 us rescaling at every rise, 670 so.
 constexpr float kSlack = 8.0f;
+// Sequences of up to this many rows (queries x heads that share a key/value head) have their
+// weights in two bf16 terms whatever runs, so that a query's rounding depends on its own sequence
+// only, not on the batch or the bounds that the launch is laid out for.
+constexpr int kTwoTermRows = 64;
 constexpr int kMaxChunk = 4096;
 constexpr int kSplitRows = 16, kTileRows = 128, kTileTokens = 64;
 static_assert(W8A8_KV_MAX_TOKENS / 16 <= 1 << 22 && W8A8_KV_MAX_PAGE / 16 <= 1 << 10, "magic");
@@ -590,6 +594,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
         const int qh = head * a.group + (live ? row - qi * a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
         const int all_see = seen(seq, rt * kTileRows / a.group, a.causal);
+        const bool two_terms = rows <= kTwoTermRows;
         // what some row of this wavefront sees
         const int wave_first = rt * kTileRows + wave * 32;
         const int wave_sees =
@@ -761,6 +766,10 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                 const uint8_t *vp = values[st] + (4 * h + ((lane & 15) >> 2)) * RSV +
                                     ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
                 u32x2 fv[2][2];
+                const auto value_of = [&](int z) __attribute__((always_inline)) {
+                    return __builtin_bit_cast(bf16x8, u32x4{fv[z & 1][0][0], fv[z & 1][0][1],
+                                                            fv[z & 1][1][0], fv[z & 1][1][1]});
+                };
                 const auto read_values = [&](int z) __attribute__((always_inline)) {
                     const uint8_t *src = vp + 16 * (z / F) * RSV + z % F * 64;
                     fv[z & 1][0] = __builtin_bit_cast(
@@ -768,6 +777,35 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                     fv[z & 1][1] = __builtin_bit_cast(
                         u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(src + 8 * RSV)));
                 };
+                if (two_terms) {
+                    // The second terms, weights computed again: code of its own in front of the
+                    // products below leaves those as they are for many rows.
+                    float own_base = base;
+                    asm volatile("" : "+v"(own_base));
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        u32x4 rest;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int w = 4 * u + i;
+                            const float x = __builtin_amdgcn_exp2f(
+                                __builtin_fmaf(s[w / 8][w % 8 * 2], a.scale, -own_base));
+                            const float y = __builtin_amdgcn_exp2f(
+                                __builtin_fmaf(s[w / 8][w % 8 * 2 + 1], a.scale, -own_base));
+                            const uint32_t r = pack_bf16(x, y);
+                            rest[i] = pack_bf16(x - __uint_as_float(r << 16),
+                                                y - __uint_as_float(r & 0xFFFF0000u));
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int f = 0; f < F; ++f) {
+                            read_values(u * F + f);
+                            o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                value_of(u * F + f), __builtin_bit_cast(bf16x8, rest), o[f], 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                }
                 u32x4 p[4];
                 const auto weight = [&](auto qc) __attribute__((always_inline)) {
                     constexpr int w = decltype(qc)::value;     // of 16 pairs
@@ -800,9 +838,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                         static_assert(2 * NU <= 4 * F, "loads between the products");
                         __builtin_amdgcn_sched_barrier(0);
                         o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            __builtin_bit_cast(bf16x8, u32x4{fv[z & 1][0][0], fv[z & 1][0][1],
-                                                             fv[z & 1][1][0], fv[z & 1][1][1]}),
-                            __builtin_bit_cast(bf16x8, p[u]), o[f], 0, 0, 0);
+                            value_of(z), __builtin_bit_cast(bf16x8, p[u]), o[f], 0, 0, 0);
                         __builtin_amdgcn_sched_barrier(0);
                     }(), ...);
                 }(std::make_integer_sequence<int, 4 * F>{});
@@ -920,15 +956,13 @@ hipError_t launch_join(const Split &sp, int64_t rows, uint16_t *out, hipStream_t
 }
 
 // Whether the tile kernel runs: it decodes keys and values once for 128 rows, the other one once
-// for 16, where 4-bit codes are fewer bytes to read again. Time of the other one by its time, 1800
-// random shapes of 17 to 64 rows of a sequence and head, e4m3 and e2m1: 17 to 32 rows 0.86, 0.75;
-// 33 to 48 0.96, 0.82; 49 to 64 1.04, 0.94.
-// Where heads and sequences alone give half the CUs work, its instructions bound the other one and
-// 16 rows fewer are many: 32 x 8 heads of 128, 16000 keys, e4m3, 48 rows 489 us, by the tile
-// kernel 288; e2m1, 56 rows 345, 259.
-bool many_rows(const KvShape &c, int seqs, int group, int max_q) {
-    const int few = (c.fmt == KV_FP8 ? 48 : 64) - ((int64_t)seqs * c.heads >= 128 ? 16 : 0);
-    return (int64_t)max_q * group > few;
+// for 16, where 4-bit codes are fewer bytes to read again. Both have two terms up to kTwoTermRows.
+// Time of the other one by its time, 348 shapes of 20 to 64 rows of a sequence and head, e4m3 and
+// e2m1: 20 and 32 rows 0.73, 0.61; 40 and 48 0.83, 0.69; 56 and 64 0.91, 0.77, and of those that
+// take 60 us or more 1.12, 0.82 (32 x 8 heads of 128, 16000 keys, 56 rows: e4m3 by the tile kernel
+// 379 us, e2m1 by it 376 and by the other one 345).
+bool many_rows(const KvShape &c, int group, int max_q) {
+    return (int64_t)max_q * group > (c.fmt == KV_FP8 ? 48 : 64);
 }
 
 // Up to here one workgroup takes all keys: a second launch costs as much. us divided and whole, 8
@@ -950,7 +984,7 @@ constexpr int kSummed = 512;
 // with 2 and with 4 times on average, and 216 row tiles of 256 wide heads had better stay whole
 // (227 us, in two parts 250).
 Split split_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
-    const bool many = many_rows(c, seqs, group, max_q);
+    const bool many = many_rows(c, group, max_q);
     const int tile_rows = many ? kTileRows : kSplitRows;
     // Row tiles: of max_q queries each, and no more than T queries in all make.
     const int64_t tiles = std::min(seqs * (((int64_t)max_q * group + tile_rows - 1) / tile_rows),
@@ -981,7 +1015,7 @@ size_t kv_attention_workspace_bytes(const KvShape &c, int64_t T, int seqs, int g
 hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
     Split sp = split_of(c, a.T, a.seqs, a.group, a.max_q, a.max_kv);
     sp.part = static_cast<float *>(ws);
-    const bool many = many_rows(c, a.seqs, a.group, a.max_q);
+    const bool many = many_rows(c, a.group, a.max_q);
     const int tile_rows = many ? kTileRows : kSplitRows;
     const int64_t pairs = (int64_t)c.heads * a.seqs, rows = a.T * c.heads * a.group;
     const int64_t units = pairs * sp.splits;

@@ -107,3 +107,76 @@ def test_scores_that_overflow_take_no_weight(fmt, qs, kvs):
         v = c.values[n:at + i + 1, :, 0]
         want, mag = attention(q[i:i + 1], v[:, 0], v[:, 1], 64 ** -0.5, False)
         assert (np.abs(y[i, 0] - want[0]) <= mag[0] * 2.0 ** -7 + 1e-30).all()
+
+
+# ---------------------------------------------------------------- rounding of the weights
+
+class Cancelling(Case):
+    """Values of +1 and -1 in pairs of tokens whose keys differ by one sign, so that outputs nearly
+    cancel: what is left shows how the weights were rounded, not how the output was."""
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        kv = _kv(sum(self.kvs), self.heads, self.dim, 77)
+        g = torch.Generator().manual_seed(78)
+        kv[:, 0] = torch.randn(kv[:, 0].shape, generator=g).to(torch.bfloat16)
+        sign = torch.where(torch.rand(kv[:, 1].shape, generator=g) < 0.5, -1.0, 1.0)
+        kv[:, 1] = sign.to(torch.bfloat16)
+        for at in range(0, kv.shape[0] - 1, 2):
+            kv[at + 1, 0], kv[at + 1, 1] = kv[at, 0], -kv[at, 1]
+            kv[at + 1, 0, :, 0] *= -1.0
+        self.write(kv, _slots(self))
+
+    def check_two_terms(self, y, only=None):
+        """Each weight within 2^-16 of itself (two bf16 terms), the exponential and its argument
+        within 2^-20, a score within dim 2^-23 of sum |q k|, sums of n weights within n 2^-23; all
+        of it twice, for the sum of weights that divides; the output's own rounding 2^-8. Values
+        are +1 and -1. One bf16 term would leave 2^-9 / sqrt(3 n) of noise, several times that."""
+        scale = 1.0 / self.dim
+        y, q = f64(y), f64(self.q)
+        at_q = at_k = 0
+        for b, (lq, lk) in enumerate(zip(self.qs, self.kvs)):
+            for h in range(self.heads * self.group):
+                if only is not None and b not in only:
+                    continue
+                kv = self.values[at_k:at_k + lk, :, h // self.group]
+                rows = q[at_q:at_q + lq, h]
+                want, _ = attention(rows, kv[:, 0], kv[:, 1], scale, True)
+                score = (np.abs(rows) @ np.abs(kv[:, 0]).T).max(1) * scale
+                tol = 2 * (2.0 ** -16 + 2.0 ** -20 + (self.dim * score[:, None] + lk) * 2.0 ** -23)
+                err = np.abs(y[at_q:at_q + lq, h] - want)
+                assert (err <= tol + np.abs(want) * 2.0 ** -8).all(), (b, lq, lk, h, (err / tol).max())
+            at_q, at_k = at_q + lq, at_k + lk
+
+
+TWO_TERMS = [
+    # dim, heads, group, page, queries, keys: up to 64 rows of a sequence and head
+    (128, 2, 4, 16, [10], [60]),
+    (128, 2, 4, 16, [10], [1400]),                  # divided keys
+    (64, 16, 4, 16, [10] * 8, [50] * 8),            # enough heads and sequences for 128-row tiles
+    (256, 16, 2, 16, [28] * 8, [44] * 8),
+    (128, 16, 4, 16, [12] * 8, [700, 30] * 4),
+    (192, 8, 1, 16, [64] * 2, [80, 700]),
+    (128, 2, 4, 16, [1] * 48, [40] * 48),           # one token each, of a batch
+    (64, 4, 1, 16, [33, 64, 1], [50, 64, 3]),
+]
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("case", range(len(TWO_TERMS)))
+def test_weights_of_few_rows_in_two_terms(fmt, case):
+    """Whatever the batch, the bounds that the launch is laid out for, and the kernel."""
+    dim, heads, group, page, qs, kvs = TWO_TERMS[case]
+    say(f"two terms {fmt} {TWO_TERMS[case]}")
+    c = Cancelling(fmt, dim, heads, group, page, qs, kvs, seed=case)
+    for hints in ({}, dict(max_q=max(qs), max_kv=max(kvs)), dict(max_q=1000), dict(max_q=1)):
+        c.check_two_terms(c.run(scale=1.0 / dim, **hints))
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+def test_weights_of_few_rows_beside_a_prompt(fmt):
+    """Decoding sequences in one call with a prompt, which may round its weights to one term."""
+    c = Cancelling(fmt, 128, 2, 4, 16, [1, 200, 16, 1], [50, 300, 41, 640], seed=3)
+    y = c.run(scale=1.0 / 128)
+    c.check_two_terms(y, only=(0, 2, 3))
+    c.check(y, scale=1.0 / 128)
