@@ -135,6 +135,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
 }
 
+// Four neighbouring outputs: v times inv. bf16 tensors may begin at any element.
+__device__ __forceinline__ void store_outputs(uint16_t *out, const f32x4 &v, float inv) {
+    *reinterpret_cast<Bytes8 *>(out) =
+        Bytes8{{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)}};
+}
+
 // Element E8 (8 values, four words) of a unit's codes.
 template <int FMT, int E8>
 __device__ __forceinline__ u32x4 decode_part(const u32x4 &codes, float s) {
@@ -486,8 +492,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 (seq.q0 + rr / a.group) * q_heads + head * a.group + rr % a.group;
             if (used <= 1) {
                 const float inv = inverse(all_l[r], all_m[r]);
-                *reinterpret_cast<u32x2 *>(a.out + out_row * D + d) =
-                    u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+                store_outputs(a.out + out_row * D + d, v, inv);
             } else {
                 float *p = sp.part + (split * a.T * q_heads + out_row) * (D + 4);
                 *reinterpret_cast<f32x4 *>(p + d) = v;
@@ -862,8 +867,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                 if (nan)
                     v = f32x4{NAN, NAN, NAN, NAN};
                 if (used <= 1)
-                    *reinterpret_cast<u32x2 *>(a.out + out_row * D + d) =
-                        u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+                    store_outputs(a.out + out_row * D + d, v, inv);
                 else
                     *reinterpret_cast<f32x4 *>(part + d) = v;
             }
@@ -939,8 +943,7 @@ kv_attention_join_kernel(const float *part, int splits, int64_t rows, uint16_t *
     }
     if (used > 1) {
         const float inv = inverse(l, m);
-        *reinterpret_cast<u32x2 *>(out + row * D + d) =
-            u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+        store_outputs(out + row * D + d, v, inv);
     }
 }
 

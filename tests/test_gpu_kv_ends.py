@@ -180,3 +180,26 @@ def test_weights_of_few_rows_beside_a_prompt(fmt):
     y = c.run(scale=1.0 / 128)
     c.check_two_terms(y, only=(0, 2, 3))
     c.check(y, scale=1.0 / 128)
+
+
+# ---------------------------------------------------------------- alignment
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("dim,qs,kvs", [(128, [1, 3], [40, 300]), (64, [1], [9000]),
+                                        (256, [2], [5000]), (128, [100, 2], [300, 7]),
+                                        (192, [120], [6000])])
+def test_queries_and_outputs_at_any_element(fmt, dim, qs, kvs):
+    """Both kernels, keys whole and divided: q and out at odd elements give the same bits, and
+    nothing around out is written."""
+    c = Case(fmt, dim, 2, 2, 16, qs, kvs, seed=31)
+    T, n = sum(qs), sum(qs) * 4 * dim
+    say(f"any element {fmt} {dim} {qs} {kvs}")
+    want = c.run()
+    for off in (1, 2, 3):
+        flat = torch.zeros(n + 8, dtype=torch.bfloat16, device="cuda")
+        q = flat[off:off + n].view(T, 4, dim)
+        q.copy_(c.q)
+        guard = torch.full((n + 8,), 7.0, dtype=torch.bfloat16, device="cuda")
+        c.run(q=q, out=guard[off:off + n].view(T, 4, dim))
+        assert torch.equal(guard[off:off + n].view(T, 4, dim), want)
+        assert (guard[:off] == 7).all() and (guard[off + n:] == 7).all()
