@@ -65,6 +65,9 @@ w8a8_status check_rows(const KvShape &c, const void *k, const void *v, const int
     return T > 0 && (!k || !v || !slots) ? W8A8_ERR_NULL : W8A8_OK;
 }
 
+// The bound on a sequence's queries that a launch is laid out for: a loose one, so never 0.
+int query_bound(int max_q) { return max_q > 1 ? max_q : 1; }
+
 }  // namespace
 
 #pragma GCC visibility push(default)
@@ -202,9 +205,9 @@ size_t w8a8_kv_attention_workspace_bytes(int page, int heads, int dim, int fmt, 
                                          int64_t T, int seqs, int max_q, int max_kv) {
     KvShape c;
     if (!cache_shape(c, 1, page, heads, dim, fmt) || group < 1 || T < 1 || seqs < 1 ||
-        max_q < 1 || max_kv < 0)
+        max_q < 0 || max_kv < 0)
         return 0;
-    return kv_attention_workspace_bytes(c, T, seqs, group, max_q, max_kv);
+    return kv_attention_workspace_bytes(c, T, seqs, group, query_bound(max_q), max_kv);
 }
 
 w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
@@ -245,7 +248,7 @@ w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head
     a.group = group;
     a.table_pages = pages > 0 ? table_pages : 0;
     a.causal = causal;
-    a.max_q = max_q > 1 ? max_q : 1;
+    a.max_q = query_bound(max_q);
     a.max_kv = max_kv;
     // The kernels scale a maximum instead of every score, and mask with minus infinity: a
     // positive factor. A zero becomes so small a one that all weights are 1.

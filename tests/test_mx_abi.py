@@ -102,6 +102,18 @@ def test_attention_refusals(lib):
     assert lib.w8a8_kv_attention_workspace_bytes(16, 2, 96, 0, 4, 6, 3, 4, 64) == 0
 
 
+def test_attention_workspace_for_a_bound_of_no_queries(lib):
+    """max_q = 0 is a bound like any other: the size that is asked for is the size that the call
+    needs."""
+    def size(max_q):
+        return lib.w8a8_kv_attention_workspace_bytes(64, 8, 128, 0, 4, 48, 48, max_q, 16384)
+    need = size(0)
+    assert need == size(1) > 0 and size(-1) == 0
+    st = lib.w8a8_kv_attention(F, 4096, 128, F, 4, 64, 8, 128, 0, F, 256, 256, F, F, 48, 48, 4, 0.1,
+                               1, 0, 16384, F, F, need - 1, None)
+    assert st == WORK
+
+
 def test_binding_refusals():
     bf, u8 = torch.bfloat16, torch.uint8
     x = torch.zeros(4, 64, dtype=bf)
