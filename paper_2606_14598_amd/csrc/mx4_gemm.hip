@@ -12,6 +12,7 @@
 // random codes, 6.4 PFLOP/s from registers; 2.3 GHz and 9.1 on zeros) and by waits for panels.
 // 4608 x 4096 x 16384 runs at 3.8 PFLOP/s, 4608 x 16384 x 4096 in one round of tiles at 4.5. Few
 // tokens: bound by reading W; 1 x 4096 x 16384 takes 9.8 us (3.7 TB/s) with its quantizer.
+#include "../../include/w8a8.h"
 #include "mx_internal.hpp"
 #include "mx_quant.hpp"
 
@@ -28,8 +29,15 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRsrcWord3 = 0x00020000;     // raw 32-bit buffer
-constexpr int kOOB = 0x7FFFFFF0;           // beyond any buffer: the load gives zero
+constexpr uint32_t kOOB = 0x7FFFFFF0;      // beyond any buffer: the load gives zero
 constexpr int kPanel = 128;                // bytes of codes of a row in a K-panel
+
+// Offset `at` moved on by some rows, forwards or back; from kOOB it stays beyond the buffer, for
+// which a sum may pass 2^31 but never 2^32.
+__host__ __device__ constexpr uint32_t rows_on(uint32_t at, int rows, int row_bytes) {
+    return at + (uint32_t)(rows * row_bytes);
+}
+constexpr int kMostRowBytes = W8A8_MX4_MAX_K / 32 * 16;
 
 __device__ __forceinline__ i32x8 frag(i32x4 v) {
     return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
@@ -97,6 +105,11 @@ mx4_gemm_kernel(Mx4Params p) {
     static_assert(WTM % 32 == 0 && WTN % 32 == 0 && NW % 4 == 0, "tile");
     static_assert(TN % SR == 0 && TM % SR == 0, "scale loads");
     static_assert(S >= 2 && (S - 1) * NV <= 63, "loads in flight");
+    // From kOOB, the longest rows: neither the last load of a stage nor the first of its tokens'
+    // rows lands in a buffer of TM or TN rows.
+    static_assert(rows_on(kOOB, NV * NW * 8, kMostRowBytes) > kOOB &&
+                      rows_on(kOOB, -TN, kMostRowBytes) > (uint32_t)(TM > TN ? TM : TN) * kMostRowBytes,
+                  "beyond the buffers");
     constexpr int RS = 2 * WTN + 16;       // output staging: bytes of a token's row
     static_assert(NW * 32 * RS <= S * STAGE && S * STAGE + TN * 4 <= 163840, "LDS");
     __shared__ __attribute__((aligned(1024))) uint8_t smem[S * STAGE + TN * 4];
@@ -134,9 +147,9 @@ mx4_gemm_kernel(Mx4Params p) {
     // past the rows' ends.
     const auto codes_at = [&](int kt) {
         const int k = (first_panel + kt) * kPanel + lchunk;
-        return kt < nk && k < row_bytes ? lrow * row_bytes + k : kOOB;
+        return kt < nk && k < row_bytes ? (uint32_t)(lrow * row_bytes + k) : kOOB;
     };
-    const auto issue = [&](auto ic, int kt, int at, int so) __attribute__((always_inline)) {
+    const auto issue = [&](auto ic, int kt, uint32_t at, int so) __attribute__((always_inline)) {
         constexpr int i = decltype(ic)::value;
         const int n = i * NW + NW <= NI ? i * NW + wave : min(i * NW + wave, NI - 1);
         if (i * NW + NW <= IC || n < IC) {
@@ -144,7 +157,7 @@ mx4_gemm_kernel(Mx4Params p) {
             uint8_t *dst = smem + so + n * 1024;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 w ? rw : rx, (__attribute__((address_space(3))) void *)dst, 16,
-                at + (i * NW * 8 - (w ? 0 : TN)) * row_bytes, 0, 0, 0);
+                (int)rows_on(at, i * NW * 8 - (w ? 0 : TN), row_bytes), 0, 0, 0);
         } else {
             const int row = (n - IC) * SR;             // of the stage's scale words
             const bool w = row < TN, in = kt < nk;     // past the last panel: an empty buffer
@@ -188,7 +201,7 @@ mx4_gemm_kernel(Mx4Params p) {
     };
     // With two stages all loads go out in the first step, else a quarter in each.
     constexpr int VPS = S == 2 ? NV : (NV + 3) / 4;
-    const auto step = [&](auto sc, int so, int kt, int at, int so_load) __attribute__((always_inline)) {
+    const auto step = [&](auto sc, int so, int kt, uint32_t at, int so_load) __attribute__((always_inline)) {
         constexpr int s = decltype(sc)::value;
         constexpr int nr = s < 3 ? NR : 0;
         constexpr int va = s * VPS < NV ? s * VPS : NV, vb = va + VPS < NV ? va + VPS : NV;
@@ -249,7 +262,8 @@ mx4_gemm_kernel(Mx4Params p) {
             for (int q = 0; q < NR; ++q)
                 read_frag(q, so, 0);
             __builtin_amdgcn_sched_barrier(0);
-            const int kl = kt + S - 1, lo = ld * STAGE, at = codes_at(kl);
+            const int kl = kt + S - 1, lo = ld * STAGE;
+            const uint32_t at = codes_at(kl);
             step(std::integral_constant<int, 0>{}, so, kl, at, lo);
             step(std::integral_constant<int, 1>{}, so, kl, at, lo);
             step(std::integral_constant<int, 2>{}, so, kl, at, lo);
