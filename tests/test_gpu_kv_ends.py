@@ -203,3 +203,75 @@ def test_queries_and_outputs_at_any_element(fmt, dim, qs, kvs):
         c.run(q=q, out=guard[off:off + n].view(T, 4, dim))
         assert torch.equal(guard[off:off + n].view(T, 4, dim), want)
         assert (guard[:off] == 7).all() and (guard[off + n:] == 7).all()
+
+
+# ---------------------------------------------------------------- divided keys
+
+def _expect(c, lens, y, queries=1):
+    """Outputs of sequences cut to `lens` tokens against the 64-bit form, within 2^-7 of the weighted
+    mean of |v| (the rounding of weights and output)."""
+    y, q = f64(y), f64(c.q)
+    starts = np.cumsum([0] + list(c.kvs))
+    for b, n in enumerate(lens):
+        kv = c.values[starts[b]:starts[b] + n]
+        rows = slice(b * queries, (b + 1) * queries)
+        for h in range(c.heads * c.group):
+            want, mag = attention(q[rows, h], kv[:, 0, h // c.group], kv[:, 1, h // c.group],
+                                  c.dim ** -0.5, True)
+            assert (np.abs(y[rows, h] - want) <= mag * 2.0 ** -7 + 1e-30).all(), (lens, b, h)
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("queries", [1, 40])
+def test_graph_of_a_step_with_divided_keys(fmt, queries):
+    """One captured call whose keys are divided among workgroups, replayed with lengths that grow
+    past shares' ends, shrink and vanish; every replay as the eager call, over a workspace of NaN."""
+    lens0 = [3000, 700, 150]
+    c = Case(fmt, 128, 2, 4, 64, [queries] * 3, lens0, seed=41)
+    table, lens, q = c.table.cuda(), c.kv_lens.clone(), c.q.cuda()
+    bound = c.table.shape[1] * 64
+    n = w8a8.load_library().w8a8_kv_attention_workspace_bytes(
+        64, 2, 128, w8a8.KV_FORMATS[fmt], 4, 3 * queries, 3, queries, bound)
+    assert n > 0
+    work = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+
+    def step(o=None, w=None):
+        return w8a8.kv_attention(q, c.cache, table, lens, fmt=fmt, out=o, workspace=w)
+
+    step(out, work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, work)
+    for now in (lens0, [130, 0, 1], [256, 257, 150], [2999, 700, 127], [1025, 513, 0], [0, 0, 0],
+                [3000, 1, 129]):
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        work.fill_(0xFF)
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(got, step())
+        _expect(c, now, got, queries)
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("qs,kvs,nan_at", [([1], [5000], 4990), ([1], [5000], 100),
+                                           ([150], [6000], 5900), ([150], [6000], 640)])
+def test_nan_tokens_where_keys_are_divided(fmt, qs, kvs, nan_at):
+    lib = w8a8.load_library()
+    for part in (0, 1):
+        c = Case(fmt, 128, 1, 2, 16, qs, kvs, seed=43)
+        assert lib.w8a8_kv_attention_workspace_bytes(16, 1, 128, w8a8.KV_FORMATS[fmt], 2, qs[0], 1,
+                                                     qs[0], kvs[0]) > 0
+        kv = _kv(kvs[0], 1, 128, 44)
+        kv[nan_at, part, 0, 70] = float("nan")
+        c.write(kv, _slots(c))
+        y = f64(c.run(max_q=qs[0], max_kv=kvs[0]))
+        sees = np.array([kvs[0] - qs[0] + i >= nan_at for i in range(qs[0])])
+        bad = np.zeros(y.shape, bool)
+        bad[sees] = True
+        if part == 1:                      # a value's block, not the others of its token
+            bad[:, :, :64], bad[:, :, 96:] = False, False
+        assert np.array_equal(np.isnan(y), bad)

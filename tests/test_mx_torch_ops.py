@@ -162,3 +162,34 @@ def test_example_is_made_of_the_operators(fmt):
                                       True)
                 assert (np.abs(got[at:at + n, h] - want) <= mag * 2.0 ** -7 + 1e-30).all()
             at += n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+def test_cache_ops_under_compile(fmt):
+    """A step that writes to the cache and attends over it, compiled whole: the cache is mutated
+    where it is read afterwards, bit for bit as in the eager step."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    o = torch.ops.w8a8
+    table = torch.tensor([[2, 0], [1, 3]], dtype=torch.int32, device="cuda")
+    g = torch.Generator().manual_seed(5)
+
+    def step(cache, qkv, slots, lens):
+        q, k, v = qkv.split((4, 2, 2), 1)
+        o.kv_write(cache, k, v, slots, fmt)
+        y = o.kv_attention(q, cache, table, lens, None, fmt, None, True, 1, 32)
+        rk, rv = o.kv_read(cache, slots, 64, fmt)
+        return y + 1.0, rk - rv
+
+    caches = [w8a8.kv_cache(4, 2, 64, 16, fmt=fmt) for _ in range(2)]
+    compiled = torch.compile(step, fullgraph=True, backend="aot_eager")
+    for pos in range(18):
+        qkv = torch.randn(2, 8, 64, generator=g).to(torch.bfloat16).cuda()
+        slots = torch.tensor([[2, 0], [1, 3]], device="cuda")[:, pos // 16] * 16 + pos % 16
+        lens = torch.full((2,), pos + 1, dtype=torch.int32, device="cuda")
+        want = step(caches[0], qkv, slots, lens)
+        got = compiled(caches[1], qkv, slots, lens)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert torch.equal(*caches)
+    assert caches[0].any()
