@@ -12,8 +12,9 @@
 // holds one row, so maxima, sums and the rescaling of O stay inside a lane but for one
 // exchange of the maximum between the lanes that share a row, and the weights P^T come out of
 // S^T in the layout the second product takes them in. Codes decode to bf16 exactly; the
-// weights are rounded for the second product: to two bf16 terms (2^-16 of each at most), or to one
-// (2^-8) in the tile kernel for sequences of more than kTwoTermRows rows, whose products bind.
+// weights are rounded for the second product: to two bf16 terms (2^-16 of each at most) in sequences
+// of few rows, to one (2^-8) in those of many, whose products bind. Each sequence gets the kernel
+// for its own rows, so that its rounding does not hang on the batch or on the caller's bounds.
 #include "../../include/w8a8.h"
 #include "mx_internal.hpp"
 #include "mx_math.hpp"
@@ -37,10 +38,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // 128), or what the lengths make of `target` if that is more, or what divides a sequence's tokens
 // among `splits` workgroups, the most that a head and row tile of it can have, if that is more.
 struct Split {
+    int rows_from, rows_to;   // sequences of this many rows (queries x group) are this kernel's
     int share, splits;
     int target;      // workgroups that the tokens of all sequences are spread over, 0: share holds
-    float *part;     // splits > 1: [splits][T * q heads][dim + 4]: O, m, l; in split 0 the
-                     // number of splits the row has (1: its output is written already)
+    float *part;     // joined: [splits][T * q heads][dim + 4]: O, m, l; in split 0 the number
+                     // of splits the row has (1: its output is written already)
+    bool joined;     // a launch that joins partial results follows
     uint64_t magic;  // n / (page / 16) = n * magic >> 32 for n < 2^22 (kMaxTokens / 16)
 };
 
@@ -49,10 +52,6 @@ struct Split {
 // float32 sums and bf16 roundings are relative; a rescaling costs as much as a product. 4 x 1000
 // queries on 6000 keys, 18 heads of 256: 783 us rescaling at every rise, 670 so.
 constexpr float kSlack = 8.0f;
-// Sequences of up to this many rows (queries x heads that share a key/value head) have their
-// weights in two bf16 terms whatever runs, so that a query's rounding depends on its own sequence
-// only, not on the batch or the bounds that the launch is laid out for.
-constexpr int kTwoTermRows = 64;
 constexpr int kMaxChunk = 4096;
 constexpr int kSplitRows = 16, kTileRows = 128, kTileTokens = 64;
 static_assert(W8A8_KV_MAX_TOKENS / 16 <= 1 << 22 && W8A8_KV_MAX_PAGE / 16 <= 1 << 10, "magic");
@@ -80,6 +79,10 @@ __device__ __forceinline__ int seen(const Seq &s, int i, int causal) {
     return max(0, causal ? min(s.kv, s.kv - s.lq + i + 1) : s.kv);
 }
 
+__device__ __forceinline__ bool mine(const Split &sp, int rows) {
+    return rows >= sp.rows_from && rows <= sp.rows_to;
+}
+
 // The share for this call's lengths: their tokens (once a head and row tile) spread evenly,
 // whatever each sequence has of them. A wavefront sums them by itself, in the same order in
 // every workgroup.
@@ -89,7 +92,8 @@ __device__ __forceinline__ int share_of(const KvShape &c, const KvAttnArgs &a, c
     float sum = 0.0f;
     for (int i = threadIdx.x & 63; i < a.seqs; i += 64) {
         const Seq s = sequence(c, a, i);
-        sum += (float)max(s.kv, 0) * (float)((max(s.lq, 0) * a.group + rows - 1) / rows);
+        if (mine(sp, s.lq * a.group))
+            sum += (float)max(s.kv, 0) * (float)((s.lq * a.group + rows - 1) / rows);
     }
 #pragma unroll
     for (int d = 32; d > 0; d /= 2)
@@ -229,10 +233,10 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
     const int pair = blockIdx.x - split * pairs;
     const int b = __builtin_amdgcn_readfirstlane(pair / c.heads), head = pair - b * c.heads;
     const Seq seq = sequence(c, a, b);
-    if (split > 0 && (int64_t)split * sp.share >= seq.kv)
+    const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
+    if (!mine(sp, rows) || (split > 0 && (int64_t)split * sp.share >= seq.kv))
         return;                            // shares are this long or longer
     const int even = share_of(c, a, sp, kSplitRows);
-    const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
     const int64_t v_offset = c.heads * c.head_bytes();     // from a page's keys to its values
     const int scales_at = c.page * CB;                     // from codes to scales
     uint8_t *const vt = lds[wave];
@@ -501,7 +505,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                     p[D + 1] = all_l[r];
                 }
             }
-            if (d == 0 && split == 0 && sp.splits > 1)
+            if (d == 0 && split == 0 && sp.joined)
                 sp.part[out_row * (D + 4) + D + 2] = (float)used;
         }
         __syncthreads();           // the next row tile writes the same LDS
@@ -576,15 +580,15 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     const int split = __builtin_amdgcn_readfirstlane(unit / pairs), pair = unit - split * pairs;
     const int b = __builtin_amdgcn_readfirstlane(pair / c.heads), head = pair - b * c.heads;
     const Seq seq = sequence(c, a, b);
-    if (split > 0 && (int64_t)split * sp.share >= seq.kv)
+    const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
+    if (!mine(sp, rows) || (split > 0 && (int64_t)split * sp.share >= seq.kv))
         return;                            // shares are this long or longer
     const int even = share_of(c, a, sp, kTileRows);
-    const int rows = seq.lq * a.group, q_heads = c.heads * a.group;
     const int64_t v_offset = c.heads * c.head_bytes();
 
     const int first_rt = tiles - 1 - in;
     const int last_rt = (rows + kTileRows - 1) / kTileRows - 1;
-    // Row tiles first_rt, first_rt + tiles, ...: more than one only where max_q was too small.
+    // Row tiles first_rt, first_rt + tiles, ...: more than one only where the grid has fewer.
     for (int rt = first_rt; rt <= last_rt; rt += tiles) {
         const int some_see =
             seen(seq, (min(rt * kTileRows + kTileRows, rows) - 1) / a.group, a.causal);   // some row
@@ -599,7 +603,6 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
         const int qh = head * a.group + (live ? row - qi * a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
         const int all_see = seen(seq, rt * kTileRows / a.group, a.causal);
-        const bool two_terms = rows <= kTwoTermRows;
         // what some row of this wavefront sees
         const int wave_first = rt * kTileRows + wave * 32;
         const int wave_sees =
@@ -771,10 +774,6 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                 const uint8_t *vp = values[st] + (4 * h + ((lane & 15) >> 2)) * RSV +
                                     ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
                 u32x2 fv[2][2];
-                const auto value_of = [&](int z) __attribute__((always_inline)) {
-                    return __builtin_bit_cast(bf16x8, u32x4{fv[z & 1][0][0], fv[z & 1][0][1],
-                                                            fv[z & 1][1][0], fv[z & 1][1][1]});
-                };
                 const auto read_values = [&](int z) __attribute__((always_inline)) {
                     const uint8_t *src = vp + 16 * (z / F) * RSV + z % F * 64;
                     fv[z & 1][0] = __builtin_bit_cast(
@@ -782,35 +781,6 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                     fv[z & 1][1] = __builtin_bit_cast(
                         u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(src + 8 * RSV)));
                 };
-                if (two_terms) {
-                    // The second terms, weights computed again: code of its own in front of the
-                    // products below leaves those as they are for many rows.
-                    float own_base = base;
-                    asm volatile("" : "+v"(own_base));
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        u32x4 rest;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int w = 4 * u + i;
-                            const float x = __builtin_amdgcn_exp2f(
-                                __builtin_fmaf(s[w / 8][w % 8 * 2], a.scale, -own_base));
-                            const float y = __builtin_amdgcn_exp2f(
-                                __builtin_fmaf(s[w / 8][w % 8 * 2 + 1], a.scale, -own_base));
-                            const uint32_t r = pack_bf16(x, y);
-                            rest[i] = pack_bf16(x - __uint_as_float(r << 16),
-                                                y - __uint_as_float(r & 0xFFFF0000u));
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                        for (int f = 0; f < F; ++f) {
-                            read_values(u * F + f);
-                            o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                value_of(u * F + f), __builtin_bit_cast(bf16x8, rest), o[f], 0, 0, 0);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
-                    }
-                }
                 u32x4 p[4];
                 const auto weight = [&](auto qc) __attribute__((always_inline)) {
                     constexpr int w = decltype(qc)::value;     // of 16 pairs
@@ -843,7 +813,9 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                         static_assert(2 * NU <= 4 * F, "loads between the products");
                         __builtin_amdgcn_sched_barrier(0);
                         o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            value_of(z), __builtin_bit_cast(bf16x8, p[u]), o[f], 0, 0, 0);
+                            __builtin_bit_cast(bf16x8, u32x4{fv[z & 1][0][0], fv[z & 1][0][1],
+                                                             fv[z & 1][1][0], fv[z & 1][1][1]}),
+                            __builtin_bit_cast(bf16x8, p[u]), o[f], 0, 0, 0);
                         __builtin_amdgcn_sched_barrier(0);
                     }(), ...);
                 }(std::make_integer_sequence<int, 4 * F>{});
@@ -876,7 +848,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
             part[D] = m;
             part[D + 1] = l;
         }
-        if (split == 0 && sp.splits > 1 && h == 0)
+        if (split == 0 && sp.joined && h == 0)
             part[D + 2] = (float)used;
     }
 }
@@ -948,31 +920,49 @@ kv_attention_join_kernel(const float *part, int splits, int64_t rows, uint16_t *
 }
 
 template <int D, int LANES, int WAYS>
-hipError_t launch_join(const Split &sp, int64_t rows, uint16_t *out, hipStream_t s) {
+hipError_t launch_join(const float *part, int splits, int64_t rows, uint16_t *out, hipStream_t s) {
     constexpr int jobs = 256 / (LANES * WAYS), pieces = D / (4 * LANES);
     const int64_t blocks = (rows * pieces + jobs - 1) / jobs;
     if (!launchable(blocks, 256))
         return hipErrorInvalidValue;
     hipLaunchKernelGGL((kv_attention_join_kernel<D, LANES, WAYS>), dim3((unsigned)blocks), dim3(256), 0, s,
-                       sp.part, sp.splits, rows, out);
+                       part, splits, rows, out);
     return hipGetLastError();
 }
 
-// Whether the tile kernel runs: it decodes keys and values once for 128 rows, the other one once
-// for 16, where 4-bit codes are fewer bytes to read again. Both have two terms up to kTwoTermRows.
-// Time of the other one by its time, 348 shapes of 20 to 64 rows of a sequence and head, e4m3 and
-// e2m1: 20 and 32 rows 0.73, 0.61; 40 and 48 0.83, 0.69; 56 and 64 0.91, 0.77, and of those that
-// take 60 us or more 1.12, 0.82 (32 x 8 heads of 128, 16000 keys, 56 rows: e4m3 by the tile kernel
-// 379 us, e2m1 by it 376 and by the other one 345).
-bool many_rows(const KvShape &c, int group, int max_q) {
-    return (int64_t)max_q * group > (c.fmt == KV_FP8 ? 48 : 64);
+// Up to this many rows of a sequence are few: the split kernel's, whose weights have two terms. The
+// tile kernel decodes keys and values once for 128 rows, that one once for 16. Its time by the
+// tile kernel's, 1800 random shapes of a sequence and head, e4m3 and e2m1: 17 to 32 rows 0.86,
+// 0.75; 33 to 48 0.96, 0.82; 49 to 64 1.04, 0.94. Where heads and sequences alone fill the card its
+// instructions bind and the tile kernel, with its one term, would be faster from 33 rows on (32 x
+// 8 heads of 128, 16000 keys: e4m3, 48 rows 493 and 270 us, 56 rows 671 and 270; e2m1, 56 rows
+// 342 and 243); a query's rounding is not to hang on the batch that it comes in.
+constexpr int kFewRows = 64;
+
+// Most rows of a sequence that each kernel gets, 0: not launched. Where sequences may be of both
+// kinds both run, one after the other, and each takes those of its own. 8 heads of 128, 4 queries a
+// head, 100 queries on 4000 keys with 63 sequences of one on up to 8000: 202 us, all by the tile
+// kernel 441; 2000 with 15 of one 158 and 278. The one without sequences takes 1 to 2 us where the
+// call is small and 12 at 4 x 1000 queries of 18 heads of 256 (660).
+struct Rows {
+    int64_t few, many;
+};
+
+Rows rows_of(int64_t T, int seqs, int group, int max_q) {
+    const int64_t rows = (seqs == 1 ? T : std::min<int64_t>(max_q, T)) * group;
+    if (rows <= kFewRows)
+        return {rows, 0};
+    return {seqs == 1 || (int64_t)max_q * seqs == T ? 0 : kFewRows, rows};
 }
 
 // Up to here one workgroup takes all keys: a second launch costs as much. us divided and whole, 8
 // heads of 128, 4 queries a head: 300 keys 9.7, 8.6; 500 9.8, 9.8; 700 10.0, 11.9.
 constexpr int kWholeTokens = 512;
-// Workgroups of a launch of many rows: more than this many with work in them gain nothing.
-constexpr int64_t kMostGroups = 1 << 20;
+// Workgroups of a launch of many rows. Most are empty where max_q is loose or one sequence long,
+// and an empty one still takes its turn; too few, and a long sequence's row tiles queue up. us with
+// 2^16, 2^18 and 2^20, 8 heads of 128, 4 queries a head: 64 x 1000 queries, max_q left out 820, 1004,
+// 1772 (809 with it); 4000 queries beside 2000 sequences of one 1622, 608, 1340.
+constexpr int64_t kMostGroups = 1 << 18;
 // Sequences whose lengths a wavefront sums, 64 at a time, at the start of every workgroup.
 constexpr int kSummed = 512;
 
@@ -986,14 +976,15 @@ constexpr int kSummed = 512;
 // 8 times 98; many rows, in whose launches empty and small workgroups cost more, take as long
 // with 2 and with 4 times on average, and 216 row tiles of 256 wide heads had better stay whole
 // (227 us, in two parts 250).
-Split split_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
-    const bool many = many_rows(c, group, max_q);
+Split split_of(const KvShape &c, int64_t T, int seqs, int group, bool many, const Rows &of, int max_kv) {
     const int tile_rows = many ? kTileRows : kSplitRows;
-    // Row tiles: of max_q queries each, and no more than T queries in all make.
-    const int64_t tiles = std::min(seqs * (((int64_t)max_q * group + tile_rows - 1) / tile_rows),
+    // Row tiles: of the most rows of a sequence, and no more than T queries in all make.
+    const int64_t tiles = std::min(seqs * (((many ? of.many : of.few) + tile_rows - 1) / tile_rows),
                                    T * group / tile_rows + seqs);
     const int64_t blocks = c.heads * tiles;
     Split sp;
+    sp.rows_from = many && of.few > 0 ? (int)of.few + 1 : 0;
+    sp.rows_to = many || of.many == 0 ? INT32_MAX : (int)of.few;
     const int64_t target = many ? (c.dim <= 128 ? 384 : 256) : 512;
     const int64_t most = target * (seqs == 1 ? 2 : many ? 3 : 16) / 2 / blocks;
     const int64_t least = blocks <= 16 ? 256 : blocks < 512 ? 512 : 1024;
@@ -1004,47 +995,84 @@ Split split_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int 
     const uint32_t pb = (uint32_t)c.page / 16;
     sp.magic = (((uint64_t)1 << 32) + pb - 1) / pb;
     sp.part = nullptr;
+    sp.joined = false;
     return sp;
+}
+
+// The launches of a call.
+struct Plan {
+    Rows rows;
+    Split few, many;
+    int splits;      // the most of them; 1: nothing to join
+};
+
+Plan plan_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
+    Plan p;
+    p.rows = rows_of(T, seqs, group, max_q);
+    p.splits = 1;
+    if (p.rows.few > 0) {
+        p.few = split_of(c, T, seqs, group, false, p.rows, max_kv);
+        p.splits = p.few.splits;
+    }
+    if (p.rows.many > 0) {
+        p.many = split_of(c, T, seqs, group, true, p.rows, max_kv);
+        p.splits = std::max(p.splits, p.many.splits);
+    }
+    return p;
+}
+
+template <int FMT, int D>
+hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, hipStream_t s) {
+    const int64_t rows = a.T * c.heads * a.group;
+    const auto run = [&](bool many, Split &sp, int64_t most_rows) {
+        sp.part = ws;
+        sp.joined = p.splits > 1;
+        const int64_t units = (int64_t)c.heads * a.seqs * sp.splits;
+        if (!many) {
+            if (!launchable(units, 256))
+                return hipErrorInvalidValue;
+            const dim3 grid((unsigned)units, (unsigned)((most_rows + kSplitRows - 1) / kSplitRows));
+            hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D>), grid, dim3(256), 0, s, c, a, sp);
+            return hipGetLastError();
+        }
+        // A workgroup goes on to every tiles-th row tile, so that a loose max_q costs empty
+        // workgroups but never more than kMostGroups of them.
+        const int64_t columns = units >= kSpreadUnits ? (units + 7) / 8 * 8 : units;
+        const int64_t tiles = std::min((most_rows + kTileRows - 1) / kTileRows,
+                                       std::max<int64_t>(kMostGroups / columns, 1));
+        if (!launchable(columns * tiles, 256))
+            return hipErrorInvalidValue;
+        hipLaunchKernelGGL((kv_attention_tile_kernel<FMT, D>), dim3((unsigned)(columns * tiles)),
+                           dim3(256), 0, s, c, a, sp, (int)tiles);
+        return hipGetLastError();
+    };
+    hipError_t e = hipSuccess;
+    if (p.rows.few > 0)
+        e = run(false, p.few, p.rows.few);
+    if (e == hipSuccess && p.rows.many > 0)
+        e = run(true, p.many, p.rows.many);
+    if (e != hipSuccess || p.splits == 1)
+        return e;
+    // Few splits: a row by D / 4 lanes. Many: 32 outputs of a row by 32 groups of 8 lanes.
+    return p.splits <= 16 || rows * (D / 4) >= 65536
+               ? launch_join<D, D / 4, 1>(ws, p.splits, rows, a.out, s)
+               : launch_join<D, 8, 32>(ws, p.splits, rows, a.out, s);
 }
 
 }  // namespace
 
 size_t kv_attention_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_q,
                                     int max_kv) {
-    const Split sp = split_of(c, T, seqs, group, max_q, max_kv);
-    return sp.splits == 1 ? 0 : (size_t)sp.splits * T * c.heads * group * (c.dim + 4) * 4;
+    const Plan p = plan_of(c, T, seqs, group, max_q, max_kv);
+    return p.splits == 1 ? 0 : (size_t)p.splits * T * c.heads * group * (c.dim + 4) * 4;
 }
 
 hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
-    Split sp = split_of(c, a.T, a.seqs, a.group, a.max_q, a.max_kv);
-    sp.part = static_cast<float *>(ws);
-    const bool many = many_rows(c, a.group, a.max_q);
-    const int tile_rows = many ? kTileRows : kSplitRows;
-    const int64_t pairs = (int64_t)c.heads * a.seqs, rows = a.T * c.heads * a.group;
-    const int64_t units = pairs * sp.splits;
-    const int64_t columns = many && units >= kSpreadUnits ? (units + 7) / 8 * 8 : units;
-    // A workgroup goes on to every tiles-th row tile, so that a loose max_q costs empty workgroups
-    // but never more than kMostGroups of them.
-    int64_t tiles = (std::min<int64_t>(a.max_q, a.T) * a.group + tile_rows - 1) / tile_rows;
-    if (many)
-        tiles = std::min(tiles, std::max<int64_t>(kMostGroups / columns, 1));
-    const int64_t blocks = many ? columns * tiles : units;
-    if (!launchable(blocks, 256) || rows > 0x7FFFFFFF)
+    if (a.T * c.heads * a.group > INT32_MAX)
         return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks, many ? 1u : (unsigned)tiles);
+    Plan p = plan_of(c, a.T, a.seqs, a.group, a.max_q, a.max_kv);
     const auto run = [&](auto dim, auto format) {
-        constexpr int D = decltype(dim)::value, FMT = decltype(format)::value;
-        if (many)
-            hipLaunchKernelGGL((kv_attention_tile_kernel<FMT, D>), grid, dim3(256), 0, s, c, a, sp,
-                               (int)tiles);
-        else
-            hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D>), grid, dim3(256), 0, s, c, a, sp);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || sp.splits == 1)
-            return e;
-        // Few splits: a row by D / 4 lanes. Many: 32 outputs of a row by 32 groups of 8 lanes.
-        return sp.splits <= 16 || rows * (D / 4) >= 65536 ? launch_join<D, D / 4, 1>(sp, rows, a.out, s)
-                               : launch_join<D, 8, 32>(sp, rows, a.out, s);
+        return run_plan<decltype(format)::value, decltype(dim)::value>(c, a, p, static_cast<float *>(ws), s);
     };
     const auto go = [&](auto dim) {
         return c.fmt == KV_FP8 ? run(dim, std::integral_constant<int, KV_FP8>{})

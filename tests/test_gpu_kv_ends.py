@@ -159,6 +159,8 @@ TWO_TERMS = [
     (192, 8, 1, 16, [64] * 2, [80, 700]),
     (128, 2, 4, 16, [1] * 48, [40] * 48),           # one token each, of a batch
     (64, 4, 1, 16, [33, 64, 1], [50, 64, 3]),
+    (128, 2, 4, 16, [1, 200, 12, 13, 3], [700, 300, 41, 70, 5000]),     # prompts among them
+    (64, 16, 4, 16, [12, 1] * 6 + [60], [700, 5000] * 6 + [100]),
 ]
 
 
@@ -169,8 +171,11 @@ def test_weights_of_few_rows_in_two_terms(fmt, case):
     dim, heads, group, page, qs, kvs = TWO_TERMS[case]
     say(f"two terms {fmt} {TWO_TERMS[case]}")
     c = Cancelling(fmt, dim, heads, group, page, qs, kvs, seed=case)
+    few = [b for b, n in enumerate(qs) if n * group <= 64]
     for hints in ({}, dict(max_q=max(qs), max_kv=max(kvs)), dict(max_q=1000), dict(max_q=1)):
-        c.check_two_terms(c.run(scale=1.0 / dim, **hints))
+        y = c.run(scale=1.0 / dim, **hints)
+        c.check_two_terms(y, only=few)
+        c.check(y, scale=1.0 / dim)
 
 
 @pytest.mark.parametrize("fmt", ["fp8", "fp4"])
