@@ -367,7 +367,9 @@ w8a8_status w8a8_kv_read(const uint8_t *cache, int64_t pages, int page, int head
  * lq * group <= 64, whatever else the call holds; in others one term (2^-8) may be all.
  * max_q and max_kv are bounds on a sequence's queries and tokens that the launch is laid out
  * for; with other values the results are the same but for such rounding (table_pages * page
- * bounds the tokens; it is at most W8A8_KV_MAX_TOKENS, else W8A8_ERR_SHAPE).
+ * bounds the tokens; it is at most W8A8_KV_MAX_TOKENS, else W8A8_ERR_SHAPE). Tight bounds are
+ * faster: a loose max_q launches workgroups without work, a loose max_kv divides one sequence
+ * into fewer parts.
  * Table entries that are read have to lie inside the cache: others read some page of it.
  * workspace: w8a8_kv_attention_workspace_bytes(...) bytes, 256-byte aligned. */
 w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head,

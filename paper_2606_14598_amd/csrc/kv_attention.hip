@@ -527,8 +527,10 @@ __device__ __forceinline__ u32x2 both_halves(float v) {
 
 // Many rows (128 a workgroup, 32 a wavefront): 64 tokens at a time are decoded once into LDS
 // for all four wavefronts, between the products of the 64 before; 32x32x16 products with the
-// rows as columns, as above. Keys lie in rows of 2 D + 16 bytes, values in rows of 2 D + 64:
-// the fragment reads (32 keys x 16 bytes; 4 values x 64 bytes) then use every bank alike.
+// rows as columns, as above. Keys lie in rows of 2 D + 16 bytes, values in rows of 2 D + 64, which
+// spreads the fragment reads (32 keys x 16 bytes; 4 values x 64 bytes) over the banks. Still a
+// quarter of the LDS cycles at heads of 256 are conflicts, by the counters: the likely ones are the
+// staging's 16-byte stores, whose neighbouring lanes write 32 bytes apart.
 //
 // Bound by instructions: per row and 64 tokens 64 exponentials and some 350 other vector
 // instructions a wavefront beside 64 (heads of 256) or 32 (128) products, two wavefronts a SIMD

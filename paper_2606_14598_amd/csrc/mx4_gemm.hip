@@ -10,8 +10,9 @@
 //
 // Many tokens: bound by the matrix cores at the clock that their power leaves (1.6 GHz on
 // random codes, 6.4 PFLOP/s from registers; 2.3 GHz and 9.1 on zeros) and by waits for panels.
-// 4608 x 4096 x 16384 runs at 3.8 PFLOP/s, 4608 x 16384 x 4096 in one round of tiles at 4.5. Few
-// tokens: bound by reading W; 1 x 4096 x 16384 takes 9.8 us (3.7 TB/s) with its quantizer.
+// 4608 x 4096 x 16384 takes 156 to 166 us on different cards (3.7 to 4.0 PFLOP/s), 4608 x 16384 x
+// 4096 in one round of tiles 138 (4.5). Few tokens: bound by reading W; 1 x 4096 x 16384 takes 10 us
+// (3.6 TB/s) with its quantizer.
 #include "../../include/w8a8.h"
 #include "mx_internal.hpp"
 #include "mx_quant.hpp"
@@ -43,8 +44,10 @@ __device__ __forceinline__ i32x8 frag(i32x4 v) {
     return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
 }
 
-// XOR of the 16-byte chunk index inside an LDS row of 128 bytes: conflict-free both for the
-// direct-to-LDS writes (8 rows of 8 chunks) and for the fragment reads (32 rows, one chunk).
+// XOR of the 16-byte chunk index inside an LDS row of 128 bytes: spreads the direct-to-LDS writes
+// (8 rows of 8 chunks) and the fragment reads (32 rows, one chunk) over the banks. Not all the way:
+// 15% of the LDS cycles of 4608 x 4096 x 16384 are bank conflicts, by the counters; which accesses
+// have them they do not tell.
 __device__ __forceinline__ int swz(int row) { return (row & 7) ^ ((row >> 3) & 3); }
 
 __host__ __device__ constexpr int waitcnt_vm(int n) {
@@ -91,7 +94,7 @@ __device__ __forceinline__ void tile_of(int bid, const Mx4Params &p, int &tm, in
 // Eight to twelve wavefronts on the large tiles: a product's operands are two LDS reads, and
 // with one wavefront a SIMD their latencies show. 256 x 256 by four, whose fragments were read a
 // step ahead across four stages of half panels, took 214 us at 4608 x 4096 x 16384 (288 x 256
-// by twelve: 160) and 258 at 4608 x 16384 x 4096 (138).
+// by twelve on the same card: 160) and 258 at 4608 x 16384 x 4096 (138).
 template <int TM, int TN, int WM, int WN, int S>
 __global__ void __launch_bounds__(WM *WN * 64)
 mx4_gemm_kernel(Mx4Params p) {

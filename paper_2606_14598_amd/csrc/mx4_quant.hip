@@ -7,9 +7,11 @@
 // that the product reads a tile's scales of one K-panel as one piece of memory.
 //
 // Bound by memory: 2 bytes read and 17/32 written per element. 4608 x 4096 with a multiplier
-// takes 10.1 us (4.7 TB/s; 13.9 before all of a wavefront's rows were loaded at once), 4608 x
-// 16384 with GELU and a multiplier 50.9 us (3.8 TB/s: the table's LDS reads; 75 with GELU
-// evaluated), and that matrix decoded again 27.9 us (6.8 TB/s, the codes still in the cache).
+// takes 10.3 us (4.6 TB/s; 13.9 before all of a wavefront's rows were loaded at once). 4608 x 16384
+// on matrices in turn takes 33 us (5.7 TB/s), 41 with GELU (its table's LDS reads), and 51 right
+// behind the 151 MB that its decoder has written (75 with GELU evaluated); on one matrix again
+// and again, which then comes from the last cache, 29 and 39. That matrix decoded again 27.9 us
+// (6.8 TB/s, the codes still in the cache).
 #include "mx_internal.hpp"
 #include "mx_quant.hpp"
 
@@ -110,9 +112,9 @@ hipError_t launch_mx4_quant(const uint16_t *x, int64_t R, int64_t K, int act,
         return hipSuccess;
     const int64_t chunks = (K + 511) / 512;
     // Eight rows a wavefront where that leaves 4096 wavefronts, 16 a CU; else a row each, as a
-    // short call's time is one row's latency. us by one and by eight, calls in a graph: 64 x 256
-    // 2.4, 5.0; 1024 x 4096 with GELU and multiplier 4.7, 5.9; 2048 x 4096 4.5, 4.3; 1152 x 16384
-    // and 4608 x 16384 with both 16.0, 15.2 and 52.7, 40.1.
+    // short call's time is one row's latency. us by one and by eight, calls on one input in a
+    // graph: 64 x 256 2.4, 5.0; 1024 x 4096 with GELU and multiplier 4.7, 5.9; 2048 x 4096 4.5,
+    // 4.3; 1152 x 16384 and 4608 x 16384 with both 16.0, 15.2 and 52.7, 40.1.
     const int rows = R * chunks >= 8 * 4096 ? 8 : 1;
     const int64_t blocks = chunks * ((R + kWaves * rows - 1) / (kWaves * rows));
     if (!launchable(blocks, kWaves * 64))

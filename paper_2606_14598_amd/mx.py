@@ -222,8 +222,12 @@ def kv_attention(q, cache, block_table, kv_lens, *, fmt: str = "fp8", q_starts=N
     sees the tokens j <= kv_len - lq + i (causal) or all kv_len; a query that sees none gives
     zeros. Query head h reads head h // (q heads / heads) of the cache. scale: of the scores,
     1 / sqrt(head_dim) by default. max_q, max_kv: bounds on a sequence's queries and tokens for
-    laying out the launch, known to the caller on the host (by default T and the table's
-    width); the results do not depend on them."""
+    laying out the launch, known to the caller on the host (by default T, or T / B without
+    q_starts, and the table's width); the results do not depend on them beyond the rounding of
+    the weights, and that not in sequences of up to 64 rows (queries x query heads that share
+    a head of the cache), which always keep two bf16 terms. Tight bounds are faster: 64 prompts of
+    1000 tokens take 0.8 ms with max_q and 1.0 without; one sequence of 2000 tokens, one query,
+    16 us with max_kv and 24 by a table of 131072 tokens (8 heads of 128, 4 queries a head)."""
     device = cache.device
     _check_heads(q, "q", device)
     T, q_heads, dim = q.shape
