@@ -250,6 +250,7 @@ def kv_attention(q, cache, block_table, kv_lens, *, fmt: str = "fp8", q_starts=N
         raise ValueError(f"{q_heads} query heads do not divide among {heads}")
     if max_q is None:
         max_q = T if q_starts is not None else T // max(B, 1)
+    max_q = min(int(max_q), T)
     width = block_table.shape[1]
     max_kv = width * page if max_kv is None else min(int(max_kv), width * page)
     if out is not None:
@@ -260,11 +261,11 @@ def kv_attention(q, cache, block_table, kv_lens, *, fmt: str = "fp8", q_starts=N
         return y
     group = q_heads // heads
     nws = _bytes("w8a8_kv_attention_workspace_bytes", page, heads, dim, f, group, T, B,
-                max(1, int(max_q)), max_kv)
+                max_q, max_kv)
     ws = _workspace(nws, device, workspace)
     _launch(device, "w8a8_kv_attention", _ptr(q), q.stride(0), q.stride(1), _ptr(cache), pages,
             page, heads, dim, f, _ptr(block_table), block_table.stride(0), width, _ptr(kv_lens),
             _ptr(q_starts), T, B, group, dim ** -0.5 if scale is None else float(scale),
-            int(bool(causal)), int(max_q), max_kv, _ptr(y), _ptr(ws),
+            int(bool(causal)), max_q, max_kv, _ptr(y), _ptr(ws),
             0 if ws is None else ws.nbytes)
     return y

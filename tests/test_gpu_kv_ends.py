@@ -40,6 +40,17 @@ def test_many_sequences_without_bounds():
     assert torch.equal(w8a8.kv_attention(q, cache, table, lens, q_starts=starts, max_q=1), want)
 
 
+def test_bounds_beyond_an_int():
+    """Bounds that stand for none, past what the C ABI's ints hold; a negative one is refused."""
+    c = Case("fp8", 64, 1, 2, 16, [3, 70], [40, 700], seed=28)
+    want = c.run()
+    for none in ((1 << 31) - 1, 1 << 31, (1 << 32) + 1, 1 << 62):
+        assert torch.equal(c.run(max_q=none, max_kv=none), want)
+    for bad in (dict(max_q=-1), dict(max_kv=-1)):
+        with pytest.raises(w8a8.W8A8Error):
+            c.run(**bad)
+
+
 @pytest.mark.parametrize("fmt", ["fp8", "fp4"])
 def test_more_tokens_than_a_grid_holds(fmt):
     """2^26 + 5 tokens in one call, padding but for the first two and the last three."""
