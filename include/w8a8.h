@@ -382,6 +382,84 @@ w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head
 size_t w8a8_kv_attention_workspace_bytes(int page, int heads, int dim, int fmt, int group,
                                          int64_t T, int seqs, int max_q, int max_kv);
 
+/* Attention of trees: as w8a8_kv_attention, for drafted tokens that continue a sequence in
+ * several ways. The last lq cached tokens of a sequence are its queries' own, in the queries'
+ * order (the nodes of the tree); query i sees every token in front of them, and node n where
+ * bit n % 64 of tree[(q_starts[b] + i) * tree_words + n / 64] is set (tree [T, tree_words]; a
+ * node sees its ancestors and itself; nodes past 64 * tree_words are seen by none, bits past lq
+ * are ignored). tree_words is 1 to W8A8_KV_MAX_TREE_WORDS (else W8A8_ERR_ARG). The workspace is
+ * that of w8a8_kv_attention, and so is everything else. */
+#define W8A8_KV_MAX_TREE_WORDS 64
+w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
+                                   const uint8_t *cache, int64_t pages, int page, int heads,
+                                   int dim, int fmt, const int32_t *table, int64_t table_stride,
+                                   int table_pages, const int32_t *kv_lens,
+                                   const int32_t *q_starts, int64_t T, int seqs, int group,
+                                   float scale, const int64_t *tree, int tree_words, int max_q,
+                                   int max_kv, uint16_t *out, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+
+/* w8a8_kv_write with rotary positions, for the keys and the queries beside them. A head's
+ * channels have `pairs` pairs (at most dim / 2): channels p and p + pairs, or 2p and 2p + 1 where
+ * interleaved is 1; channels from 2 * pairs on are left as they are. Pair p of token t is turned by
+ * angle positions[t * axes + n] * inv_freq[p], with n the pair's axis: sections[n] pairs one after
+ * the other belong to axis n (sections [axes] on the HOST, of sum `pairs`; not read with one axis;
+ * axes is 1 to W8A8_ROPE_MAX_AXES):
+ *   (a, b) -> (a c - b s, b c + a s), float32, every operation rounded, with c and s the angle's
+ *   cosine and sine, taken in 64 bits and rounded to float32.
+ * positions: [T, axes]; any values whose product with inv_freq is below 2^50. inv_freq: [pairs].
+ * Keys are quantized from float32, values as by w8a8_kv_write, into slots [T] (same rules;
+ * padding is not written). Queries q [T, q_heads, dim] (strides in elements; q_heads 0: none) are
+ * rounded to bf16 into q_out [T, q_heads, dim], contiguous, which must not overlap q, k or v;
+ * padding's too. */
+#define W8A8_ROPE_MAX_AXES 4
+w8a8_status w8a8_kv_append(uint8_t *cache, int64_t pages, int page, int heads, int dim, int fmt,
+                           const uint16_t *q, int64_t q_token, int64_t q_head, int q_heads,
+                           const uint16_t *k, int64_t k_token, int64_t k_head, const uint16_t *v,
+                           int64_t v_token, int64_t v_head, const int64_t *slots,
+                           const int64_t *positions, int axes, const int32_t *sections,
+                           const float *inv_freq, int pairs, int interleaved, int64_t T,
+                           uint16_t *q_out, void *stream);
+
+/* ---- The norm in front of a linear, and the log probabilities behind the last one.
+ *
+ * Root-mean-square norm of rows, quantized for w8a8_gemm or w8a8_mx4_gemm:
+ *   h = x, or bf16(x + residual), which is then written to sum;
+ *   r = float32(1 / sqrt(sum_k h[k]^2 / K + eps)), the sum and the root in 64 bits;
+ *   v[k] = (h[k] * r) * weight[k], float32 (weight NULL: ones),
+ * and v as by w8a8_quantize_act or w8a8_mx4_quantize. x, residual, sum: [M,K] bf16; sum may be x
+ * or residual itself, and is not written without a residual (NULL). weight: [K] float32, with
+ * SmoothQuant's 1/s folded in where the linear is smoothed. eps above 0 (else W8A8_ERR_ARG). K is at
+ * most W8A8_MAX_K (int8) or W8A8_MX4_MAX_K (W8A8_ERR_K_OVERFLOW). For non-finite h or weight int8
+ * results are unspecified; in 4 bits a block with a non-finite v is NaN (with a NaN in h that is all
+ * of its row; an infinity makes r zero). */
+w8a8_status w8a8_rms_norm_quantize(const uint16_t *x, const uint16_t *residual, uint16_t *sum,
+                                   const float *weight, double eps, int64_t M, int64_t K, int8_t *xq,
+                                   float *x_scale, void *stream);
+w8a8_status w8a8_rms_norm_mx4_quantize(const uint16_t *x, const uint16_t *residual, uint16_t *sum,
+                                       const float *weight, double eps, int64_t M, int64_t K,
+                                       uint8_t *codes, uint8_t *scales, void *stream);
+
+/* Log probabilities of rows of logits [T, V] (f32 0: bf16, 1: float32; rows row_stride elements
+ * apart). With p = softmax(logits / temperature) of a row:
+ *   logp [T]           log p[tokens[t]]; 0 where tokens[t] (int64 [T]) is below 0 or past V (padding)
+ *   entropy [T]        -sum p log p
+ *   top_ids [T, top]   the `top` largest logits, the lower index first where they are equal
+ *   top_logp [T, top]  their log p
+ * in float32. A logit of minus infinity has p = 0 and log p = minus infinity; a row of nothing
+ * else, or with a NaN or plus infinity, gives NaN (its top_ids are some indices of the row). V is 1
+ * to W8A8_LOGPROBS_MAX_V (else W8A8_ERR_SHAPE), top 0 to W8A8_LOGPROBS_MAX_TOP (W8A8_ERR_ARG) and
+ * at most V (W8A8_ERR_SHAPE); temperature is above 0 and finite, and so is its inverse
+ * (W8A8_ERR_ARG). workspace: w8a8_token_logprobs_workspace_bytes(T, V, top) bytes, 256-byte aligned
+ * (NULL allowed when that is 0). */
+#define W8A8_LOGPROBS_MAX_V ((int64_t)INT32_MAX)
+#define W8A8_LOGPROBS_MAX_TOP 64
+w8a8_status w8a8_token_logprobs(const void *logits, int f32, int64_t row_stride, int64_t T, int64_t V,
+                                const int64_t *tokens, int top, float temperature, float *logp,
+                                float *entropy, float *top_logp, int64_t *top_ids, void *workspace,
+                                size_t workspace_bytes, void *stream);
+size_t w8a8_token_logprobs_workspace_bytes(int64_t T, int64_t V, int top);
+
 /* Static description of a status code. */
 const char *w8a8_status_string(w8a8_status status);
 

@@ -26,6 +26,12 @@ key/value cache and the attention over it:
 
   mx4_quantize, mx4_dequantize, mx4_gemm, mx4_linear
   kv_cache, kv_write, kv_read, kv_attention
+  kv_append, kv_tree_attention       rotary positions on the way; trees of drafted tokens
+
+and what stands before the linears and behind the last one (lm.py):
+
+  rms_norm_quantize(x, weight)       -> (xq int8 [M,K], x_scale fp32 [M], h bf16 [M,K])
+  token_logprobs(logits, tokens)     -> (logp, entropy, top_logp, top_ids)
 
 If the library is missing, every call raises: there is no fallback.
 """
@@ -114,6 +120,15 @@ def load_library():
         "w8a8_kv_attention": ([P, I64, I64, P, I64, INT, INT, INT, INT, P, I64, INT, P, P, I64, INT,
                                INT, ctypes.c_float, INT, INT, INT, P, P, SZ, P], INT),
         "w8a8_kv_attention_workspace_bytes": ([INT, INT, INT, INT, INT, I64, INT, INT, INT], SZ),
+        "w8a8_kv_tree_attention": ([P, I64, I64, P, I64, INT, INT, INT, INT, P, I64, INT, P, P, I64,
+                                    INT, INT, ctypes.c_float, P, INT, INT, INT, P, P, SZ, P], INT),
+        "w8a8_kv_append": ([P, I64, INT, INT, INT, INT, P, I64, I64, INT, P, I64, I64, P, I64, I64, P,
+                            P, INT, P, P, INT, INT, I64, P, P], INT),
+        "w8a8_rms_norm_quantize": ([P, P, P, P, ctypes.c_double, I64, I64, P, P, P], INT),
+        "w8a8_rms_norm_mx4_quantize": ([P, P, P, P, ctypes.c_double, I64, I64, P, P, P], INT),
+        "w8a8_token_logprobs": ([P, INT, I64, I64, I64, P, INT, ctypes.c_float, P, P, P, P, P, SZ, P],
+                                INT),
+        "w8a8_token_logprobs_workspace_bytes": ([I64, I64, INT], SZ),
     }
     for name, (args, res) in sigs.items():
         f = getattr(lib, name)
@@ -478,8 +493,10 @@ def read_ceiling(buf: torch.Tensor, *, out=None):
     return sums
 
 
-from .mx import (KV_FORMATS, MX4_MAX_K, kv_attention, kv_cache, kv_read, kv_write,  # noqa: E402
-                 mx4_dequantize, mx4_gemm, mx4_linear, mx4_quantize)
+from .mx import (KV_FORMATS, MX4_MAX_K, kv_append, kv_attention, kv_cache, kv_read,  # noqa: E402
+                 kv_tree_attention, kv_write, mx4_dequantize, mx4_gemm, mx4_linear, mx4_quantize)
+from .lm import NORM_FORMATS, rms_norm_quantize, token_logprobs  # noqa: E402
 
 __all__ += ["mx4_quantize", "mx4_dequantize", "mx4_gemm", "mx4_linear", "kv_cache", "kv_write",
-            "kv_read", "kv_attention", "KV_FORMATS", "MX4_MAX_K"]
+            "kv_read", "kv_attention", "kv_append", "kv_tree_attention", "KV_FORMATS", "MX4_MAX_K",
+            "rms_norm_quantize", "token_logprobs", "NORM_FORMATS"]

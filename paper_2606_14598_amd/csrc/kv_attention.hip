@@ -79,6 +79,47 @@ __device__ __forceinline__ int seen(const Seq &s, int i, int causal) {
     return max(0, causal ? min(s.kv, s.kv - s.lq + i + 1) : s.kv);
 }
 
+// Tokens that some query up to i sees, and that every query from i on does. In a tree: all, as any
+// node may see any other, and those in front of it.
+template <bool TREE>
+__device__ __forceinline__ int some_seen(const Seq &s, int i, int causal) {
+    return TREE ? max(0, s.kv) : seen(s, i, causal);
+}
+template <bool TREE>
+__device__ __forceinline__ int all_seen(const Seq &s, int i, int causal) {
+    return TREE ? max(0, s.kv - s.lq) : seen(s, i, causal);
+}
+
+// What a row of a tree sees: the tokens in front of the tree, and nodes by its bits.
+struct TreeRow {
+    const uint32_t *bits;     // nullptr: a row that is none and sees nothing
+    int words, prefix, kv;    // the tree's first token (below 0: its first nodes are not cached)
+    __device__ __forceinline__ TreeRow(const KvAttnArgs &a, const Seq &s, int qi, bool live)
+        : bits(live ? a.tree + (s.q0 + qi) * a.tree_words : nullptr), words(a.tree_words),
+          prefix(s.kv - s.lq), kv(s.kv) {}
+    __device__ __forceinline__ uint32_t word(int i) const { return i < words ? bits[i] : 0; }
+    // Tokens j .. j + 31, the first in the lowest bit.
+    __device__ __forceinline__ uint32_t window(int j) const {
+        if (!bits || j >= kv)
+            return 0;
+        const int node = j - prefix;
+        uint32_t w;
+        if (node <= -32)
+            w = ~0u;
+        else if (node < 0)
+            w = word(0) << -node | ((1u << -node) - 1);
+        else
+            w = (uint32_t)((word(node / 32) | (uint64_t)word(node / 32 + 1) << 32) >> node % 32);
+        return kv - j < 32 ? w & ((1u << (kv - j)) - 1) : w;
+    }
+    __device__ __forceinline__ bool any() const {
+        uint32_t w = 0;
+        for (int j = 0; w == 0 && j < kv; j += 32)
+            w = window(j);
+        return w != 0;
+    }
+};
+
 __device__ __forceinline__ bool mine(const Split &sp, int rows) {
     return rows >= sp.rows_from && rows <= sp.rows_to;
 }
@@ -111,7 +152,7 @@ __device__ __forceinline__ int chunk_of(int share) {
 // A row's maximum before its first key: minus infinity where it sees none, else the least finite
 // number. A sum of zero then tells a row without keys (zeros) from one all of whose scores are
 // minus infinity, as a query with an infinity has them (NaN, as exp(-inf - -inf) is).
-__device__ __forceinline__ float start_of(int limit) { return limit > 0 ? -__FLT_MAX__ : -INFINITY; }
+__device__ __forceinline__ float start_of(bool sees) { return sees ? -__FLT_MAX__ : -INFINITY; }
 
 __device__ __forceinline__ float inverse(float l, float m) {
     return l == 0.0f ? (m == -INFINITY ? 0.0f : NAN) : 1.0f / l;
@@ -206,7 +247,7 @@ __device__ __forceinline__ void fill_places(Places &pl, const KvShape &c, const 
 // head) at 5.4 TB/s, 16 of 8000 with 18 heads of 256 at 5.6; one of 200000 in e2m1, 8 queries a
 // head, at 4.6 (about 370 instructions for 32 tokens of 4.3 KB); 48 sequences of very different
 // lengths at 4.0 (unequal shares, more workgroups that start).
-template <int FMT, int D>
+template <int FMT, int D, bool TREE>
 __global__ void __launch_bounds__(256, D <= 128 ? 3 : 2)
 kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
     constexpr int KU = FMT == KV_FP4 && D % 128 == 0 ? 32 : 16;   // elements of a key unit
@@ -243,7 +284,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 
     for (int rt = blockIdx.y; rt * kSplitRows < rows; rt += gridDim.y) {
         const int some_see =
-            seen(seq, (min(rt * kSplitRows + kSplitRows, rows) - 1) / a.group, a.causal);   // some row
+            some_seen<TREE>(seq, (min(rt * kSplitRows + kSplitRows, rows) - 1) / a.group, a.causal);
         const int share = max(even, ((some_see + sp.splits - 1) / sp.splits + 127) & ~127);
         const int used = (some_see + share - 1) / share;
         if (split >= max(used, 1))
@@ -254,7 +295,8 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
         const int qi = live ? row / a.group : 0;
         const int qh = head * a.group + (live ? row % a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
-        const int all_see = seen(seq, rt * kSplitRows / a.group, a.causal);   // every live row
+        const TreeRow tree(a, seq, qi, live);
+        const int all_see = all_seen<TREE>(seq, rt * kSplitRows / a.group, a.causal);   // every live row
         u32x4 q[NK][KU / 8];
         {
             const uint16_t *src = a.q + (seq.q0 + qi) * a.q_token + qh * a.q_head;
@@ -271,7 +313,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x4{};
-        float m = start_of(limit);
+        float m = start_of(TREE ? tree.any() : limit > 0);
         f32x4 sums = {};           // in each element: the sum of a row's weights
         uint32_t row_nan = 0;      // blocks of the row's output that a seen NaN value reaches
 
@@ -371,6 +413,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 }
                 if (part_seen && __any(any_nan)) {
                     // Rare: which rows see a NaN value, and in which blocks of 32 outputs.
+                    const uint32_t visible = TREE ? tree.window(j0) : 0;
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
                         uint64_t marked = __ballot(vs[i] == 256);
@@ -378,7 +421,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                             const int src = __builtin_ctzll(marked);
                             marked &= marked - 1;
                             const int unit = i * 64 + src;
-                            if (j0 + unit / VT < limit)
+                            if (TREE ? visible >> (unit / VT) & 1 : j0 + unit / VT < limit)
                                 row_nan |= 1u << (unit % VT * VU / 32);
                         }
                     }
@@ -388,12 +431,14 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 
                 if (part_seen) {
                     const int left = limit - j0 - 4 * g;
+                    const uint32_t visible = TREE ? tree.window(j0) >> 4 * g : 0;
                     keep_branch();
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            s[h][e] = 16 * h + e < left ? s[h][e] : -INFINITY;
+                            s[h][e] = (TREE ? visible >> (16 * h + e) & 1 : 16 * h + e < left) ? s[h][e]
+                                                                                               : -INFINITY;
                 }
                 float top = -INFINITY;
 #pragma unroll
@@ -547,7 +592,7 @@ __device__ __forceinline__ u32x2 both_halves(float v) {
 // tiles, 670 and 382 so.
 constexpr int kSpreadUnits = 32;
 
-template <int FMT, int D>
+template <int FMT, int D, bool TREE>
 __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1)
 kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     constexpr int TT = kTileTokens;
@@ -593,7 +638,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     // Row tiles first_rt, first_rt + tiles, ...: more than one only where the grid has fewer.
     for (int rt = first_rt; rt <= last_rt; rt += tiles) {
         const int some_see =
-            seen(seq, (min(rt * kTileRows + kTileRows, rows) - 1) / a.group, a.causal);   // some row
+            some_seen<TREE>(seq, (min(rt * kTileRows + kTileRows, rows) - 1) / a.group, a.causal);
         const int share = max(even, ((some_see + sp.splits - 1) / sp.splits + 127) & ~127);
         const int used = (some_see + share - 1) / share;
         if (split >= max(used, 1))
@@ -604,11 +649,12 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
         const int qi = live ? row / a.group : 0;
         const int qh = head * a.group + (live ? row - qi * a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
-        const int all_see = seen(seq, rt * kTileRows / a.group, a.causal);
+        const TreeRow tree(a, seq, qi, live);
+        const int all_see = all_seen<TREE>(seq, rt * kTileRows / a.group, a.causal);
         // what some row of this wavefront sees
         const int wave_first = rt * kTileRows + wave * 32;
         const int wave_sees =
-            wave_first < rows ? seen(seq, (min(wave_first + 32, rows) - 1) / a.group, a.causal) : 0;
+            wave_first < rows ? some_seen<TREE>(seq, (min(wave_first + 32, rows) - 1) / a.group, a.causal) : 0;
         u32x4 q[KS];
         {
             const uint16_t *src = a.q + (seq.q0 + qi) * a.q_token + qh * a.q_head + 8 * h;
@@ -622,7 +668,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x16{};
-        float m = start_of(limit), l = 0.0f;
+        float m = start_of(TREE ? tree.any() : limit > 0), l = 0.0f;
         uint32_t row_nan = 0;
 
         for (int ch = split; ch < nch; ch += used) {
@@ -704,10 +750,14 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                 lds_barrier();       // this tile is staged, the other stage's last one is read
                 if (partly_seen(j0 + TT) && tile + 1 < ntile)
                     mark(j0 + TT, st ^ 1);
-                if (part_seen && nan_any)      // rare: which rows see a NaN block
+                if (part_seen && nan_any) {    // rare: which rows see a NaN block
+                    const uint64_t visible =
+                        TREE ? tree.window(j0) | (uint64_t)tree.window(j0 + 32) << 32 : 0;
                     for (int unit = 0; unit < UNITS; ++unit)
-                        if (nan_unit[st][unit] && j0 + unit / VT < limit)
+                        if (nan_unit[st][unit] &&
+                            (TREE ? visible >> (unit / VT) & 1 : j0 + unit / VT < limit))
                             row_nan |= 1u << (unit % VT * VU / 32);
+                }
                 // Scores: token 32 t + 8 (i / 4) + 4 h + i % 4 in s[t][i]. Between the products
                 // the next tile is staged (after the last tile: itself again, unread).
                 f32x16 s[2] = {f32x16{}, f32x16{}};
@@ -742,12 +792,20 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 
                 if (part_seen) {
                     const int left = limit - j0 - 4 * h;
+                    uint32_t visible[2] = {};
+                    if constexpr (TREE) {
+                        visible[0] = tree.window(j0) >> 4 * h;
+                        visible[1] = tree.window(j0 + 32) >> 4 * h;
+                    }
                     keep_branch();
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            s[t][i] = 32 * t + 8 * (i / 4) + i % 4 < left ? s[t][i] : -INFINITY;
+                            s[t][i] = (TREE ? visible[t] >> (8 * (i / 4) + i % 4) & 1
+                                            : 32 * t + 8 * (i / 4) + i % 4 < left)
+                                          ? s[t][i]
+                                          : -INFINITY;
                 }
                 float top = -INFINITY;
 #pragma unroll
@@ -1023,7 +1081,7 @@ Plan plan_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int ma
     return p;
 }
 
-template <int FMT, int D>
+template <int FMT, int D, bool TREE>
 hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, hipStream_t s) {
     const int64_t rows = a.T * c.heads * a.group;
     const auto run = [&](bool many, Split &sp, int64_t most_rows) {
@@ -1034,7 +1092,7 @@ hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, h
             if (!launchable(units, 256))
                 return hipErrorInvalidValue;
             const dim3 grid((unsigned)units, (unsigned)((most_rows + kSplitRows - 1) / kSplitRows));
-            hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D>), grid, dim3(256), 0, s, c, a, sp);
+            hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D, TREE>), grid, dim3(256), 0, s, c, a, sp);
             return hipGetLastError();
         }
         // A workgroup goes on to every tiles-th row tile, so that a loose max_q costs empty
@@ -1044,7 +1102,7 @@ hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, h
                                        std::max<int64_t>(kMostGroups / columns, 1));
         if (!launchable(columns * tiles, 256))
             return hipErrorInvalidValue;
-        hipLaunchKernelGGL((kv_attention_tile_kernel<FMT, D>), dim3((unsigned)(columns * tiles)),
+        hipLaunchKernelGGL((kv_attention_tile_kernel<FMT, D, TREE>), dim3((unsigned)(columns * tiles)),
                            dim3(256), 0, s, c, a, sp, (int)tiles);
         return hipGetLastError();
     };
@@ -1074,7 +1132,9 @@ hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, 
         return hipErrorInvalidValue;
     Plan p = plan_of(c, a.T, a.seqs, a.group, a.max_q, a.max_kv);
     const auto run = [&](auto dim, auto format) {
-        return run_plan<decltype(format)::value, decltype(dim)::value>(c, a, p, static_cast<float *>(ws), s);
+        constexpr int F = decltype(format)::value, D = decltype(dim)::value;
+        return a.tree ? run_plan<F, D, true>(c, a, p, static_cast<float *>(ws), s)
+                      : run_plan<F, D, false>(c, a, p, static_cast<float *>(ws), s);
     };
     const auto go = [&](auto dim) {
         return c.fmt == KV_FP8 ? run(dim, std::integral_constant<int, KV_FP8>{})

@@ -8,8 +8,7 @@
 //
 // Four lanes hold a block, 8 values each; bound by memory: 20000 tokens of 8 heads of 128 are
 // written in 4 bits in 19 us (5.4 TB/s read and written) and read back in 19.
-#include "mx_internal.hpp"
-#include "mx_math.hpp"
+#include "kv_layout.hpp"
 
 namespace w8a8 {
 namespace {
@@ -21,47 +20,15 @@ using namespace mx;
 // takes are done once.
 constexpr int kLoads = 4;
 
-struct Token {
-    int64_t t;                 // of the call; past its tokens: nothing to do
-    int64_t keys;              // its page in the cache; below 0 for padding
-    int at;                    // its place in the page
-};
-
-__device__ __forceinline__ Token token_of(const KvShape &c, const int64_t *slots, int64_t T) {
-    Token k;
-    k.t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    k.keys = -1;
-    k.at = 0;
-    if (k.t >= T)
-        return k;
-    const int64_t slot = slots[k.t];
-    if (slot < 0 || slot >= c.pages * c.page)
-        return k;
-    const int64_t page = slot >> 31 ? slot / c.page : (uint32_t)slot / (uint32_t)c.page;
-    k.at = (int)(slot - page * c.page);
-    k.keys = page * 2 * c.heads * c.head_bytes();
-    return k;
+// The token of this wavefront.
+__device__ __forceinline__ Token wave_token(const KvShape &c, const int64_t *slots, int64_t T) {
+    return token_of(c, slots, (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), T);
 }
-
-// Unit u of a token: 8 values of keys or values; heads * 2 * D / 8 of them.
-template <int FMT, int D>
-struct Unit8 {
-    static constexpr int CB = FMT == KV_FP8 ? D : D / 2;
-    int head, e;               // head over keys, then values; first of the 8 values
-    int64_t codes, scale;      // in the cache
-    __device__ __forceinline__ Unit8(const KvShape &c, const Token &k, int u) {
-        head = u / (D / 8);
-        e = u % (D / 8) * 8;
-        const int64_t base = k.keys + head * c.head_bytes();
-        codes = base + k.at * CB + (FMT == KV_FP8 ? e : e / 2);
-        scale = base + c.page * CB + k.at * (D / 32) + e / 32;
-    }
-};
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(256)
 kv_write_kernel(uint8_t *cache, KvShape c, KvRows k, KvRows v, const int64_t *slots, int64_t T) {
-    const Token tok = token_of(c, slots, T);
+    const Token tok = wave_token(c, slots, T);
     if (tok.keys < 0)
         return;
     const int units = 2 * c.heads * (D / 8), u0 = blockIdx.y * (64 * kLoads) + (threadIdx.x & 63);
@@ -102,7 +69,7 @@ kv_write_kernel(uint8_t *cache, KvShape c, KvRows k, KvRows v, const int64_t *sl
 template <int FMT, int D>
 __global__ void __launch_bounds__(256)
 kv_read_kernel(const uint8_t *cache, KvShape c, KvRows k, KvRows v, const int64_t *slots, int64_t T) {
-    const Token tok = token_of(c, slots, T);
+    const Token tok = wave_token(c, slots, T);
     if (tok.t >= T)
         return;
     const int units = 2 * c.heads * (D / 8), u0 = blockIdx.y * (64 * kLoads) + (threadIdx.x & 63);

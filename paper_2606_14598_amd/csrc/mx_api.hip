@@ -1,7 +1,7 @@
 // C ABI of the microscaled operators: argument validation and launches on the caller's
 // stream. Nothing here allocates, frees or synchronizes.
 #include "../../include/w8a8.h"
-#include "mx_internal.hpp"
+#include "lm_internal.hpp"
 
 namespace {
 
@@ -17,6 +17,7 @@ w8a8_status from_hip(hipError_t e) { return e == hipSuccess ? W8A8_OK : W8A8_ERR
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 static_assert(W8A8_KV_FP8 == KV_FP8 && W8A8_KV_FP4 == KV_FP4, "cache formats");
+static_assert(W8A8_ROPE_MAX_AXES == kMaxAxes, "axes");
 
 w8a8_status check_matrix(int64_t R, int64_t K) {
     if (R < 0 || K < 0 || !product_ok(R, K))
@@ -67,6 +68,60 @@ w8a8_status check_rows(const KvShape &c, const void *k, const void *v, const int
 
 // The bound on a sequence's queries that a launch is laid out for: a loose one, so never 0.
 int query_bound(int max_q) { return max_q > 1 ? max_q : 1; }
+
+// Attention by the causal rule or by a tree's bits.
+w8a8_status attend(const uint16_t *q, int64_t q_token, int64_t q_head, const uint8_t *cache,
+                   int64_t pages, int page, int heads, int dim, int fmt, const int32_t *table,
+                   int64_t table_stride, int table_pages, const int32_t *kv_lens,
+                   const int32_t *q_starts, int64_t T, int seqs, int group, float scale, int causal,
+                   const int64_t *tree, int tree_words, int max_q, int max_kv, uint16_t *out,
+                   void *workspace, size_t workspace_bytes, void *stream) {
+    KvShape c;
+    if (!cache_shape(c, pages, page, heads, dim, fmt) || group < 1 ||
+        group > W8A8_KV_MAX_HEADS || (causal != 0 && causal != 1) || !__builtin_isfinite(scale))
+        return W8A8_ERR_ARG;
+    if (T < 0 || seqs < 0 || table_pages < 0 || table_stride < 0 || q_token < 0 || q_head < 0 ||
+        max_q < 0 || max_kv < 0 || !product_ok(T, (int64_t)heads * group * dim) ||
+        (int64_t)table_pages * page > W8A8_KV_MAX_TOKENS)
+        return W8A8_ERR_SHAPE;
+    if (T == 0 || seqs == 0)
+        return T == 0 ? W8A8_OK : W8A8_ERR_SHAPE;
+    if (!q_starts && T % seqs != 0)
+        return W8A8_ERR_SHAPE;
+    if (!q || !out || !kv_lens || (table_pages > 0 && pages > 0 && (!cache || !table)))
+        return W8A8_ERR_NULL;
+    if (!aligned(cache, 16))
+        return W8A8_ERR_ARG;
+    KvAttnArgs a;
+    a.q = q;
+    a.q_token = q_token;
+    a.q_head = q_head;
+    a.cache = cache;
+    a.table = table;
+    a.table_stride = table_stride;
+    a.kv_lens = kv_lens;
+    a.q_starts = q_starts;
+    a.out = out;
+    a.T = T;
+    a.seqs = seqs;
+    a.group = group;
+    a.table_pages = pages > 0 ? table_pages : 0;
+    a.causal = causal;
+    a.tree = reinterpret_cast<const uint32_t *>(tree);
+    a.tree_words = 2 * tree_words;
+    a.max_q = query_bound(max_q);
+    a.max_kv = max_kv;
+    // The kernels scale a maximum instead of every score, and mask with minus infinity: a
+    // positive factor. A zero becomes so small a one that all weights are 1.
+    a.q_sign = scale < 0.0f ? 0x80008000u : 0u;
+    a.scale = __builtin_fabsf(scale) * 1.44269504088896341f;
+    if (a.scale < 0x1p-126f)
+        a.scale = 0x1p-126f;
+    const size_t need = kv_attention_workspace_bytes(c, T, seqs, group, a.max_q, max_kv);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
+        return W8A8_ERR_WORKSPACE;
+    return from_hip(launch_kv_attention(c, a, workspace, as_stream(stream)));
+}
 
 }  // namespace
 
@@ -217,49 +272,77 @@ w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head
                               int64_t T, int seqs, int group, float scale, int causal, int max_q,
                               int max_kv, uint16_t *out, void *workspace, size_t workspace_bytes,
                               void *stream) {
-    KvShape c;
-    if (!cache_shape(c, pages, page, heads, dim, fmt) || group < 1 ||
-        group > W8A8_KV_MAX_HEADS || (causal != 0 && causal != 1) || !__builtin_isfinite(scale))
+    return attend(q, q_token, q_head, cache, pages, page, heads, dim, fmt, table, table_stride, table_pages,
+                  kv_lens, q_starts, T, seqs, group, scale, causal, nullptr, 0, max_q, max_kv, out,
+                  workspace, workspace_bytes, stream);
+}
+
+w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
+                              const uint8_t *cache, int64_t pages, int page, int heads, int dim,
+                              int fmt, const int32_t *table, int64_t table_stride,
+                              int table_pages, const int32_t *kv_lens, const int32_t *q_starts,
+                              int64_t T, int seqs, int group, float scale, const int64_t *tree,
+                              int tree_words, int max_q,
+                              int max_kv, uint16_t *out, void *workspace, size_t workspace_bytes,
+                              void *stream) {
+    if (tree_words < 1 || tree_words > W8A8_KV_MAX_TREE_WORDS)
         return W8A8_ERR_ARG;
-    if (T < 0 || seqs < 0 || table_pages < 0 || table_stride < 0 || q_token < 0 || q_head < 0 ||
-        max_q < 0 || max_kv < 0 || !product_ok(T, (int64_t)heads * group * dim) ||
-        (int64_t)table_pages * page > W8A8_KV_MAX_TOKENS)
-        return W8A8_ERR_SHAPE;
-    if (T == 0 || seqs == 0)
-        return T == 0 ? W8A8_OK : W8A8_ERR_SHAPE;
-    if (!q_starts && T % seqs != 0)
-        return W8A8_ERR_SHAPE;
-    if (!q || !out || !kv_lens || (table_pages > 0 && pages > 0 && (!cache || !table)))
+    if (T > 0 && seqs > 0 && !tree)
         return W8A8_ERR_NULL;
-    if (!aligned(cache, 16))
+    return attend(q, q_token, q_head, cache, pages, page, heads, dim, fmt, table, table_stride, table_pages,
+                  kv_lens, q_starts, T, seqs, group, scale, 0, tree, tree_words, max_q, max_kv, out,
+                  workspace, workspace_bytes, stream);
+}
+
+w8a8_status w8a8_kv_append(uint8_t *cache, int64_t pages, int page, int heads, int dim, int fmt,
+                           const uint16_t *q, int64_t q_token, int64_t q_head, int q_heads,
+                           const uint16_t *k, int64_t k_token, int64_t k_head, const uint16_t *v,
+                           int64_t v_token, int64_t v_head, const int64_t *slots,
+                           const int64_t *positions, int axes, const int32_t *sections,
+                           const float *inv_freq, int pairs, int interleaved, int64_t T,
+                           uint16_t *q_out, void *stream) {
+    KvShape c;
+    if (!cache_shape(c, pages, page, heads, dim, fmt) || axes < 1 || axes > W8A8_ROPE_MAX_AXES ||
+        pairs < 0 || pairs > dim / 2 || (interleaved != 0 && interleaved != 1) || q_heads < 0 ||
+        q_heads > W8A8_KV_MAX_HEADS * W8A8_KV_MAX_HEADS)
         return W8A8_ERR_ARG;
-    KvAttnArgs a;
-    a.q = q;
-    a.q_token = q_token;
-    a.q_head = q_head;
-    a.cache = cache;
-    a.table = table;
-    a.table_stride = table_stride;
-    a.kv_lens = kv_lens;
-    a.q_starts = q_starts;
-    a.out = out;
+    AppendArgs a;
+    int at = 0;
+    for (int n = 0; n < kMaxAxes; ++n) {
+        if (axes > 1 && n < axes) {
+            if (!sections)
+                return W8A8_ERR_NULL;
+            if (sections[n] < 0 || sections[n] > pairs - at)
+                return W8A8_ERR_ARG;
+            at += sections[n];
+        }
+        a.section_end[n] = axes > 1 ? at : pairs;
+    }
+    if (axes > 1 && at != pairs)
+        return W8A8_ERR_ARG;
+    const w8a8_status st = check_rows(c, k, v, slots, T);
+    if (st != W8A8_OK || T == 0)
+        return st;
+    if (!product_ok(T, (int64_t)q_heads * dim))
+        return W8A8_ERR_SHAPE;
+    if ((pages > 0 && !cache) || (q_heads > 0 && (!q || !q_out)) || (pairs > 0 && (!positions || !inv_freq)))
+        return W8A8_ERR_NULL;
+    if (!aligned(cache, 16) || q_token < 0 || q_head < 0 || k_token < 0 || k_head < 0 || v_token < 0 ||
+        v_head < 0)
+        return W8A8_ERR_ARG;
+    a.q = {const_cast<uint16_t *>(q), q_token, q_head};
+    a.k = {const_cast<uint16_t *>(k), k_token, k_head};
+    a.v = {const_cast<uint16_t *>(v), v_token, v_head};
+    a.q_out = q_out;
+    a.q_heads = q_heads;
+    a.slots = slots;
+    a.positions = positions;
+    a.inv_freq = inv_freq;
+    a.axes = axes;
+    a.pairs = pairs;
+    a.interleaved = interleaved;
     a.T = T;
-    a.seqs = seqs;
-    a.group = group;
-    a.table_pages = pages > 0 ? table_pages : 0;
-    a.causal = causal;
-    a.max_q = query_bound(max_q);
-    a.max_kv = max_kv;
-    // The kernels scale a maximum instead of every score, and mask with minus infinity: a
-    // positive factor. A zero becomes so small a one that all weights are 1.
-    a.q_sign = scale < 0.0f ? 0x80008000u : 0u;
-    a.scale = __builtin_fabsf(scale) * 1.44269504088896341f;
-    if (a.scale < 0x1p-126f)
-        a.scale = 0x1p-126f;
-    const size_t need = kv_attention_workspace_bytes(c, T, seqs, group, a.max_q, max_kv);
-    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
-        return W8A8_ERR_WORKSPACE;
-    return from_hip(launch_kv_attention(c, a, workspace, as_stream(stream)));
+    return from_hip(launch_kv_append(cache, c, a, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -72,6 +72,8 @@ struct KvAttnArgs {
     int max_q, max_kv;            // what the grid is laid out for; the results don't depend on them
     float scale;                  // of the scores, times log2(e); above 0
     uint32_t q_sign;              // 0x80008000: the scale's sign, taken into q; else 0
+    const uint32_t *tree;         // [T, tree_words] or nullptr: which of a sequence's last lq tokens
+    int tree_words;               // a query sees, a bit each (causal is not read then)
 };
 
 size_t kv_attention_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_q,

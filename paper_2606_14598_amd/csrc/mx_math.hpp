@@ -85,6 +85,17 @@ __device__ __forceinline__ uint32_t encode8_bf16(uint32_t a, uint32_t b, uint32_
     return __builtin_bit_cast(uint32_t, c);
 }
 
+// Four float32 values to e4m3 elements; top: the exponent field of the block's largest.
+__device__ __forceinline__ uint32_t encode8_f32(float v0, float v1, float v2, float v3, uint32_t top,
+                                                float scale) {
+    const float most = __uint_as_float(max(top, (uint32_t)kTop8) << 23 | 0x600000u);
+    const auto clamp = [&](float v) { return __builtin_amdgcn_fmed3f(v, -most, most); };
+    i16x2 c = {0, 0};
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, clamp(v0), clamp(v1), scale, false);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, clamp(v2), clamp(v3), scale, true);
+    return __builtin_bit_cast(uint32_t, c);
+}
+
 // Two bf16 values (a word) of byte SEL of e2m1 codes, or of half SEL of e4m3 codes. Exact:
 // both formats' values times a power of two are bf16 values (scale 255 gives NaN).
 template <int SEL>

@@ -10,10 +10,14 @@ formats and rules); imported by the package, whose conventions hold here too.
   kv_cache(pages, heads, head_dim)         -> cache uint8 [pages, 2, heads, head bytes]
   kv_write(cache, k, v, slots)                quantizes k, v [T, heads, head_dim] into slots
   kv_read(cache, slots, head_dim)          -> k, v bf16 [T, heads, head_dim]
+  kv_append(cache, k, v, slots, positions, inv_freq, q=q)
+                                           -> q, turned; keys turned, then as kv_write
   kv_attention(q, cache, block_table, kv_lens) -> bf16 [T, q heads, head_dim]
+  kv_tree_attention(q, cache, block_table, kv_lens, tree)   the same for drafted trees
 """
 from __future__ import annotations
 
+import ctypes
 import functools
 
 import torch
@@ -25,7 +29,7 @@ from . import (_act, _check, _check_out, _col_mul, _launch, _ptr, _same_device, 
 _bytes = functools.lru_cache(maxsize=4096)(_size)
 
 __all__ = ["mx4_quantize", "mx4_dequantize", "mx4_gemm", "mx4_linear", "kv_cache", "kv_write",
-           "kv_read", "kv_attention", "KV_FORMATS", "MX4_MAX_K"]
+           "kv_read", "kv_append", "kv_attention", "kv_tree_attention", "KV_FORMATS", "MX4_MAX_K"]
 
 MX4_MAX_K = 1 << 22
 KV_FORMATS = {"fp8": 0, "fp4": 1}
@@ -211,6 +215,66 @@ def kv_read(cache, slots, head_dim: int, *, fmt: str = "fp8"):
     return k, v
 
 
+@functools.lru_cache(maxsize=256)
+def _sections(sections, axes: int, pairs: int):
+    """The sections as the C ABI takes them (host memory)."""
+    if sections is None:
+        if axes != 1:
+            raise ValueError(f"positions of {axes} axes need sections, the pairs of each")
+        return None
+    if len(sections) != axes or any(n < 0 for n in sections) or sum(sections) != pairs:
+        raise ValueError(f"sections must be {axes} counts of sum {pairs}, got {sections}")
+    return (ctypes.c_int32 * axes)(*sections)
+
+
+def kv_append(cache, k, v, slots, positions, inv_freq, *, q=None, fmt: str = "fp8", sections=None,
+              interleaved: bool = False, out=None):
+    """kv_write with rotary positions: keys (and queries) are turned by angles
+    positions * inv_freq, taken in 64 bits, before keys and values are quantized into the slots.
+
+    k, v bf16 [T, heads, head_dim], slots as in kv_write. positions int64 [T], or [T, axes] (up to 4:
+    time, height, width) with sections, the number of neighbouring pairs that each axis turns.
+    inv_freq fp32 [pairs]: up to head_dim / 2, channels past 2 pairs stay as they are. A pair is
+    channels p and p + pairs, or 2p and 2p + 1 with interleaved. q bf16 [T, q heads, head_dim] (any
+    strides of token and head): returned turned, rounded to bf16, contiguous, or in `out`, which may
+    not overlap q; padding's queries too. Returns None without q."""
+    device = cache.device
+    _check_heads(k, "k", device)
+    _check_heads(v, "v", device)
+    T, heads, dim = k.shape
+    shape = _check_cache(cache, dim, fmt)
+    if k.shape != v.shape or heads != shape[2]:
+        raise ValueError("shape mismatch")
+    _check_slots(slots, T, device)
+    two = isinstance(positions, torch.Tensor) and positions.dim() == 2
+    _check(positions, torch.int64, 2 if two else 1, "positions")
+    axes = positions.shape[1] if two else 1
+    _check(inv_freq, torch.float32, 1, "inv_freq")
+    _same_device(cache, positions, inv_freq)
+    pairs = inv_freq.shape[0]
+    if positions.shape[0] != T or not 1 <= axes <= 4:
+        raise ValueError(f"positions must be [{T}] or [{T}, up to 4], got {tuple(positions.shape)}")
+    if pairs > dim // 2:
+        raise ValueError(f"{pairs} pairs in heads of {dim}")
+    sec = _sections(None if sections is None else tuple(sections), axes, pairs)
+    q_heads = q_token = q_head = 0
+    y = None
+    if q is not None:
+        _check_heads(q, "q", device)
+        if q.shape[0] != T or q.shape[2] != dim:
+            raise ValueError("shape mismatch")
+        q_heads, q_token, q_head = q.shape[1], q.stride(0), q.stride(1)
+        if out is not None:
+            _check_out(out, torch.bfloat16, tuple(q.shape), device)
+        y = out if out is not None else torch.empty(q.shape, dtype=torch.bfloat16, device=device)
+    elif out is not None:
+        raise ValueError("out needs q")
+    _launch(device, "w8a8_kv_append", _ptr(cache), *shape, _ptr(q), q_token, q_head, q_heads, _ptr(k),
+            k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1), _ptr(slots),
+            _ptr(positions), axes, sec, _ptr(inv_freq), pairs, int(bool(interleaved)), T, _ptr(y))
+    return y
+
+
 def kv_attention(q, cache, block_table, kv_lens, *, fmt: str = "fp8", q_starts=None,
                  scale: float | None = None, causal: bool = True, max_q: int | None = None,
                  max_kv: int | None = None, out=None, workspace=None):
@@ -228,6 +292,26 @@ def kv_attention(q, cache, block_table, kv_lens, *, fmt: str = "fp8", q_starts=N
     a head of the cache), which always keep two bf16 terms. Tight bounds are faster: 64 prompts of
     1000 tokens take 0.8 ms with max_q and 1.0 without; one sequence of 2000 tokens, one query,
     16 us with max_kv and 24 by a table of 131072 tokens (8 heads of 128, 4 queries a head)."""
+    return _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, bool(causal), None, max_q,
+                   max_kv, out, workspace)
+
+
+def kv_tree_attention(q, cache, block_table, kv_lens, tree, *, fmt: str = "fp8", q_starts=None,
+                      scale: float | None = None, max_q: int | None = None,
+                      max_kv: int | None = None, out=None, workspace=None):
+    """kv_attention of drafted tokens that continue each sequence in several ways. A sequence's
+    queries are the nodes of a tree, its last cached tokens, in order; all of them see the tokens in
+    front of the tree, and query i of a sequence sees node n where bit n % 64 of
+    tree[q_starts[b] + i, n // 64] is set: itself and its ancestors (tree int64 [T, words], up to
+    64 words). A query that sees nothing gives zeros. Everything else is as in kv_attention."""
+    if not isinstance(tree, torch.Tensor) or tree.dtype != torch.int64:
+        raise TypeError("tree must be an int64 torch.Tensor")
+    return _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, False, tree, max_q, max_kv,
+                   out, workspace)
+
+
+def _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, causal, tree, max_q, max_kv, out,
+            workspace):
     device = cache.device
     _check_heads(q, "q", device)
     T, q_heads, dim = q.shape
@@ -245,7 +329,11 @@ def kv_attention(q, cache, block_table, kv_lens, *, fmt: str = "fp8", q_starts=N
             raise ValueError(f"q_starts must have {B + 1} entries, got {q_starts.shape[0]}")
     elif T != 0 and (B == 0 or T % B != 0):
         raise ValueError(f"{T} queries do not divide among {B} sequences")
-    _same_device(cache, kv_lens, block_table, q_starts)
+    if tree is not None:
+        _check(tree, torch.int64, 2, "tree")
+        if tree.shape[0] != T or not 1 <= tree.shape[1] <= 64:
+            raise ValueError(f"tree must be [{T}, 1 to 64], got {tuple(tree.shape)}")
+    _same_device(cache, kv_lens, block_table, q_starts, tree)
     if q_heads == 0 or q_heads % heads != 0:
         raise ValueError(f"{q_heads} query heads do not divide among {heads}")
     if max_q is None:
@@ -263,9 +351,10 @@ def kv_attention(q, cache, block_table, kv_lens, *, fmt: str = "fp8", q_starts=N
     nws = _bytes("w8a8_kv_attention_workspace_bytes", page, heads, dim, f, group, T, B,
                 max_q, max_kv)
     ws = _workspace(nws, device, workspace)
-    _launch(device, "w8a8_kv_attention", _ptr(q), q.stride(0), q.stride(1), _ptr(cache), pages,
-            page, heads, dim, f, _ptr(block_table), block_table.stride(0), width, _ptr(kv_lens),
-            _ptr(q_starts), T, B, group, dim ** -0.5 if scale is None else float(scale),
-            int(bool(causal)), max_q, max_kv, _ptr(y), _ptr(ws),
+    rule = (int(causal),) if tree is None else (_ptr(tree), tree.shape[1])
+    _launch(device, "w8a8_kv_attention" if tree is None else "w8a8_kv_tree_attention", _ptr(q),
+            q.stride(0), q.stride(1), _ptr(cache), pages, page, heads, dim, f, _ptr(block_table),
+            block_table.stride(0), width, _ptr(kv_lens), _ptr(q_starts), T, B, group,
+            dim ** -0.5 if scale is None else float(scale), *rule, max_q, max_kv, _ptr(y), _ptr(ws),
             0 if ws is None else ws.nbytes)
     return y

@@ -17,6 +17,13 @@ and, for the microscaled operators,
   torch.ops.w8a8.kv_read(cache, slots, head_dim, fmt)           -> (k, v) bf16
   torch.ops.w8a8.kv_attention(q, cache, block_table, kv_lens, q_starts, fmt, scale, causal,
                               max_q, max_kv)                    -> bf16 like q
+  torch.ops.w8a8.kv_append(cache, k, v, slots, positions, inv_freq, q, fmt, sections, interleaved)
+                                                 -> bf16 like q (writes to cache; empty without q)
+  torch.ops.w8a8.kv_tree_attention(q, cache, block_table, kv_lens, tree, q_starts, fmt, scale,
+                                   max_q, max_kv)               -> bf16 like q
+  torch.ops.w8a8.rms_norm_quantize(x, weight, residual, eps, fmt) -> (codes, scales, h)
+  torch.ops.w8a8.token_logprobs(logits, tokens, top, temperature)
+                                                 -> (logp, entropy, top_logp, top_ids)
 
 The ops are inference-only (no autograd formula): the integer codes have no useful
 gradient. The real implementations are the HIP library's entry points; the fake ones
@@ -28,8 +35,9 @@ from typing import Optional
 
 import torch
 
-from . import (ACTS, gemm, kv_attention, kv_read, kv_write, linear, mx4_linear, mx4_quantize,
-               quantize_act, quantize_weight)
+from . import (ACTS, gemm, kv_append, kv_attention, kv_read, kv_tree_attention, kv_write, linear,
+               mx4_linear, mx4_quantize, quantize_act, quantize_weight, rms_norm_quantize,
+               token_logprobs)
 
 _ACT_NAMES = {v: k for k, v in ACTS.items()}
 
@@ -174,6 +182,68 @@ def kv_attention_op(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Ten
 @kv_attention_op.register_fake
 def _kv_attention_fake(q, cache, block_table, kv_lens, q_starts, fmt, scale, causal, max_q, max_kv):
     return q.new_empty(q.shape)
+
+
+@torch.library.custom_op("w8a8::kv_append", mutates_args=("cache",))
+def kv_append_op(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor,
+                 positions: torch.Tensor, inv_freq: torch.Tensor, q: Optional[torch.Tensor], fmt: str,
+                 sections: Optional[list[int]], interleaved: bool) -> torch.Tensor:
+    y = kv_append(cache, k, v, slots, positions, inv_freq, q=q, fmt=fmt, sections=sections,
+                  interleaved=interleaved)
+    return k.new_empty((k.shape[0], 0, k.shape[2])) if y is None else y
+
+
+@kv_append_op.register_fake
+def _kv_append_fake(cache, k, v, slots, positions, inv_freq, q, fmt, sections, interleaved):
+    torch._check(k.shape == v.shape, lambda: "shape mismatch")
+    return k.new_empty((k.shape[0], 0, k.shape[2])) if q is None else q.new_empty(q.shape)
+
+
+@torch.library.custom_op("w8a8::kv_tree_attention", mutates_args=())
+def kv_tree_attention_op(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor,
+                         kv_lens: torch.Tensor, tree: torch.Tensor, q_starts: Optional[torch.Tensor],
+                         fmt: str, scale: Optional[float], max_q: Optional[int],
+                         max_kv: Optional[int]) -> torch.Tensor:
+    return kv_tree_attention(q, cache, block_table, kv_lens, tree, fmt=fmt, q_starts=q_starts,
+                             scale=scale, max_q=max_q, max_kv=max_kv)
+
+
+@kv_tree_attention_op.register_fake
+def _kv_tree_attention_fake(q, cache, block_table, kv_lens, tree, q_starts, fmt, scale, max_q, max_kv):
+    return q.new_empty(q.shape)
+
+
+@torch.library.custom_op("w8a8::rms_norm_quantize", mutates_args=())
+def rms_norm_quantize_op(x: torch.Tensor, weight: Optional[torch.Tensor],
+                         residual: Optional[torch.Tensor], eps: float,
+                         fmt: str) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    codes, scales, h = rms_norm_quantize(x, weight, residual=residual, eps=eps, fmt=fmt)
+    return codes, scales, x.clone() if residual is None else h     # an op's output is no input of it
+
+
+@rms_norm_quantize_op.register_fake
+def _rms_norm_quantize_fake(x, weight, residual, eps, fmt):
+    M, K = x.shape
+    if fmt == "int8":
+        codes, scales = x.new_empty((M, K), dtype=torch.int8), x.new_empty((M,), dtype=torch.float32)
+    else:
+        codes = x.new_empty((M, (K + 31) // 32 * 16), dtype=torch.uint8)
+        scales = x.new_empty(((K + 255) // 256, M, 8), dtype=torch.uint8)
+    return codes, scales, x.new_empty((M, K))
+
+
+@torch.library.custom_op("w8a8::token_logprobs", mutates_args=())
+def token_logprobs_op(logits: torch.Tensor, tokens: torch.Tensor, top: int, temperature: float) -> tuple[
+        torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    # outputs of an op are no views of one another
+    return tuple(t.clone() for t in token_logprobs(logits, tokens, top=top, temperature=temperature))
+
+
+@token_logprobs_op.register_fake
+def _token_logprobs_fake(logits, tokens, top, temperature):
+    T, f = logits.shape[0], torch.float32
+    return (logits.new_empty((T,), dtype=f), logits.new_empty((T,), dtype=f),
+            logits.new_empty((T, top), dtype=f), logits.new_empty((T, top), dtype=torch.int64))
 
 
 class MX4Linear(torch.nn.Module):

@@ -1,0 +1,229 @@
+"""Attention of drafted trees over the cache against a plain 64-bit form."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_14598_amd as w8a8
+from _helpers import say
+from _lm_ref import bit_words, masked_attention, tree_bits, tree_visible
+from _mx_ref import f64
+from test_gpu_kv import Case, _kv
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    yield
+    torch.cuda.synchronize()
+
+
+class Tree(Case):
+    """A cache and queries, and a tree a sequence: parents at random among the nodes before."""
+
+    def __init__(self, *args, words=None, bits=None, **kw):
+        super().__init__(*args, **kw)
+        rng = random.Random(kw.get("seed", 0) + 1)
+        words = words or -(-max(self.qs) // 64)
+        if bits is None:
+            bits = np.concatenate([tree_bits([rng.randrange(-1, i) for i in range(n)], words)
+                                   for n in self.qs])
+        self.bits = bits
+        self.tree = torch.from_numpy(bits).cuda()
+
+    def run(self, q=None, **kw):
+        kw.setdefault("q_starts", self.q_starts)
+        return w8a8.kv_tree_attention(self.q.cuda() if q is None else q, self.cache, self.table.cuda(),
+                                      self.kv_lens, self.tree, fmt=self.fmt, **kw)
+
+    def check(self, y, scale=None, terms=2.0 ** -7):
+        """Within the rounding of the weights and of the output to bf16 (2^-8 of the weighted mean of
+        |v| each)."""
+        scale = self.dim ** -0.5 if scale is None else scale
+        y, q = f64(y), f64(self.q)
+        assert np.isfinite(y).all()
+        at_q = at_k = 0
+        for lq, lk in zip(self.qs, self.kvs):
+            see = tree_visible(self.bits[at_q:at_q + lq], lq, lk)
+            for h in range(self.heads * self.group):
+                kv = self.values[at_k:at_k + lk, :, h // self.group]
+                want, mag = masked_attention(q[at_q:at_q + lq, h], kv[:, 0], kv[:, 1], scale, see)
+                err = np.abs(y[at_q:at_q + lq, h] - want)
+                assert (err <= mag * terms + 1e-30).all(), (lq, lk, h, err.max(), mag.max())
+            at_q, at_k = at_q + lq, at_k + lk
+
+
+TREES = [
+    # dim, heads, group, page, nodes, tokens
+    (128, 2, 4, 16, [1], [1]),
+    (128, 2, 4, 16, [1, 5, 3, 2], [1, 5, 20, 300]),       # no tokens in front of two trees
+    (64, 1, 1, 16, [33, 7], [64, 40]),
+    (192, 3, 3, 48, [12, 1, 20], [60, 48, 220]),
+    (256, 2, 1, 64, [26, 64], [129, 64]),
+    (128, 1, 16, 64, [60, 13], [1000, 31]),
+    (128, 2, 1, 128, [13], [5000]),                       # few rows, several parts
+    (64, 2, 3, 16, [65, 2], [190, 90]),                   # more nodes than a word has bits
+    (256, 1, 1, 64, [100, 17], [301, 300]),
+    (128, 2, 4, 64, [70, 1, 130], [200, 1, 131]),
+    (192, 1, 5, 16, [40], [41]),
+    (128, 1, 4, 16, [300], [1100]),
+    (128, 1, 2, 16, [200], [9000]),                       # many rows, several parts
+    (128, 1, 2, 16, [9, 4, 70], [3, 0, 40]),              # nodes that are not cached
+    (64, 1, 1, 16, [129] * 3 + [1] * 3, [2000, 129, 700, 1, 3000, 64]),
+]
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("case", range(len(TREES)))
+def test_trees(fmt, case):
+    dim, heads, group, page, nodes, kvs = TREES[case]
+    say(f"tree {fmt} {TREES[case]}")
+    c = Tree(fmt, dim, heads, group, page, nodes, kvs, seed=case)
+    y = c.run()
+    c.check(y)
+    assert torch.equal(y, c.run())
+    for mq, mk in ((1, 1), (max(nodes), max(kvs)), (1000, 1 << 20)):
+        c.check(c.run(max_q=mq, max_kv=mk))
+    c.check(c.run(scale=-0.3), scale=-0.3)
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("dim,heads,group,nodes,kvs", [(128, 2, 4, [5, 1, 9], [5, 40, 300]),
+                                                       (64, 1, 3, [100, 70], [2000, 70])])
+def test_a_chain_is_the_causal_rule(fmt, dim, heads, group, nodes, kvs):
+    """Every node on the one before: bit for bit as kv_attention with the causal rule."""
+    bits = np.concatenate([tree_bits(range(-1, n - 1), -(-max(nodes) // 64)) for n in nodes])
+    c = Tree(fmt, dim, heads, group, 16, nodes, kvs, seed=1, bits=bits)
+    y = c.run()
+    assert torch.equal(y, Case.run(c))
+    bits = np.full_like(bits, -1)
+    c = Tree(fmt, dim, heads, group, 16, nodes, kvs, seed=1, bits=bits)
+    assert torch.equal(c.run(), Case.run(c, causal=False))
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("nodes,kvs", [([20], [20]), ([90, 40], [90, 41]), ([30], [12])])
+def test_masks_of_any_kind(fmt, nodes, kvs):
+    """Bits at random, also of later nodes; rows without any: zeros where nothing lies in front of
+    the tree; bits and words past the tree are ignored."""
+    rng = random.Random(5)
+    words = -(-max(nodes) // 64) + 1
+    masks = [rng.getrandbits(64 * words) & rng.getrandbits(64 * words) for _ in range(sum(nodes))]
+    masks[0] = 0
+    masks[7] = 1 << nodes[0] | 1 << 64 * words - 1
+    c = Tree(fmt, 128, 1, 3, 16, nodes, kvs, seed=2, bits=bit_words(masks, words))
+    y = c.run()
+    c.check(y)
+    if kvs[0] <= nodes[0]:
+        assert (y[0] == 0).all() and (y[7] == 0).all()
+    past = c.bits.copy()
+    at = 0
+    for n in nodes:
+        for i in range(at, at + n):
+            for b in range(n, 64 * words):
+                past[i, b // 64] ^= np.int64(np.uint64(1 << b % 64).view(np.int64))
+        at += n
+    c.tree = torch.from_numpy(past).cuda()
+    assert torch.equal(y, c.run())
+
+
+def test_fewer_words_than_nodes():
+    """Nodes past the words are seen by none."""
+    c = Tree("fp8", 128, 1, 2, 16, [100], [150], seed=3)
+    c.bits = np.ascontiguousarray(c.bits[:, :1])
+    c.tree = torch.from_numpy(c.bits).cuda()
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("nodes,kv,node", [(6, 50, 2), (40, 40, 17), (200, 400, 130)])
+def test_nan_nodes_reach_only_who_sees_them(fmt, nodes, kv, node):
+    for part in (0, 1):
+        c = Tree(fmt, 128, 1, 2, 16, [nodes], [kv], seed=7)
+        new = _kv(kv, 1, 128, 8)
+        j = kv - nodes + node
+        new[j, part, 0, 70] = float("nan")
+        pages = c.table[0].tolist()
+        c.write(new, [pages[i // 16] * 16 + i % 16 for i in range(kv)])
+        y = f64(c.run())
+        see = tree_visible(c.bits, nodes, kv)
+        bad = np.zeros(y.shape, bool)
+        bad[see[:, j]] = True
+        if part == 1:
+            bad[:, :, :64], bad[:, :, 96:] = False, False
+        assert np.array_equal(np.isnan(y), bad) and see[:, j].any() and not see[:, j].all()
+        for h in range(2):
+            want, mag = masked_attention(f64(c.q)[:, h], c.values[:, 0, 0], c.values[:, 1, 0], 128 ** -0.5, see)
+            ok = ~see[:, j]
+            assert (np.abs(y[ok, h] - want[ok]) <= mag[ok] * 2.0 ** -7).all()
+
+
+def test_without_starts_strided_queries_and_a_buffer():
+    c = Tree("fp8", 128, 2, 4, 16, [7, 7, 7], [20, 7, 333], seed=4)
+    want = c.run()
+    wide = torch.zeros(21, 20, 128, dtype=torch.bfloat16, device="cuda")
+    wide[:, 7:15] = c.q.cuda()
+    guard = torch.full((23, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y = c.run(q=wide[:, 7:15], q_starts=None, out=guard[1:-1])
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    c.check(y)
+    assert torch.equal(y, want) and (guard[0] == 7).all() and (guard[-1] == 7).all()
+
+
+def test_offsets_beyond_32_bits():
+    page_bytes = w8a8.kv_cache(0, 2, 128, 128, fmt="fp8").shape[1:].numel()
+    c = Tree("fp8", 128, 2, 4, 128, [70, 3], [400, 129], seed=10, base=(1 << 32) // page_bytes + 5)
+    c.check(c.run())
+
+
+def test_graph_replays_with_other_trees():
+    c = Tree("fp8", 128, 2, 4, 16, [20, 20], [700, 40], seed=12)
+    q, table, out = c.q.cuda(), c.table.cuda(), None
+    width = c.table.shape[1] * 16
+    n = w8a8.load_library().w8a8_kv_attention_workspace_bytes(16, 2, 128, 0, 4, 40, 2, 20, width)
+    work = torch.empty(n, dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+
+    def step(o=None, w=None):
+        return w8a8.kv_tree_attention(q, c.cache, table, c.kv_lens, c.tree, q_starts=c.q_starts, max_q=20,
+                                      max_kv=width, out=o, workspace=w)
+    step(out, work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, work)
+    for i in range(3):
+        rng = random.Random(i)
+        c.bits = np.concatenate([tree_bits([rng.randrange(-1, j) for j in range(20)], 1) for _ in range(2)])
+        c.tree.copy_(torch.from_numpy(c.bits))
+        c.kvs = [700 - 16 * i, 40 - i]
+        c.kv_lens.copy_(torch.tensor(c.kvs, dtype=torch.int32))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(got, step())
+        values = c.values
+        c.values = np.concatenate([values[:c.kvs[0]], values[700:700 + c.kvs[1]]])
+        c.check(got)
+        c.values = values
+
+
+def test_binding_refusals():
+    c = Tree("fp8", 128, 2, 4, 16, [5], [50], seed=13)
+    good = c.tree
+    for t in (good[:4], good[:, 0], good.cpu(), good.expand(5, 1)[:, :0], good.repeat(1, 65), good.t()):
+        c.tree = t
+        with pytest.raises(ValueError):
+            c.run()
+    c.tree = good.int()
+    with pytest.raises(TypeError):
+        c.run()
