@@ -387,17 +387,23 @@ size_t w8a8_kv_attention_workspace_bytes(int page, int heads, int dim, int fmt, 
  * order (the nodes of the tree); query i sees every token in front of them, and node n where
  * bit n % 64 of tree[(q_starts[b] + i) * tree_words + n / 64] is set (tree [T, tree_words]; a
  * node sees its ancestors and itself; nodes past 64 * tree_words are seen by none, bits past lq
- * are ignored). tree_words is 1 to W8A8_KV_MAX_TREE_WORDS (else W8A8_ERR_ARG). The workspace is
- * that of w8a8_kv_attention, and so is everything else. */
+ * are ignored). tree_words is 1 to W8A8_KV_MAX_TREE_WORDS (else W8A8_ERR_ARG). The weights are
+ * rounded to one bf16 term (2^-8). q_starts [seqs + 1] may end before T: rows behind the last
+ * sequence are neither read nor written. max_kv is a bound on a sequence's tokens: up to 512 one
+ * launch is enough; with a wrong one the results are the same but for rounding. Everything else is
+ * as there. workspace: w8a8_kv_tree_attention_workspace_bytes(...) bytes, 256-byte aligned (NULL
+ * allowed when that is 0). */
 #define W8A8_KV_MAX_TREE_WORDS 64
 w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
                                    const uint8_t *cache, int64_t pages, int page, int heads,
                                    int dim, int fmt, const int32_t *table, int64_t table_stride,
                                    int table_pages, const int32_t *kv_lens,
                                    const int32_t *q_starts, int64_t T, int seqs, int group,
-                                   float scale, const int64_t *tree, int tree_words, int max_q,
-                                   int max_kv, uint16_t *out, void *workspace,
-                                   size_t workspace_bytes, void *stream);
+                                   float scale, const int64_t *tree, int tree_words, int max_kv,
+                                   uint16_t *out, void *workspace, size_t workspace_bytes,
+                                   void *stream);
+size_t w8a8_kv_tree_attention_workspace_bytes(int page, int heads, int dim, int fmt, int group,
+                                              int64_t T, int seqs, int max_kv);
 
 /* w8a8_kv_write with rotary positions, for the keys and the queries beside them. A head's
  * channels have `pairs` pairs (at most dim / 2): channels p and p + pairs, or 2p and 2p + 1 where

@@ -31,7 +31,7 @@ FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++20", "-fPIC", "-fvisibility=h
          "-Wall", "-Wno-unused-command-line-argument"]
 
 SOURCES = ["quant_rows.hip", "gemm_i8.hip", "mfma_ceiling.hip", "w8a8_api.hip", "mx4_quant.hip",
-           "mx4_gemm.hip", "kv_cache.hip", "kv_append.hip", "kv_attention.hip", "mx_api.hip",
+           "mx4_gemm.hip", "kv_cache.hip", "kv_append.hip", "kv_attention.hip", "kv_tree.hip", "mx_api.hip",
            "norm_quant.hip", "logprobs.hip", "lm_api.hip"]
 
 

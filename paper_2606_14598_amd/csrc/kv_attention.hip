@@ -15,24 +15,12 @@
 // weights are rounded for the second product: to two bf16 terms (2^-16 of each at most) in sequences
 // of few rows, to one (2^-8) in those of many, whose products bind. Each sequence gets the kernel
 // for its own rows, so that its rounding does not hang on the batch or on the caller's bounds.
-#include "../../include/w8a8.h"
-#include "mx_internal.hpp"
-#include "mx_math.hpp"
-#include "quant_math.hpp"
+#include "kv_attention.hpp"
 
 #include <algorithm>
 
 namespace w8a8 {
 namespace {
-
-using namespace mx;
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // How the keys of a launch are divided: a workgroup's share is `share` tokens (a multiple of
 // 128), or what the lengths make of `target` if that is more, or what divides a sequence's tokens
@@ -47,78 +35,13 @@ struct Split {
     uint64_t magic;  // n / (page / 16) = n * magic >> 32 for n < 2^22 (kMaxTokens / 16)
 };
 
-// The maximum that exponents are taken from may lag behind by this much: O and l are rescaled
-// only when a row's maximum rises further. Weights up to 2^8 instead of 1 lose nothing, as
-// float32 sums and bf16 roundings are relative; a rescaling costs as much as a product. 4 x 1000
-// queries on 6000 keys, 18 heads of 256: 783 us rescaling at every rise, 670 so.
-constexpr float kSlack = 8.0f;
-constexpr int kMaxChunk = 4096;
 constexpr int kSplitRows = 16, kTileRows = 128, kTileTokens = 64;
 static_assert(W8A8_KV_MAX_TOKENS / 16 <= 1 << 22 && W8A8_KV_MAX_PAGE / 16 <= 1 << 10, "magic");
-
-struct Seq {
-    int64_t q0;      // first query
-    int lq, kv;
-};
-
-__device__ __forceinline__ Seq sequence(const KvShape &c, const KvAttnArgs &a, int b) {
-    Seq s;
-    if (a.q_starts) {      // kept inside the queries whatever the array holds
-        s.q0 = min(max((int64_t)a.q_starts[b], (int64_t)0), a.T);
-        s.lq = (int)(min((int64_t)a.q_starts[b + 1], a.T) - s.q0);
-    } else {
-        s.lq = (int)(a.T / a.seqs);
-        s.q0 = (int64_t)b * s.lq;
-    }
-    s.kv = min(a.kv_lens[b], a.table_pages * c.page);
-    return s;
-}
 
 // Tokens that query i sees.
 __device__ __forceinline__ int seen(const Seq &s, int i, int causal) {
     return max(0, causal ? min(s.kv, s.kv - s.lq + i + 1) : s.kv);
 }
-
-// Tokens that some query up to i sees, and that every query from i on does. In a tree: all, as any
-// node may see any other, and those in front of it.
-template <bool TREE>
-__device__ __forceinline__ int some_seen(const Seq &s, int i, int causal) {
-    return TREE ? max(0, s.kv) : seen(s, i, causal);
-}
-template <bool TREE>
-__device__ __forceinline__ int all_seen(const Seq &s, int i, int causal) {
-    return TREE ? max(0, s.kv - s.lq) : seen(s, i, causal);
-}
-
-// What a row of a tree sees: the tokens in front of the tree, and nodes by its bits.
-struct TreeRow {
-    const uint32_t *bits;     // nullptr: a row that is none and sees nothing
-    int words, prefix, kv;    // the tree's first token (below 0: its first nodes are not cached)
-    __device__ __forceinline__ TreeRow(const KvAttnArgs &a, const Seq &s, int qi, bool live)
-        : bits(live ? a.tree + (s.q0 + qi) * a.tree_words : nullptr), words(a.tree_words),
-          prefix(s.kv - s.lq), kv(s.kv) {}
-    __device__ __forceinline__ uint32_t word(int i) const { return i < words ? bits[i] : 0; }
-    // Tokens j .. j + 31, the first in the lowest bit.
-    __device__ __forceinline__ uint32_t window(int j) const {
-        if (!bits || j >= kv)
-            return 0;
-        const int node = j - prefix;
-        uint32_t w;
-        if (node <= -32)
-            w = ~0u;
-        else if (node < 0)
-            w = word(0) << -node | ((1u << -node) - 1);
-        else
-            w = (uint32_t)((word(node / 32) | (uint64_t)word(node / 32 + 1) << 32) >> node % 32);
-        return kv - j < 32 ? w & ((1u << (kv - j)) - 1) : w;
-    }
-    __device__ __forceinline__ bool any() const {
-        uint32_t w = 0;
-        for (int j = 0; w == 0 && j < kv; j += 32)
-            w = window(j);
-        return w != 0;
-    }
-};
 
 __device__ __forceinline__ bool mine(const Split &sp, int rows) {
     return rows >= sp.rows_from && rows <= sp.rows_to;
@@ -149,15 +72,6 @@ __device__ __forceinline__ int chunk_of(int share) {
     return ((share + pieces - 1) / pieces + 127) & ~127;
 }
 
-// A row's maximum before its first key: minus infinity where it sees none, else the least finite
-// number. A sum of zero then tells a row without keys (zeros) from one all of whose scores are
-// minus infinity, as a query with an infinity has them (NaN, as exp(-inf - -inf) is).
-__device__ __forceinline__ float start_of(bool sees) { return sees ? -__FLT_MAX__ : -INFINITY; }
-
-__device__ __forceinline__ float inverse(float l, float m) {
-    return l == 0.0f ? (m == -INFINITY ? 0.0f : NAN) : 1.0f / l;
-}
-
 __device__ __forceinline__ float max_of_row(float v) {
     // lanes l, l ^ 16, l ^ 32, l ^ 48 hold the same row
     u32x2 r = __builtin_bit_cast(
@@ -173,69 +87,6 @@ __device__ __forceinline__ bf16x8 ones() {
     return __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
 }
 
-// In a branch that few tiles take: without it the compiler computes both sides in every tile.
-__device__ __forceinline__ void keep_branch() { asm volatile(""); }
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
-}
-
-// Four neighbouring outputs: v times inv. bf16 tensors may begin at any element.
-__device__ __forceinline__ void store_outputs(uint16_t *out, const f32x4 &v, float inv) {
-    *reinterpret_cast<Bytes8 *>(out) =
-        Bytes8{{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)}};
-}
-
-// Element E8 (8 values, four words) of a unit's codes.
-template <int FMT, int E8>
-__device__ __forceinline__ u32x4 decode_part(const u32x4 &codes, float s) {
-    if constexpr (FMT == KV_FP8) {
-        return u32x4{decode8<0>(codes[2 * E8], s), decode8<1>(codes[2 * E8], s),
-                     decode8<0>(codes[2 * E8 + 1], s), decode8<1>(codes[2 * E8 + 1], s)};
-    } else {
-        return u32x4{decode4<0>(codes[E8], s), decode4<1>(codes[E8], s),
-                     decode4<2>(codes[E8], s), decode4<3>(codes[E8], s)};
-    }
-}
-
-template <int N>
-struct Unit;
-template <>
-struct Unit<16> {
-    static __device__ __forceinline__ u32x4 load(const uint8_t *p) {
-        return *reinterpret_cast<const u32x4 *>(p);
-    }
-};
-template <>
-struct Unit<8> {
-    static __device__ __forceinline__ u32x4 load(const uint8_t *p) {
-        const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
-        return u32x4{v[0], v[1], 0, 0};
-    }
-};
-
-// Where the tokens of a chunk lie, 16 at a time: the first one's place in its page, and the
-// page's keys of the head, from which its codes, scales and values follow.
-struct Places {
-    int64_t page[kMaxChunk / 16];
-    int at[kMaxChunk / 16];
-};
-
-// Fills `count` entries from token j_first on; those past token j_end - 1 repeat its block.
-__device__ __forceinline__ void fill_places(Places &pl, const KvShape &c, const KvAttnArgs &a,
-                                            const Split &sp, int b, int head, int j_first, int j_end,
-                                            int count) {
-    const uint32_t last = (uint32_t)(j_end - 1) / 16;
-    const int32_t *table = a.table + b * a.table_stride;
-    for (int i = threadIdx.x; i < count; i += 256) {
-        const uint32_t blk = min((uint32_t)(j_first / 16 + i), last);
-        const uint32_t entry = (uint32_t)(blk * sp.magic >> 32);
-        const int64_t page = min((int64_t)max(table[entry], 0), c.pages - 1);
-        pl.page[i] = (page * 2 * c.heads + head) * c.head_bytes();
-        pl.at[i] = (int)(blk - entry * (uint32_t)(c.page / 16)) * 16;
-    }
-}
-
 // Few rows (16 a workgroup): the keys are divided among workgroups, and among the four
 // wavefronts of each in tiles of 32 tokens; every wavefront keeps its own m, l and O, joined
 // in LDS at the end. Keys go from memory to the matrix registers as they are: lane (t, g) =
@@ -247,7 +98,7 @@ __device__ __forceinline__ void fill_places(Places &pl, const KvShape &c, const 
 // head) at 5.4 TB/s, 16 of 8000 with 18 heads of 256 at 5.6; one of 200000 in e2m1, 8 queries a
 // head, at 4.6 (about 370 instructions for 32 tokens of 4.3 KB); 48 sequences of very different
 // lengths at 4.0 (unequal shares, more workgroups that start).
-template <int FMT, int D, bool TREE>
+template <int FMT, int D>
 __global__ void __launch_bounds__(256, D <= 128 ? 3 : 2)
 kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
     constexpr int KU = FMT == KV_FP4 && D % 128 == 0 ? 32 : 16;   // elements of a key unit
@@ -284,7 +135,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 
     for (int rt = blockIdx.y; rt * kSplitRows < rows; rt += gridDim.y) {
         const int some_see =
-            some_seen<TREE>(seq, (min(rt * kSplitRows + kSplitRows, rows) - 1) / a.group, a.causal);
+            seen(seq, (min(rt * kSplitRows + kSplitRows, rows) - 1) / a.group, a.causal);   // some row
         const int share = max(even, ((some_see + sp.splits - 1) / sp.splits + 127) & ~127);
         const int used = (some_see + share - 1) / share;
         if (split >= max(used, 1))
@@ -295,8 +146,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
         const int qi = live ? row / a.group : 0;
         const int qh = head * a.group + (live ? row % a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
-        const TreeRow tree(a, seq, qi, live);
-        const int all_see = all_seen<TREE>(seq, rt * kSplitRows / a.group, a.causal);   // every live row
+        const int all_see = seen(seq, rt * kSplitRows / a.group, a.causal);   // every live row
         u32x4 q[NK][KU / 8];
         {
             const uint16_t *src = a.q + (seq.q0 + qi) * a.q_token + qh * a.q_head;
@@ -313,7 +163,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x4{};
-        float m = start_of(TREE ? tree.any() : limit > 0);
+        float m = start_of(limit);
         f32x4 sums = {};           // in each element: the sum of a row's weights
         uint32_t row_nan = 0;      // blocks of the row's output that a seen NaN value reaches
 
@@ -322,7 +172,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
             const int j_end = min(j_first + chunk, some_see);
             const int ntile = (j_end - j_first + 31) / 32;
             __syncthreads();       // the places and the LDS rows of what came before are read
-            fill_places(places, c, a, sp, b, head, j_first, j_end, 2 * ntile);
+            fill_places(places, c, a, sp.magic, b, head, j_first, j_end, 2 * ntile);
             __syncthreads();
 
             u32x4 kc[2][NK], vc[NV];
@@ -413,7 +263,6 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 }
                 if (part_seen && __any(any_nan)) {
                     // Rare: which rows see a NaN value, and in which blocks of 32 outputs.
-                    const uint32_t visible = TREE ? tree.window(j0) : 0;
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
                         uint64_t marked = __ballot(vs[i] == 256);
@@ -421,7 +270,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                             const int src = __builtin_ctzll(marked);
                             marked &= marked - 1;
                             const int unit = i * 64 + src;
-                            if (TREE ? visible >> (unit / VT) & 1 : j0 + unit / VT < limit)
+                            if (j0 + unit / VT < limit)
                                 row_nan |= 1u << (unit % VT * VU / 32);
                         }
                     }
@@ -431,14 +280,12 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 
                 if (part_seen) {
                     const int left = limit - j0 - 4 * g;
-                    const uint32_t visible = TREE ? tree.window(j0) >> 4 * g : 0;
                     keep_branch();
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            s[h][e] = (TREE ? visible >> (16 * h + e) & 1 : 16 * h + e < left) ? s[h][e]
-                                                                                               : -INFINITY;
+                            s[h][e] = 16 * h + e < left ? s[h][e] : -INFINITY;
                 }
                 float top = -INFINITY;
 #pragma unroll
@@ -557,19 +404,6 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
     }
 }
 
-// Barrier that orders LDS only: loads from memory stay in flight across it.
-__device__ __forceinline__ void lds_barrier() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
-// The other half's value beside this one's: lanes l and l ^ 32 hold the same row.
-__device__ __forceinline__ u32x2 both_halves(float v) {
-    return __builtin_bit_cast(
-        u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
-}
-
 // Many rows (128 a workgroup, 32 a wavefront): 64 tokens at a time are decoded once into LDS
 // for all four wavefronts, between the products of the 64 before; 32x32x16 products with the
 // rows as columns, as above. Keys lie in rows of 2 D + 16 bytes, values in rows of 2 D + 64, which
@@ -592,7 +426,7 @@ __device__ __forceinline__ u32x2 both_halves(float v) {
 // tiles, 670 and 382 so.
 constexpr int kSpreadUnits = 32;
 
-template <int FMT, int D, bool TREE>
+template <int FMT, int D>
 __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1)
 kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     constexpr int TT = kTileTokens;
@@ -638,7 +472,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
     // Row tiles first_rt, first_rt + tiles, ...: more than one only where the grid has fewer.
     for (int rt = first_rt; rt <= last_rt; rt += tiles) {
         const int some_see =
-            some_seen<TREE>(seq, (min(rt * kTileRows + kTileRows, rows) - 1) / a.group, a.causal);
+            seen(seq, (min(rt * kTileRows + kTileRows, rows) - 1) / a.group, a.causal);   // some row
         const int share = max(even, ((some_see + sp.splits - 1) / sp.splits + 127) & ~127);
         const int used = (some_see + share - 1) / share;
         if (split >= max(used, 1))
@@ -649,12 +483,11 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
         const int qi = live ? row / a.group : 0;
         const int qh = head * a.group + (live ? row - qi * a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
-        const TreeRow tree(a, seq, qi, live);
-        const int all_see = all_seen<TREE>(seq, rt * kTileRows / a.group, a.causal);
+        const int all_see = seen(seq, rt * kTileRows / a.group, a.causal);
         // what some row of this wavefront sees
         const int wave_first = rt * kTileRows + wave * 32;
         const int wave_sees =
-            wave_first < rows ? some_seen<TREE>(seq, (min(wave_first + 32, rows) - 1) / a.group, a.causal) : 0;
+            wave_first < rows ? seen(seq, (min(wave_first + 32, rows) - 1) / a.group, a.causal) : 0;
         u32x4 q[KS];
         {
             const uint16_t *src = a.q + (seq.q0 + qi) * a.q_token + qh * a.q_head + 8 * h;
@@ -668,7 +501,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x16{};
-        float m = start_of(TREE ? tree.any() : limit > 0), l = 0.0f;
+        float m = start_of(limit), l = 0.0f;
         uint32_t row_nan = 0;
 
         for (int ch = split; ch < nch; ch += used) {
@@ -678,7 +511,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
             __syncthreads();
             if (threadIdx.x == 0)
                 nan_any = 0;
-            fill_places(places, c, a, sp, b, head, j_first, j_end, ntile * (TT / 16));
+            fill_places(places, c, a, sp.magic, b, head, j_first, j_end, ntile * (TT / 16));
             __syncthreads();
 
             u32x4 kc[NU], vc[NU];
@@ -750,14 +583,10 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
                 lds_barrier();       // this tile is staged, the other stage's last one is read
                 if (partly_seen(j0 + TT) && tile + 1 < ntile)
                     mark(j0 + TT, st ^ 1);
-                if (part_seen && nan_any) {    // rare: which rows see a NaN block
-                    const uint64_t visible =
-                        TREE ? tree.window(j0) | (uint64_t)tree.window(j0 + 32) << 32 : 0;
+                if (part_seen && nan_any)      // rare: which rows see a NaN block
                     for (int unit = 0; unit < UNITS; ++unit)
-                        if (nan_unit[st][unit] &&
-                            (TREE ? visible >> (unit / VT) & 1 : j0 + unit / VT < limit))
+                        if (nan_unit[st][unit] && j0 + unit / VT < limit)
                             row_nan |= 1u << (unit % VT * VU / 32);
-                }
                 // Scores: token 32 t + 8 (i / 4) + 4 h + i % 4 in s[t][i]. Between the products
                 // the next tile is staged (after the last tile: itself again, unread).
                 f32x16 s[2] = {f32x16{}, f32x16{}};
@@ -792,20 +621,12 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 
                 if (part_seen) {
                     const int left = limit - j0 - 4 * h;
-                    uint32_t visible[2] = {};
-                    if constexpr (TREE) {
-                        visible[0] = tree.window(j0) >> 4 * h;
-                        visible[1] = tree.window(j0 + 32) >> 4 * h;
-                    }
                     keep_branch();
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            s[t][i] = (TREE ? visible[t] >> (8 * (i / 4) + i % 4) & 1
-                                            : 32 * t + 8 * (i / 4) + i % 4 < left)
-                                          ? s[t][i]
-                                          : -INFINITY;
+                            s[t][i] = 32 * t + 8 * (i / 4) + i % 4 < left ? s[t][i] : -INFINITY;
                 }
                 float top = -INFINITY;
 #pragma unroll
@@ -1081,7 +902,7 @@ Plan plan_of(const KvShape &c, int64_t T, int seqs, int group, int max_q, int ma
     return p;
 }
 
-template <int FMT, int D, bool TREE>
+template <int FMT, int D>
 hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, hipStream_t s) {
     const int64_t rows = a.T * c.heads * a.group;
     const auto run = [&](bool many, Split &sp, int64_t most_rows) {
@@ -1092,7 +913,7 @@ hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, h
             if (!launchable(units, 256))
                 return hipErrorInvalidValue;
             const dim3 grid((unsigned)units, (unsigned)((most_rows + kSplitRows - 1) / kSplitRows));
-            hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D, TREE>), grid, dim3(256), 0, s, c, a, sp);
+            hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D>), grid, dim3(256), 0, s, c, a, sp);
             return hipGetLastError();
         }
         // A workgroup goes on to every tiles-th row tile, so that a loose max_q costs empty
@@ -1102,7 +923,7 @@ hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, h
                                        std::max<int64_t>(kMostGroups / columns, 1));
         if (!launchable(columns * tiles, 256))
             return hipErrorInvalidValue;
-        hipLaunchKernelGGL((kv_attention_tile_kernel<FMT, D, TREE>), dim3((unsigned)(columns * tiles)),
+        hipLaunchKernelGGL((kv_attention_tile_kernel<FMT, D>), dim3((unsigned)(columns * tiles)),
                            dim3(256), 0, s, c, a, sp, (int)tiles);
         return hipGetLastError();
     };
@@ -1132,9 +953,7 @@ hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, 
         return hipErrorInvalidValue;
     Plan p = plan_of(c, a.T, a.seqs, a.group, a.max_q, a.max_kv);
     const auto run = [&](auto dim, auto format) {
-        constexpr int F = decltype(format)::value, D = decltype(dim)::value;
-        return a.tree ? run_plan<F, D, true>(c, a, p, static_cast<float *>(ws), s)
-                      : run_plan<F, D, false>(c, a, p, static_cast<float *>(ws), s);
+        return run_plan<decltype(format)::value, decltype(dim)::value>(c, a, p, static_cast<float *>(ws), s);
     };
     const auto go = [&](auto dim) {
         return c.fmt == KV_FP8 ? run(dim, std::integral_constant<int, KV_FP8>{})

@@ -96,7 +96,6 @@ w8a8_status w8a8_token_logprobs(const void *logits, int f32, int64_t row_stride,
     a.tokens = tokens;
     a.top = top;
     a.factor = 1.44269504088896341f / temperature;
-    a.inverse = 1.0 / (double)temperature;
     a.logp = logp;
     a.entropy = entropy;
     a.top_logp = top_logp;

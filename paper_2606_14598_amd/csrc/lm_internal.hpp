@@ -46,7 +46,6 @@ struct LogprobArgs {
     const int64_t *tokens;          // [T]
     int top;
     float factor;                   // log2(e) / temperature
-    double inverse;                 // 1 / temperature
     float *logp, *entropy;          // [T]
     float *top_logp;                // [T, top]
     int64_t *top_ids;               // [T, top]

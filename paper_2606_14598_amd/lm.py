@@ -53,7 +53,7 @@ def rms_norm_quantize(x, weight=None, *, residual=None, eps: float = 1e-6, fmt: 
     _same_device(x, weight, residual)
     if fmt == "int8":
         name = "w8a8_rms_norm_quantize"
-        codes = torch.empty((M, K), dtype=torch.int8, device=device)
+        codes = torch.empty_like(x, dtype=torch.int8)
         scales = torch.empty(M, dtype=torch.float32, device=device)
     else:
         name = "w8a8_rms_norm_mx4_quantize"
@@ -87,10 +87,9 @@ def token_logprobs(logits, tokens, *, top: int = 0, temperature: float = 1.0, wo
     top = int(top)
     if not 0 <= top <= min(MAX_TOP, V):
         raise ValueError(f"top must be 0 to {min(MAX_TOP, V)}, got {top}")
-    # one allocation for the three: logp, entropy, top_logp
-    values = torch.empty(T * (2 + top), dtype=torch.float32, device=device)
-    logp, entropy, top_logp = values[:T], values[T:2 * T], values[2 * T:].view(T, top)
-    ids = torch.empty((T, top), dtype=torch.int64, device=device)
+    logp = torch.empty_like(tokens, dtype=torch.float32)
+    entropy = torch.empty_like(logp)
+    top_logp, ids = logp.new_empty((T, top)), tokens.new_empty((T, top))
     ws = _workspace(_bytes("w8a8_token_logprobs_workspace_bytes", T, V, top), device, workspace)
     _launch(device, "w8a8_token_logprobs", logits.data_ptr(), int(logits.dtype == torch.float32),
             logits.stride(0), T, V, _ptr(tokens), top, temperature, logp.data_ptr(),

@@ -303,7 +303,9 @@ def kv_tree_attention(q, cache, block_table, kv_lens, tree, *, fmt: str = "fp8",
     queries are the nodes of a tree, its last cached tokens, in order; all of them see the tokens in
     front of the tree, and query i of a sequence sees node n where bit n % 64 of
     tree[q_starts[b] + i, n // 64] is set: itself and its ancestors (tree int64 [T, words], up to
-    64 words). A query that sees nothing gives zeros. Everything else is as in kv_attention."""
+    64 words). A query that sees nothing gives zeros. The weights are rounded to one bf16 term.
+    q_starts may end before T: rows of q and the output behind the last sequence are neither read nor
+    written. max_kv as in kv_attention; max_q makes no difference here. Everything else is as there."""
     if not isinstance(tree, torch.Tensor) or tree.dtype != torch.int64:
         raise TypeError("tree must be an int64 torch.Tensor")
     return _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, False, tree, max_q, max_kv,
@@ -348,13 +350,15 @@ def _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, causal, tree, 
     if T == 0:
         return y
     group = q_heads // heads
-    nws = _bytes("w8a8_kv_attention_workspace_bytes", page, heads, dim, f, group, T, B,
-                max_q, max_kv)
+    at = (_ptr(q), q.stride(0), q.stride(1), _ptr(cache), pages, page, heads, dim, f, _ptr(block_table),
+          block_table.stride(0), width, _ptr(kv_lens), _ptr(q_starts), T, B, group,
+          dim ** -0.5 if scale is None else float(scale))
+    if tree is None:
+        nws = _bytes("w8a8_kv_attention_workspace_bytes", page, heads, dim, f, group, T, B, max_q, max_kv)
+        name, rule = "w8a8_kv_attention", (int(causal), max_q, max_kv)
+    else:
+        nws = _bytes("w8a8_kv_tree_attention_workspace_bytes", page, heads, dim, f, group, T, B, max_kv)
+        name, rule = "w8a8_kv_tree_attention", (_ptr(tree), tree.shape[1], max_kv)
     ws = _workspace(nws, device, workspace)
-    rule = (int(causal),) if tree is None else (_ptr(tree), tree.shape[1])
-    _launch(device, "w8a8_kv_attention" if tree is None else "w8a8_kv_tree_attention", _ptr(q),
-            q.stride(0), q.stride(1), _ptr(cache), pages, page, heads, dim, f, _ptr(block_table),
-            block_table.stride(0), width, _ptr(kv_lens), _ptr(q_starts), T, B, group,
-            dim ** -0.5 if scale is None else float(scale), *rule, max_q, max_kv, _ptr(y), _ptr(ws),
-            0 if ws is None else ws.nbytes)
+    _launch(device, name, *at, *rule, _ptr(y), _ptr(ws), 0 if ws is None else ws.nbytes)
     return y

@@ -235,8 +235,7 @@ def _rms_norm_quantize_fake(x, weight, residual, eps, fmt):
 @torch.library.custom_op("w8a8::token_logprobs", mutates_args=())
 def token_logprobs_op(logits: torch.Tensor, tokens: torch.Tensor, top: int, temperature: float) -> tuple[
         torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
-    # outputs of an op are no views of one another
-    return tuple(t.clone() for t in token_logprobs(logits, tokens, top=top, temperature=temperature))
+    return token_logprobs(logits, tokens, top=top, temperature=temperature)
 
 
 @token_logprobs_op.register_fake

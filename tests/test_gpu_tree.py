@@ -95,14 +95,44 @@ def test_trees(fmt, case):
 @pytest.mark.parametrize("dim,heads,group,nodes,kvs", [(128, 2, 4, [5, 1, 9], [5, 40, 300]),
                                                        (64, 1, 3, [100, 70], [2000, 70])])
 def test_a_chain_is_the_causal_rule(fmt, dim, heads, group, nodes, kvs):
-    """Every node on the one before: bit for bit as kv_attention with the causal rule."""
-    bits = np.concatenate([tree_bits(range(-1, n - 1), -(-max(nodes) // 64)) for n in nodes])
-    c = Tree(fmt, dim, heads, group, 16, nodes, kvs, seed=1, bits=bits)
+    """Every node on the one before: what kv_attention gives with the causal rule; masks of all
+    nodes: without it. Both are within 2^-7 of the weighted mean of |v| of the exact values."""
+    for causal, bits in ((True, np.concatenate([tree_bits(range(-1, n - 1), -(-max(nodes) // 64)) for n in nodes])),
+                         (False, np.full((sum(nodes), -(-max(nodes) // 64)), -1))):
+        c = Tree(fmt, dim, heads, group, 16, nodes, kvs, seed=1, bits=bits)
+        y = c.run()
+        c.check(y)
+        Case.check(c, y, causal=causal)
+        Case.check(c, Case.run(c, causal=causal), causal=causal)
+
+
+def test_rows_behind_the_last_sequence():
+    """q_starts that end before T: the rest of the output is left as it was, whatever the queries
+    there hold; also where the keys are divided."""
+    for nodes, kvs in (([9, 30], [40, 300]), ([20, 70], [3000, 5000])):
+        c = Tree("fp8", 128, 2, 4, 16, nodes, kvs, seed=6)
+        want = c.run()
+        n = sum(nodes)
+        q = torch.full((n + 50, 8, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+        q[:n] = c.q.cuda()
+        c.tree = torch.cat((c.tree, torch.full((50, c.tree.shape[1]), -1, device="cuda")))
+        out = torch.full_like(q, 7.0)
+        c.run(q=q, out=out)
+        c.check(out[:n])
+        assert (out[n:] == 7).all() and torch.allclose(out[:n].float(), want.float(), rtol=2 ** -6, atol=2 ** -6)
+
+
+@pytest.mark.parametrize("seqs", [70, 600])
+def test_many_sequences(seqs):
+    """More sequences than a wavefront sums at once, and than it sums at all; some without nodes."""
+    rng = random.Random(seqs)
+    nodes = [rng.choice([0, 1, 3, 9, 40]) for _ in range(seqs)]
+    kvs = [n + rng.choice([0, 1, 50, 300]) for n in nodes]
+    kvs[1] += 9000
+    c = Tree("fp8", 64, 2, 3, 16, nodes, kvs, seed=8, words=1)
     y = c.run()
-    assert torch.equal(y, Case.run(c))
-    bits = np.full_like(bits, -1)
-    c = Tree(fmt, dim, heads, group, 16, nodes, kvs, seed=1, bits=bits)
-    assert torch.equal(c.run(), Case.run(c, causal=False))
+    c.check(y)
+    assert torch.equal(y, c.run())
 
 
 @pytest.mark.parametrize("fmt", ["fp8", "fp4"])
@@ -188,7 +218,7 @@ def test_graph_replays_with_other_trees():
     c = Tree("fp8", 128, 2, 4, 16, [20, 20], [700, 40], seed=12)
     q, table, out = c.q.cuda(), c.table.cuda(), None
     width = c.table.shape[1] * 16
-    n = w8a8.load_library().w8a8_kv_attention_workspace_bytes(16, 2, 128, 0, 4, 40, 2, 20, width)
+    n = w8a8.load_library().w8a8_kv_tree_attention_workspace_bytes(16, 2, 128, 0, 4, 40, 2, width)
     work = torch.empty(n, dtype=torch.uint8, device="cuda")
     out = torch.empty_like(q)
 
