@@ -12,9 +12,9 @@
 // of a head and sequence, and a part of its keys) are numbered one after the other, about as many
 // as the card runs at once, each of about the same cost; a workgroup finds the piece of its own
 // number by a scan over the sequences. Partial results lie in the pieces' own slots of the workspace,
-// and a second launch joins those of a row tile, found by the same scan. So everything follows from
-// the lengths on the device, no row outside the sequences is read or written, and sums have a fixed
-// order.
+// and a second launch joins those of each row tile, whose first piece has left a note where they are.
+// So everything follows from the lengths on the device, no row outside the sequences is read or
+// written, and sums have a fixed order.
 #include "kv_attention.hpp"
 
 #include <algorithm>
@@ -23,13 +23,24 @@ namespace w8a8 {
 namespace {
 
 constexpr int kRows = 128, kTokens = 64;       // of a row tile, and staged at a time
+constexpr int kMostTiles = 1 << 20;            // counted of a sequence: far more than run at once
 // Sequences over whose tokens a wavefront sums, 64 at a time; with more of them keys stay whole.
 constexpr int kSummed = 512;
+
+// Where the pieces of a row tile are.
+struct Note {
+    int b, head, tile;
+    int used;          // pieces; of the first note: the row tiles of the call
+    int slot, stride;  // of the tile's first piece, and from one to the next
+    int pad[2];
+};
 
 struct TreePlan {
     int target;        // pieces that the keys are divided for, 0: every row tile is one
     int least;         // tokens of a piece at least (a multiple of 64)
     int grid;          // pieces there can be
+    int tiles;         // row tiles there can be
+    struct Note *notes;   // [1 + tiles]: the number of row tiles, then each of them
     float *part;       // [grid][kRows][dim + 4]: O, m, l of a piece
     uint64_t magic;    // n / (page / 16) = n * magic >> 32 for n < 2^22
 };
@@ -57,101 +68,152 @@ struct TreeRow {
         return kv - j < 32 ? w & ((1u << (kv - j)) - 1) : w;
     }
     __device__ __forceinline__ bool any() const {
-        uint32_t w = 0;
+        uint32_t w = bits && prefix > 0;       // else at most as many tokens as nodes
+        if (!bits)
+            return false;
         for (int j = 0; w == 0 && j < kv; j += 32)
             w = window(j);
         return w != 0;
     }
 };
 
-// A piece, or a row tile with all of its pieces.
 struct Job {
     bool found;
+    Note note;
+    int number, split; // of its row tile in the call, and of the piece in that
     Seq seq;
-    int b, head, tile, split;
-    int used;          // pieces of a row tile of this sequence
-    int slot, stride;  // of the tile's first piece, and from one to the next
 };
 
 // Eighths of the cost of a full row tile: up to half as many rows take products of half the size,
 // but the same staging (measured).
-__device__ __forceinline__ int eighths(int rows) { return rows <= kRows / 2 ? 5 : 8; }
+__device__ __forceinline__ int eighths(int rows) { return rows <= kRows / 2 ? 6 : 8; }
 
-// Job number `index` of the call's pieces, or (WHOLE) of its row tiles.
-template <bool WHOLE>
+__device__ __forceinline__ int rows_of(const KvAttnArgs &a, const Seq &s) { return max(s.lq, 0) * a.group; }
+__device__ __forceinline__ int tiles_of(int rows) { return (rows + kRows - 1) / kRows; }
+
+// Pieces of a row tile of a sequence. share: their cost, in eighths of a token of a full tile.
+__device__ __forceinline__ int used_of(const TreePlan &plan, int kv, int rows, float share) {
+    if (plan.target == 0 || kv <= plan.least)
+        return 1;
+    const float tokens = fmaxf(share * (rows <= kRows / 2 ? 1.0f / 6.0f : 0.125f), (float)plan.least);
+    return min((int)ceilf((float)kv * __builtin_amdgcn_rcpf(tokens)), (kv + plan.least - 1) / plan.least);
+}
+
+// Sums over the lanes up to each, in DPP operands (a shuffle goes through LDS).
+template <typename V>
+__device__ __forceinline__ V lanes_scan(V v) {
+    const auto step = [&](auto ctrl, auto rows) {
+        const int x = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value,
+                                                  decltype(rows)::value, 0xF, true);
+        v += __builtin_bit_cast(V, x);
+    };
+    using std::integral_constant;
+    step(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});   // row_shr:1
+    step(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});   // row_shr:2
+    step(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});   // row_shr:4
+    step(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});   // row_shr:8
+    step(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});   // row_bcast:15, rows 1, 3
+    step(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});   // row_bcast:31, rows 2, 3
+    return v;
+}
+
+__device__ __forceinline__ float last_lane(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+
+// The cost of a piece: the call's divided by the target, rounded up to the least that makes no more
+// pieces than the target (what runs at once), up to half as much again: one sequence of 9.1 shares
+// makes 10 pieces a row tile, and the last of them a second round. Where none does, as with many
+// row tiles of very different lengths, three quarters of it: the rounds then even out. With up to 64
+// sequences, a lane each. Sums have a fixed order: the same result in every workgroup.
+__device__ __forceinline__ float share_of(const KvShape &c, const TreePlan &plan, int seqs, float sum,
+                                          int kv, int rows) {
+    const float even = last_lane(lanes_scan(sum)) * (float)c.heads * __builtin_amdgcn_rcpf((float)plan.target);
+    if (seqs <= 64) {
+        const int tiles = tiles_of(rows), most = plan.target / c.heads;
+        if (qmath::wave_sum(min(tiles, kMostTiles)) <= most)
+            for (int n = 8; n <= 12; ++n) {
+                const float share = even * (float)n * 0.125f;
+                if (qmath::wave_sum(min(tiles * used_of(plan, kv, rows, share), kMostTiles)) <= most)
+                    return share;
+            }
+    }
+    return even * 0.75f;
+}
+
+// Piece number `index` of the call.
 __device__ __forceinline__ Job find_job(const KvShape &c, const KvAttnArgs &a, const TreePlan &plan,
                                         int index) {
     const int lane = threadIdx.x & 63;
-    const auto rows_of = [&](const Seq &s) { return max(s.lq, 0) * a.group; };
-    const auto tiles_of = [&](int rows) { return (rows + kRows - 1) / kRows; };
-    // The share of a piece, in eighths of a token of a full tile. Float32 in a fixed order: the same
-    // in every workgroup.
+    // the first 64 sequences stay in registers
+    int kv = 0, rows = 0;
+    const auto fetch = [&](int i) {
+        kv = rows = 0;
+        if (i < a.seqs) {
+            const Seq s = sequence(c, a, i);
+            kv = max(s.kv, 0);
+            rows = rows_of(a, s);
+        }
+    };
     float share = 0.0f;
     if (plan.target > 0) {
-        for (int i = lane; i < a.seqs; i += 64) {
-            const Seq s = sequence(c, a, i);
-            const int rows = rows_of(s);
-            share += (float)max(s.kv, 0) * (float)(tiles_of(rows) * eighths(rows));
+        for (int i0 = (a.seqs - 1) / 64 * 64; i0 >= 0; i0 -= 64) {
+            fetch(i0 + lane);
+            share += (float)kv * (float)(tiles_of(rows) * eighths(rows));
         }
-#pragma unroll
-        for (int d = 32; d > 0; d /= 2)
-            share += __shfl_xor(share, d);
-        share *= (float)c.heads / (float)plan.target;
+        share = share_of(c, plan, a.seqs, share, kv, rows);
+    } else {
+        fetch(lane);
     }
     Job job;
     job.found = false;
-    int pieces = 0, jobs = 0;              // in front of the 64 sequences at hand
+    int pieces = 0, numbers = 0;           // in front of the 64 sequences at hand
     for (int i0 = 0; i0 < a.seqs; i0 += 64) {
-        const int i = i0 + lane;
-        int used = 0, tiles = 0;
-        if (i < a.seqs) {
-            const Seq s = sequence(c, a, i);
-            const int rows = rows_of(s);
-            tiles = tiles_of(rows);
-            used = 1;
-            if (plan.target > 0 && s.kv > plan.least) {
-                const float tokens = fmaxf(share / (float)eighths(rows), (float)plan.least);
-                used = min((int)ceilf((float)s.kv / tokens), (s.kv + plan.least - 1) / plan.least);
-            }
-        }
+        if (i0 > 0)
+            fetch(i0 + lane);
+        const int tiles = tiles_of(rows), used = tiles > 0 ? used_of(plan, kv, rows, share) : 0;
         // what comes to more than a grid is some malformed array's: counted as one past it
         const int most = plan.grid + 1;
-        const int own = (int)min((int64_t)c.heads * tiles * used, (int64_t)most);
-        const int own_jobs = WHOLE ? (int)min((int64_t)c.heads * tiles, (int64_t)most) : own;
-        int sum = own, sum_jobs = own_jobs;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int x = __shfl_up(sum, d), y = __shfl_up(sum_jobs, d);
-            if (lane >= d) {
-                sum += x;
-                sum_jobs += y;
-            }
-        }
-        const uint64_t past = __ballot(jobs + sum_jobs > index);
+        const int own_tiles = (int)min((int64_t)c.heads * tiles, (int64_t)most);
+        const int own = (int)min((int64_t)own_tiles * used, (int64_t)most);
+        const int sum = lanes_scan(own), sum_tiles = lanes_scan(own_tiles);
+        const uint64_t past = __ballot(pieces + sum > index);
         if (past) {
             const int at = __builtin_ctzll(past);
             const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+            const int first = pieces + of(sum - own);
+            uint32_t in = index - first;
             job.found = true;
-            job.b = i0 + at;
-            job.seq = sequence(c, a, job.b);
-            job.used = of(used);
-            job.stride = c.heads * of(tiles);
-            int in = index - jobs - of(sum_jobs - own_jobs);
-            job.split = 0;
-            if constexpr (!WHOLE) {
-                job.split = in / job.stride;
-                in -= job.split * job.stride;
-            }
+            job.note.b = i0 + at;
+            job.note.used = of(used);
+            job.note.stride = of(own_tiles);
+            job.split = in / (uint32_t)job.note.stride;
+            in -= job.split * job.note.stride;
             // heads fastest: the row tiles of a head go to one XCD where heads come in eights
-            job.tile = in / c.heads;
-            job.head = in - job.tile * c.heads;
-            job.slot = pieces + of(sum - own) + in;
+            job.note.tile = in / (uint32_t)c.heads;
+            job.note.head = in - job.note.tile * c.heads;
+            job.note.slot = first + in;
+            job.number = numbers + of(sum_tiles - own_tiles) + in;
+            job.seq = sequence(c, a, job.note.b);
             return job;
         }
         pieces = min(pieces + __builtin_amdgcn_readlane(sum, 63), most);
-        jobs = min(jobs + __builtin_amdgcn_readlane(sum_jobs, 63), most);
+        numbers = min(numbers + __builtin_amdgcn_readlane(sum_tiles, 63), most);
     }
     return job;
+}
+
+// All row tiles of the call: what find_job counts, to its end.
+__device__ __forceinline__ int count_tiles(const KvShape &c, const KvAttnArgs &a, const TreePlan &plan) {
+    int n = 0;
+    for (int i0 = 0; i0 < a.seqs; i0 += 64) {
+        int tiles = 0;
+        if (i0 + (int)(threadIdx.x & 63) < a.seqs)
+            tiles = tiles_of(rows_of(a, sequence(c, a, i0 + (threadIdx.x & 63))));
+        tiles = (int)min((int64_t)c.heads * tiles, (int64_t)plan.tiles);
+        n = min(n + __builtin_amdgcn_readlane(lanes_scan(tiles), 63), plan.tiles);
+    }
+    return n;
 }
 
 // The other half's value beside this one's: lanes l and l ^ 32 hold the same row.
@@ -182,17 +244,24 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
     __shared__ uint32_t other_nan[2][64];
     static_assert(sizeof(keys) >= 2 * 64 * (D / 2) * sizeof(float), "O of two wavefronts");
 
-    const Job job = find_job<false>(c, a, plan, blockIdx.x);
+    if (blockIdx.x == 0 && plan.target > 0) {
+        const int n = count_tiles(c, a, plan);
+        if (threadIdx.x == 0)
+            plan.notes[0].used = n;
+    }
+    const Job job = find_job(c, a, plan, blockIdx.x);
     if (!job.found)
         return;
+    if (plan.target > 0 && job.split == 0 && threadIdx.x == 0 && job.number < plan.tiles)
+        plan.notes[1 + job.number] = job.note;
     const Seq seq = job.seq;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r32 = lane & 31, h = lane >> 5;
-    const int rows = seq.lq * a.group, q_heads = c.heads * a.group, head = job.head;
+    const int rows = seq.lq * a.group, q_heads = c.heads * a.group, head = job.note.head;
     const int64_t v_offset = c.heads * c.head_bytes();
     const int kv = max(seq.kv, 0);
-    const int per = ((kv + job.used - 1) / job.used + TT - 1) / TT * TT;
+    const int per = ((kv + job.note.used - 1) / job.note.used + TT - 1) / TT * TT;
     const int piece_first = min(job.split * per, kv), piece_end = min(piece_first + per, kv);
     const int all_see = max(0, seq.kv - seq.lq);       // tokens that every row sees
 
@@ -200,7 +269,7 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
         constexpr int RG = decltype(groups)::value, TG = 4 / RG;      // of rows, of tokens
         constexpr int NS = 2 / TG, US = 4 / TG;        // fragments of 32 keys, steps of 16 values
         const int rg = wave % RG, tg = wave / RG;
-        const int first_row = job.tile * kRows + rg * 32, row = first_row + r32;
+        const int first_row = job.note.tile * kRows + rg * 32, row = first_row + r32;
         const bool live = row < rows, wave_live = first_row < rows;
         const int qi = live ? row / a.group : 0;
         const int qh = head * a.group + (live ? row - qi * a.group : 0);
@@ -227,7 +296,7 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
             __syncthreads();
             if (threadIdx.x == 0)
                 nan_any = 0;
-            fill_places(places, c, a, plan.magic, job.b, head, j_first, j_end, ntile * (TT / 16));
+            fill_places(places, c, a, plan.magic, job.note.b, head, j_first, j_end, ntile * (TT / 16));
             __syncthreads();
 
             u32x4 kc[NU], vc[NU];
@@ -468,8 +537,8 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
             return;
         const int64_t out_row = (seq.q0 + qi) * q_heads + qh;
         const float inv = inverse(l, m);
-        const int64_t slot = job.slot + (int64_t)job.split * job.stride;
-        float *const part = plan.part + (slot * kRows + row - job.tile * kRows) * (D + 4);
+        const int64_t slot = job.note.slot + (int64_t)job.split * job.note.stride;
+        float *const part = plan.part + (slot * kRows + row - job.note.tile * kRows) * (D + 4);
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             const bool nan = row_nan >> f & 1;
@@ -479,59 +548,99 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
                 f32x4 v = {o[f][i], o[f][i + 1], o[f][i + 2], o[f][i + 3]};
                 if (nan)
                     v = f32x4{NAN, NAN, NAN, NAN};
-                if (job.used == 1)
+                if (job.note.used == 1)
                     store_outputs(a.out + out_row * D + d, v, inv);
                 else
                     *reinterpret_cast<f32x4 *>(part + d) = v;
             }
         }
-        if (job.used > 1 && h == 0) {
-            part[D] = m;
-            part[D + 1] = l;
-        }
+        if (job.note.used > 1 && h == 0)
+            *reinterpret_cast<f32x4 *>(part + D) = f32x4{m, l, 0.0f, 0.0f};
     };
-    if (rows - job.tile * kRows <= kRows / 2)
+    if (rows - job.note.tile * kRows <= kRows / 2)
         run(std::integral_constant<int, 2>{});
     else
         run(std::integral_constant<int, 4>{});
 }
 
-// Joins the pieces of a row tile with weights 2^(m_s - max m): D / 4 lanes a row, blockIdx.y a
-// quarter of the tile.
-constexpr int kJoinParts = 4;
+// Joins the pieces of a row tile with weights 2^(m_s - max m): D / 4 lanes hold a row's outputs. Few
+// pieces: a row a group of lanes; many: the groups take a row's pieces in turn and meet in LDS.
+// gridDim.y workgroups share a tile's rows.
+constexpr int kFewPieces = 16;
+
+struct Part {
+    float m, l;
+    f32x4 v;
+    // piece p of a row, outputs d .. d + 3
+    __device__ __forceinline__ void add(const float *p, int dim, int d) {
+        const f32x4 ml = *reinterpret_cast<const f32x4 *>(p + dim);
+        add(ml[0], ml[1], *reinterpret_cast<const f32x4 *>(p + d));
+    }
+    __device__ __forceinline__ void add(float m2, float l2, const f32x4 &v2) {
+        const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
+        const float keep = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(m2 - base);
+        m = top;
+        l = l * keep + l2 * w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = v[e] * keep + v2[e] * w;
+    }
+};
 
 template <int D>
 __global__ void __launch_bounds__(256)
 kv_tree_join_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
-    constexpr int LANES = D / 4, ROWS = 256 / LANES;
-    const Job job = find_job<true>(c, a, plan, blockIdx.x);
-    if (!job.found || job.used == 1)
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ f32x4 other_v[GROUPS][LANES];
+    __shared__ float other_m[GROUPS], other_l[GROUPS];
+    const Note job = plan.notes[1 + blockIdx.x];
+    if ((int)blockIdx.x >= plan.notes[0].used || job.used <= 1 ||
+        job.slot + (int64_t)(job.used - 1) * job.stride >= plan.grid)
         return;
-    const int lane = threadIdx.x % LANES, first = threadIdx.x / LANES, d = 4 * lane;
-    const int rows = min(job.seq.lq * a.group - job.tile * kRows, kRows), q_heads = c.heads * a.group;
-    const int used = job.slot + (int64_t)(job.used - 1) * job.stride < plan.grid ? job.used : 0;
-    if (first >= ROWS)
-        return;
-    for (int r = blockIdx.y * ROWS + first; r < rows; r += kJoinParts * ROWS) {
-        const float *p = plan.part + ((int64_t)job.slot * kRows + r) * (D + 4);
-        const int64_t stride = (int64_t)job.stride * kRows * (D + 4);
-        float m = -INFINITY, l = 0.0f;
-        f32x4 v = {};
-#pragma unroll 4
-        for (int s = 0; s < used; ++s) {
-            const float mm = p[s * stride + D], ll = p[s * stride + D + 1];
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(p + s * stride + d);
-            const float top = fmaxf(m, mm), base = top == -INFINITY ? 0.0f : top;
-            const float keep = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(mm - base);
-            m = top;
-            l = l * keep + ll * w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = v[e] * keep + x[e] * w;
-        }
+    const Seq seq = sequence(c, a, job.b);
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, d = 4 * lane;
+    const int rows = min(seq.lq * a.group - job.tile * kRows, kRows), q_heads = c.heads * a.group;
+    const float *first = plan.part + (int64_t)job.slot * kRows * (D + 4);
+    const int64_t stride = (int64_t)job.stride * kRows * (D + 4);
+    const auto store = [&](int r, const Part &x) {
         const int row = job.tile * kRows + r, qi = row / a.group;
-        const int64_t out_row = (job.seq.q0 + qi) * q_heads + job.head * a.group + row - qi * a.group;
-        store_outputs(a.out + out_row * D + d, v, inverse(l, m));
+        const int64_t out_row = (seq.q0 + qi) * q_heads + job.head * a.group + row - qi * a.group;
+        store_outputs(a.out + out_row * D + d, x.v, inverse(x.l, x.m));
+    };
+    if (job.used <= kFewPieces) {
+        if (group >= GROUPS)
+            return;
+        for (int r = blockIdx.y * GROUPS + group; r < rows; r += gridDim.y * GROUPS) {
+            Part x = {-INFINITY, 0.0f, {}};
+            const float *p = first + r * (D + 4);
+#pragma unroll 4
+            for (int s = 0; s < job.used; ++s)
+                x.add(p + s * stride, D, d);
+            store(r, x);
+        }
+        return;
+    }
+    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+        Part x = {-INFINITY, 0.0f, {}};
+        const float *p = first + r * (D + 4);
+        if (group < GROUPS) {
+#pragma unroll 4
+            for (int s = group; s < job.used; s += GROUPS)
+                x.add(p + s * stride, D, d);
+            other_v[group][lane] = x.v;
+            if (lane == 0) {
+                other_m[group] = x.m;
+                other_l[group] = x.l;
+            }
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int g = 1; g < GROUPS; ++g)
+                x.add(other_m[g], other_l[g], other_v[g][lane]);
+            store(r, x);
+        }
+        __syncthreads();
     }
 }
 
@@ -547,36 +656,43 @@ TreePlan plan_of(const KvShape &c, int64_t T, int seqs, int group, int max_kv) {
     const int64_t blocks = blocks_of(c, T, seqs, group);
     const bool divided = max_kv > kWholeTokens && seqs <= kSummed;
     p.target = divided ? (c.dim <= 128 ? 512 : 256) : 0;
-    p.least = 256;
+    p.least = 128;
     // pieces: a share less than their number for each row tile, and the target in all
+    p.tiles = (int)std::min<int64_t>(blocks, INT32_MAX / 2);
     p.grid = (int)std::min<int64_t>(blocks + p.target + p.target / 16, INT32_MAX / 2);
     const uint32_t pb = (uint32_t)c.page / 16;
     p.magic = (((uint64_t)1 << 32) + pb - 1) / pb;
+    p.notes = nullptr;
     p.part = nullptr;
     return p;
 }
+
+size_t notes_bytes(const TreePlan &p) { return (1 + (size_t)p.tiles) * sizeof(Note); }
 
 }  // namespace
 
 size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_kv) {
     const TreePlan p = plan_of(c, T, seqs, group, max_kv);
-    return p.target == 0 ? 0 : (size_t)p.grid * kRows * (c.dim + 4) * 4;
+    return p.target == 0 ? 0 : notes_bytes(p) + (size_t)p.grid * kRows * (c.dim + 4) * 4;
 }
 
 hipError_t launch_kv_tree(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
     if (a.T * c.heads * a.group > INT32_MAX)
         return hipErrorInvalidValue;
     TreePlan plan = plan_of(c, a.T, a.seqs, a.group, a.max_kv);
-    plan.part = static_cast<float *>(ws);
+    plan.notes = static_cast<Note *>(ws);
+    plan.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + notes_bytes(plan));
     const int64_t blocks = blocks_of(c, a.T, a.seqs, a.group);
     if (!launchable(plan.grid, 256) || !launchable(blocks, 256))
         return hipErrorInvalidValue;
+    // The join's workgroups a row tile: a row a group of lanes, or, with few tiles, a row each.
+    const int64_t join_parts = std::max<int64_t>(16, std::min<int64_t>(128, 8192 / blocks));
     const auto run = [&](auto dim, auto format) {
         constexpr int F = decltype(format)::value, D = decltype(dim)::value;
         hipLaunchKernelGGL((kv_tree_kernel<F, D>), dim3((unsigned)plan.grid), dim3(256), 0, s, c, a, plan);
         if (plan.target > 0 && hipPeekAtLastError() == hipSuccess)
-            hipLaunchKernelGGL((kv_tree_join_kernel<D>), dim3((unsigned)blocks, kJoinParts), dim3(256), 0,
-                               s, c, a, plan);
+            hipLaunchKernelGGL((kv_tree_join_kernel<D>), dim3((unsigned)blocks, (unsigned)join_parts), dim3(256),
+                               0, s, c, a, plan);
         return hipGetLastError();
     };
     const auto go = [&](auto dim) {
