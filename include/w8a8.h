@@ -388,7 +388,8 @@ size_t w8a8_kv_attention_workspace_bytes(int page, int heads, int dim, int fmt, 
  * bit n % 64 of tree[(q_starts[b] + i) * tree_words + n / 64] is set (tree [T, tree_words]; a
  * node sees its ancestors and itself; nodes past 64 * tree_words are seen by none, bits past lq
  * are ignored). tree_words is 1 to W8A8_KV_MAX_TREE_WORDS (else W8A8_ERR_ARG). The weights are
- * rounded to one bf16 term (2^-8). q_starts [seqs + 1] may end before T: rows behind the last
+ * rounded to two bf16 terms (2^-16) where a sequence's rows lq * group, or the last of them behind
+ * a multiple of 128, are up to 64; to one (2^-8) elsewhere. q_starts [seqs + 1] may end before T: rows behind the last
  * sequence are neither read nor written. max_kv is a bound on a sequence's tokens: up to 512 one
  * launch is enough; with a wrong one the results are the same but for rounding. Everything else is
  * as there. workspace: w8a8_kv_tree_attention_workspace_bytes(...) bytes, 256-byte aligned (NULL

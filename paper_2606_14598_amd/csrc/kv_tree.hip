@@ -4,8 +4,11 @@
 // i sees all tokens in front of the tree and the nodes whose bits its mask has set, itself and its
 // ancestors. The mathematics is that of kv_attention.hip: the queries of all the heads that share a
 // key/value head are the rows of one problem, one pass over the keys keeps a running maximum m and
-// sum l a row in float32, S^T = K Q^T and O^T = V^T P^T on the bf16 matrix instructions, and the
-// weights are rounded to one bf16 term (2^-8 of each) for the second product.
+// sum l a row in float32, S^T = K Q^T and O^T = V^T P^T on the bf16 matrix instructions. The weights
+// are rounded for the second product: to two bf16 terms (2^-16 of each at most) in row tiles of up to
+// 64 rows, to one (2^-8) in others, whose products bind. There l sums the rounded weights: what a
+// weight's rounding by d does to an output is then d (v - o) / l and not d v / l, less where a few
+// weights are most of the sum.
 //
 // A step of a sequence has some tens of nodes, so a row tile of 128 rows is seldom full, and the
 // lengths of a batch differ: the work is divided by what there is. The pieces of a call (a row tile
@@ -235,6 +238,9 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
     constexpr int CB = FMT == KV_FP8 ? D : D / 2;
     constexpr int RSK = 2 * D + 16, RSV = 2 * D + 64;
     constexpr int KS = D / 16, F = D / 32;
+    // Tiles whose codes are in registers: two give the loads a step more time (32 trees of 60 nodes on
+    // 8192 tokens 320 us with one, 311 with two); above 128 channels there is no room for them.
+    constexpr int SETS = D <= 128 ? 2 : 1;
     __shared__ __attribute__((aligned(16))) uint8_t keys[2][TT * RSK];
     __shared__ __attribute__((aligned(16))) uint8_t values[2][TT * RSV];
     __shared__ Places places;
@@ -268,6 +274,7 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
     const auto run = [&](auto groups) __attribute__((always_inline)) {
         constexpr int RG = decltype(groups)::value, TG = 4 / RG;      // of rows, of tokens
         constexpr int NS = 2 / TG, US = 4 / TG;        // fragments of 32 keys, steps of 16 values
+        constexpr int TERMS = TG;                      // bf16 terms of a weight
         const int rg = wave % RG, tg = wave / RG;
         const int first_row = job.note.tile * kRows + rg * 32, row = first_row + r32;
         const bool live = row < rows, wave_live = first_row < rows;
@@ -299,10 +306,11 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
             fill_places(places, c, a, plan.magic, job.note.b, head, j_first, j_end, ntile * (TT / 16));
             __syncthreads();
 
-            u32x4 kc[NU], vc[NU];
-            uint32_t ks[NU], vs[NU];
-            const auto load = [&](auto ic, int tile) __attribute__((always_inline)) {
-                constexpr int i = decltype(ic)::value;
+            // Codes and scales on their way to the stages.
+            u32x4 kc[SETS][NU], vc[SETS][NU];
+            uint32_t ks[SETS][NU], vs[SETS][NU];
+            const auto load = [&](auto set, auto ic, int tile) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value, b = decltype(set)::value % SETS;
                 const int unit = min(i * 256 + (int)threadIdx.x, UNITS - 1);
                 const int tok = unit / VT, part = unit % VT;
                 const int blk = tile * (TT / 16) + tok / 16;
@@ -310,41 +318,43 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
                 const uint8_t *p = a.cache + places.page[blk];
                 const uint32_t code = at * CB + part * 16;
                 const uint32_t scale = c.page * CB + at * (D / 32) + part * VU / 32;
-                kc[i] = Unit<16>::load(p + code);
-                ks[i] = p[scale];
-                vc[i] = Unit<16>::load(p + v_offset + code);
-                vs[i] = p[v_offset + scale];
+                kc[b][i] = Unit<16>::load(p + code);
+                ks[b][i] = p[scale];
+                vc[b][i] = Unit<16>::load(p + v_offset + code);
+                vs[b][i] = p[v_offset + scale];
             };
-            const auto load_all = [&](int tile) {
+            const auto load_all = [&](auto set, int tile) __attribute__((always_inline)) {
                 [&]<int... i>(std::integer_sequence<int, i...>) __attribute__((always_inline)) {
-                    (load(std::integral_constant<int, i>{}, tile), ...);
+                    (load(set, std::integral_constant<int, i>{}, tile), ...);
                 }(std::make_integer_sequence<int, NU>{});
             };
             // Values past the end, and NaN blocks in tiles that only some rows see whole, become
             // zeros before they are staged (a zero weight would not silence them).
-            const auto mark = [&](int j0, int st) {
+            const auto mark = [&](auto set, int j0) __attribute__((always_inline)) {
+                constexpr int st = decltype(set)::value, b = st % SETS;
 #pragma unroll
                 for (int i = 0; i < NU; ++i) {
                     const int unit = min(i * 256 + (int)threadIdx.x, UNITS - 1);
                     const bool past = j0 + unit / VT >= seq.kv;
-                    const bool nan = vs[i] == kNaNScale && !past;
+                    const bool nan = vs[b][i] == kNaNScale && !past;
                     nan_unit[st][unit] = nan;
                     if (nan)
                         nan_any = 1;
                     if (past || nan) {
-                        vc[i] = u32x4{};
-                        vs[i] = 0;
+                        vc[b][i] = u32x4{};
+                        vs[b][i] = 0;
                     }
                 }
             };
-            // Half z of 4 NU half units into stage st: keys, then values.
-            const auto stage = [&](auto zc, int st) __attribute__((always_inline)) {
+            // Half z of 4 NU half units of a set into its stage: keys, then values.
+            const auto stage = [&](auto set, auto zc) __attribute__((always_inline)) {
                 constexpr int z = decltype(zc)::value / 2, half = decltype(zc)::value % 2, i = z % NU;
+                constexpr int st = decltype(set)::value, b = st % SETS;
                 const int unit = i * 256 + threadIdx.x, tok = unit / VT, part = unit % VT;
                 if (UNITS % 256 != 0 && unit >= UNITS)
                     return;
-                const u32x4 codes = z < NU ? kc[i] : vc[i];
-                const float sc = scale_operand(z < NU ? ks[i] : vs[i]);
+                const u32x4 codes = z < NU ? kc[b][i] : vc[b][i];
+                const float sc = scale_operand(z < NU ? ks[b][i] : vs[b][i]);
                 u32x4 *d = reinterpret_cast<u32x4 *>(
                     (z < NU ? keys[st] + tok * RSK : values[st] + tok * RSV) + part * VU * 2);
                 if constexpr (VU == 16) {
@@ -355,20 +365,27 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
                 }
             };
             const auto partly_seen = [&](int j0) { return j0 + TT > all_see; };
-            load_all(0);
+            constexpr std::integral_constant<int, 0> even;
+            constexpr std::integral_constant<int, 1> odd;
+            load_all(even, 0);
+            if constexpr (SETS == 2)
+                load_all(odd, min(1, ntile - 1));
             if (partly_seen(j_first))
-                mark(j_first, 0);
+                mark(even, j_first);
             [&]<int... z>(std::integer_sequence<int, z...>) __attribute__((always_inline)) {
-                (stage(std::integral_constant<int, z>{}, 0), ...);
+                (stage(even, std::integral_constant<int, z>{}), ...);
             }(std::make_integer_sequence<int, 4 * NU>{});
-            load_all(min(1, ntile - 1));
-            for (int tile = 0; tile < ntile; ++tile) {
-                const int j0 = j_first + tile * TT, st = tile & 1;
+            load_all(even, min(SETS, ntile - 1));
+            // Tile `tile`, of even or odd number: multiplied, the one behind it staged, and the next that
+            // has room loaded.
+            const auto step = [&](auto number, auto next, int tile) __attribute__((always_inline)) {
+                constexpr int st = decltype(number)::value;
+                const int j0 = j_first + tile * TT;
                 const int mine = j0 + 32 * tg;         // this wavefront's first token
                 const bool part_seen = partly_seen(j0);
                 lds_barrier();       // this tile is staged, the other stage's last one is read
                 if (partly_seen(j0 + TT) && tile + 1 < ntile)
-                    mark(j0 + TT, st ^ 1);
+                    mark(next, j0 + TT);
                 if (part_seen && nan_any) {    // rare: which rows see a NaN block
                     const uint64_t visible = tree.window(j0) | (uint64_t)tree.window(j0 + 32) << 32;
                     for (int unit = 0; unit < UNITS; ++unit)
@@ -376,7 +393,7 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
                             row_nan |= 1u << (unit % VT * VU / 32);
                 }
                 // Scores: token 32 t + 8 (i / 4) + 4 h + i % 4 in s[t][i]. Between the products
-                // the next tile is staged (after the last tile: itself again, unread).
+                // the next tile is staged (after the last tile: some tile again, unread).
                 f32x16 s[NS];
 #pragma unroll
                 for (int t = 0; t < NS; ++t)
@@ -395,7 +412,7 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
                             read_keys(k + 1);
                         constexpr int z0 = k * 4 * NU / KS, z1 = (k + 1) * 4 * NU / KS;
                         if constexpr (z0 < z1)
-                            stage(std::integral_constant<int, z0>{}, st ^ 1);
+                            stage(next, std::integral_constant<int, z0>{});
                         static_assert(z1 - z0 <= 1, "half units of a step");
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -407,8 +424,8 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
                 }(std::make_integer_sequence<int, KS>{});
                 // The next loads go out between the products with the values.
                 if (!wave_live || mine >= seq.kv) {
-                    load_all(min(tile + 2, ntile - 1));
-                    continue;
+                    load_all(next, min(tile + SETS + 1, ntile - 1));
+                    return;
                 }
 
                 if (part_seen) {
@@ -457,15 +474,23 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
                     fv[z & 1][1] = __builtin_bit_cast(
                         u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(src + 8 * RSV)));
                 };
-                u32x4 p[US];
+                u32x4 p[US], p2[TERMS == 2 ? US : 1];
                 const auto weight = [&](auto qc) __attribute__((always_inline)) {
                     constexpr int w = decltype(qc)::value;     // of 8 NS pairs
                     const float x = __builtin_amdgcn_exp2f(
                         __builtin_fmaf(s[w / 8][w % 8 * 2], a.scale, -base));
                     const float y = __builtin_amdgcn_exp2f(
                         __builtin_fmaf(s[w / 8][w % 8 * 2 + 1], a.scale, -base));
-                    l += x + y;
-                    p[w / 4][w % 4] = pack_bf16(x, y);
+                    const uint32_t both = pack_bf16(x, y);
+                    p[w / 4][w % 4] = both;
+                    if constexpr (TERMS == 2) {
+                        l += x + y;
+                        p2[w / 4][w % 4] = pack_bf16(x - __uint_as_float(both << 16),
+                                                     y - __uint_as_float(both & 0xFFFF0000u));
+                    } else {
+                        l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, both),
+                                                            bf16x2{1.0f, 1.0f}, l, false);
+                    }
                 };
                 weight(std::integral_constant<int, 0>{});
                 weight(std::integral_constant<int, 1>{});
@@ -485,16 +510,24 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
                                 weight(std::integral_constant<int, w0 + 1>{});
                         }
                         if constexpr (z < 2 * NU && z % 2 == 1)
-                            load(std::integral_constant<int, z / 2>{}, min(tile + 2, ntile - 1));
+                            load(next, std::integral_constant<int, z / 2>{}, min(tile + SETS + 1, ntile - 1));
                         static_assert(2 * NU <= US * F, "loads between the products");
                         __builtin_amdgcn_sched_barrier(0);
-                        o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            __builtin_bit_cast(bf16x8, u32x4{fv[z & 1][0][0], fv[z & 1][0][1],
-                                                             fv[z & 1][1][0], fv[z & 1][1][1]}),
-                            __builtin_bit_cast(bf16x8, p[u]), o[f], 0, 0, 0);
+                        const bf16x8 v = __builtin_bit_cast(
+                            bf16x8, u32x4{fv[z & 1][0][0], fv[z & 1][0][1], fv[z & 1][1][0], fv[z & 1][1][1]});
+                        o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p[u]),
+                                                                       o[f], 0, 0, 0);
+                        if constexpr (TERMS == 2)
+                            o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                v, __builtin_bit_cast(bf16x8, p2[u]), o[f], 0, 0, 0);
                         __builtin_amdgcn_sched_barrier(0);
                     }(), ...);
                 }(std::make_integer_sequence<int, US * F>{});
+            };
+            for (int tile = 0; tile < ntile; tile += 2) {
+                step(even, odd, tile);
+                if (tile + 1 < ntile)
+                    step(odd, even, tile + 1);
             }
         }
 

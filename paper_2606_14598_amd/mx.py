@@ -303,8 +303,8 @@ def kv_tree_attention(q, cache, block_table, kv_lens, tree, *, fmt: str = "fp8",
     queries are the nodes of a tree, its last cached tokens, in order; all of them see the tokens in
     front of the tree, and query i of a sequence sees node n where bit n % 64 of
     tree[q_starts[b] + i, n // 64] is set: itself and its ancestors (tree int64 [T, words], up to
-    64 words). A query that sees nothing gives zeros. The weights are rounded to one bf16 term.
-    q_starts may end before T: rows of q and the output behind the last sequence are neither read nor
+    64 words). A query that sees nothing gives zeros. The weights are rounded to bf16, to two
+    terms in sequences of up to 64 rows. q_starts may end before T: rows of q and the output behind the last sequence are neither read nor
     written. max_kv as in kv_attention; max_q makes no difference here. Everything else is as there."""
     if not isinstance(tree, torch.Tensor) or tree.dtype != torch.int64:
         raise TypeError("tree must be an int64 torch.Tensor")
