@@ -12,12 +12,15 @@
 #include "kv_layout.hpp"
 #include "lm_internal.hpp"
 
+#include <algorithm>
+
 namespace w8a8 {
 namespace {
 
 using namespace mx;
 
-enum Pairing : int { HALVES = 0, HALVES_ANY = 1, NEIGHBOURS = 2 };   // HALVES: P a multiple of 8
+// HALVES: P a multiple of 8. HALVES_ANY: any other.
+enum Pairing : int { HALVES = 0, HALVES_ANY = 1, NEIGHBOURS = 2 };
 
 // cos and sin of an angle of a * b radians. Turns a b / 2 pi in two terms, less whole ones, then
 // quarters of a turn and a remainder of at most 1/8 turn, for which the Taylor polynomials are
@@ -52,14 +55,19 @@ __device__ __forceinline__ void cos_sin(double a, double b, float &cosine, float
 
 // A workgroup takes a token. Thread -> unit of 8 channels, the same in every head that it works
 // on, so that its cosines and sines stay in registers; HEADS heads at a time, LOADS times that in
-// flight. Queries first, then keys, then values.
+// flight. Queries first, then keys, then values. The other half of a unit's pairs is a second load of
+// 16 bytes, at the row's own alignment. Where the first half ends inside a unit (HALVES_ANY: one unit
+// of a head), the partners of its channels are the last of the second half and the first of the first:
+// two loads, shifted together; with fewer than 8 pairs they are loaded one by one.
 template <int D>
 constexpr int append_threads() { return D == 192 ? 192 : 256; }
+template <int D>
+constexpr int append_heads() { return append_threads<D>() / (D / 8); }
 
-template <int FMT, int D, int PAIRING>
+template <int FMT, int D, int PAIRING, int LOADS>
 __global__ void __launch_bounds__(append_threads<D>())
 kv_append_kernel(uint8_t *cache, KvShape c, AppendArgs a) {
-    constexpr int UNITS = D / 8, HEADS = append_threads<D>() / UNITS, LOADS = 4;
+    constexpr int UNITS = D / 8, HEADS = append_heads<D>();
     __shared__ float cosines[D / 2], sines[D / 2];
     const int unit = threadIdx.x % UNITS, first = threadIdx.x / UNITS, e = unit * 8;
     const int64_t t = blockIdx.x;
@@ -93,10 +101,11 @@ kv_append_kernel(uint8_t *cache, KvShape c, AppendArgs a) {
         cs[i] = on[i] ? cosines[p] : 1.0f;
         sn[i] = second ? s : -s;
     }
-    // Where the other half of each pair lies, from this thread's unit (HALVES: of all 8).
-    const int across = e < a.pairs ? a.pairs : on[0] ? -a.pairs : 0;
+    // Where the other half of each pair lies, from this thread's unit.
+    const bool mixed = PAIRING == HALVES_ANY && e < a.pairs && e + 8 > a.pairs;
+    const int across = mixed ? max(2 * a.pairs - 8, 0) - e : e < a.pairs ? a.pairs : on[0] ? -a.pairs : 0;
 
-    for (int h0 = first; h0 < heads; h0 += HEADS * LOADS) {
+    for (int h0 = first + blockIdx.y * (HEADS * LOADS); h0 < heads; h0 += gridDim.y * (HEADS * LOADS)) {
         uint32_t x[LOADS][4], y[LOADS][4];
 #pragma unroll
         for (int n = 0; n < LOADS; ++n) {
@@ -106,24 +115,53 @@ kv_append_kernel(uint8_t *cache, KvShape c, AppendArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 x[n][i] = own.w[i];
-            if constexpr (PAIRING == HALVES) {
+            if constexpr (PAIRING != NEIGHBOURS) {
                 const Bytes16 other = *reinterpret_cast<const Bytes16 *>(src + across);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     y[n][i] = other.w[i];
-            } else if constexpr (PAIRING == HALVES_ANY) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const auto other = [&](int k) -> uint32_t {
-                        const int ch = e + k;
-                        return src[k + (ch < a.pairs ? a.pairs : ch < 2 * a.pairs ? -a.pairs : 0)];
-                    };
-                    y[n][i] = other(2 * i) | other(2 * i + 1) << 16;
-                }
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     y[n][i] = x[n][i] >> 16 | x[n][i] << 16;
+            }
+        }
+        if constexpr (PAIRING == HALVES_ANY) {
+            if (mixed) {
+                const int skip = e + 8 - a.pairs;          // of the second half's last 8
+#pragma unroll
+                for (int n = 0; n < LOADS; ++n) {
+                    const uint16_t *row = row_of(min(h0 + n * HEADS, heads - 1));
+                    if (a.pairs < 8) {                     // unit 0 holds all pairs
+                        const auto other = [&](int k) -> uint32_t {
+                            return row[k < a.pairs ? k + a.pairs : k < 2 * a.pairs ? k - a.pairs : k];
+                        };
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            y[n][i] = other(2 * i) | other(2 * i + 1) << 16;
+                    } else {
+                        const Bytes16 head = *reinterpret_cast<const Bytes16 *>(row);
+                        uint32_t w[8];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            w[i] = y[n][i];
+                            w[i + 4] = head.w[i];
+                        }
+                        // selects on values: one between array elements would put the array in memory
+                        const auto moved = [&](bool by, uint32_t here, uint32_t there) {
+                            return by ? there : here;
+                        };
+#pragma unroll
+                        for (int i = 0; i < 6; ++i)
+                            w[i] = moved(skip & 4, w[i], w[i + 2]);
+#pragma unroll
+                        for (int i = 0; i < 5; ++i)
+                            w[i] = moved(skip & 2, w[i], w[i + 1]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            y[n][i] = moved(skip & 1, w[i], w[i] >> 16 | w[i + 1] << 16);
+                    }
+                }
             }
         }
 #pragma unroll
@@ -189,13 +227,33 @@ hipError_t launch_kv_append(uint8_t *cache, const KvShape &c, const AppendArgs &
             a.q_out += t0 * a.q_heads * D;
             a.slots += t0;
             a.positions += t0 * a.axes;
-            const dim3 grid((unsigned)a.T), block(append_threads<D>());
+            const int passes = (args.q_heads + 2 * c.heads + append_heads<D>() - 1) / append_heads<D>();
+            const auto go = [&](auto pairing, auto loads) {
+                // Few tokens: several workgroups a token, up to what the card holds at once.
+                constexpr int L = decltype(loads)::value;
+                const int64_t parts = std::min<int64_t>((passes + L - 1) / L, std::max<int64_t>(2048 / a.T, 1));
+                const dim3 grid((unsigned)a.T, (unsigned)parts), block(append_threads<D>());
+                hipLaunchKernelGGL((kv_append_kernel<F, D, decltype(pairing)::value, decltype(loads)::value>),
+                                   grid, block, 0, s, cache, c, a);
+            };
+            const auto with_loads = [&](auto pairing) {
+                // As many in flight as divide the passes over the heads best, the more the better:
+                // 20000 tokens of 48 heads of 128 (three passes) 86.9 us with three, 96.6 with four; 9000 of
+                // 45 heads of 64 (two) 25.0 with two, 30.2 with four.
+                const auto over = [&](int n) { return (passes + n - 1) / n * n; };
+                if (over(4) <= std::min(over(3), over(2)))
+                    go(pairing, std::integral_constant<int, 4>{});
+                else if (over(3) <= over(2))
+                    go(pairing, std::integral_constant<int, 3>{});
+                else
+                    go(pairing, std::integral_constant<int, 2>{});
+            };
             if (pairing == HALVES)
-                hipLaunchKernelGGL((kv_append_kernel<F, D, HALVES>), grid, block, 0, s, cache, c, a);
+                with_loads(std::integral_constant<int, HALVES>{});
             else if (pairing == HALVES_ANY)
-                hipLaunchKernelGGL((kv_append_kernel<F, D, HALVES_ANY>), grid, block, 0, s, cache, c, a);
+                with_loads(std::integral_constant<int, HALVES_ANY>{});
             else
-                hipLaunchKernelGGL((kv_append_kernel<F, D, NEIGHBOURS>), grid, block, 0, s, cache, c, a);
+                with_loads(std::integral_constant<int, NEIGHBOURS>{});
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess)
                 return e;
