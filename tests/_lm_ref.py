@@ -32,15 +32,16 @@ def int8_rows(v):
 
 def cos_sin(positions, inv_freq, sections):
     """float32 cosines and sines [T, pairs], and the tokens where one of them hangs on the last bits
-    of a 64-bit value: the kernel's are 2^-44 off at most (2^-45 from the polynomials, the rest from
-    the reduction of the angle)."""
+    of a 64-bit value: the kernel's are 2^-45 of the value off at most by the polynomials, and 2^-50 by
+    the rounding of the reduced angle (of at most 2 quarter turns, 2^-52, times pi / 2) and of this
+    reference; not at all at no angle."""
     p = positions.reshape(positions.shape[0], -1).astype(np.float64)
     axis = np.zeros(len(inv_freq), int) if sections is None else np.repeat(np.arange(len(sections)), sections)
     angle = p[:, axis] * inv_freq.astype(np.float64)
     out, near = [], np.zeros(p.shape[0], bool)
     for f in (np.cos(angle), np.sin(angle)):
         r = f.astype(np.float32)
-        d = 2.0 ** -44
+        d = np.where(angle == 0, 0.0, 2.0 ** -45 * np.abs(f) + 2.0 ** -50)
         near |= (((f - d).astype(np.float32) != r) | ((f + d).astype(np.float32) != r)).any(1) \
             if f.size else near
         out.append(r)
