@@ -390,9 +390,8 @@ size_t w8a8_kv_attention_workspace_bytes(int page, int heads, int dim, int fmt, 
  * are ignored). tree_words is 1 to W8A8_KV_MAX_TREE_WORDS (else W8A8_ERR_ARG). The weights are
  * rounded to two bf16 terms (2^-16) where a sequence's rows lq * group, or the last of them behind
  * a multiple of 128, are up to 64; to one (2^-8) elsewhere. q_starts [seqs + 1] may end before T: rows behind the last
- * sequence are neither read nor written. max_kv is a bound on a sequence's tokens: up to 512 one
- * launch is enough; with a wrong one the results are the same but for rounding. Everything else is
- * as there. workspace: w8a8_kv_tree_attention_workspace_bytes(...) bytes, 256-byte aligned (NULL
+ * sequence are neither read nor written. max_q and max_kv are bounds as there: with few rows
+ * (max_q * group) another kernel runs, up to 512 tokens one launch is enough. Everything else is as there. workspace: w8a8_kv_tree_attention_workspace_bytes(...) bytes, 256-byte aligned (NULL
  * allowed when that is 0). */
 #define W8A8_KV_MAX_TREE_WORDS 64
 w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
@@ -400,11 +399,11 @@ w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q
                                    int dim, int fmt, const int32_t *table, int64_t table_stride,
                                    int table_pages, const int32_t *kv_lens,
                                    const int32_t *q_starts, int64_t T, int seqs, int group,
-                                   float scale, const int64_t *tree, int tree_words, int max_kv,
-                                   uint16_t *out, void *workspace, size_t workspace_bytes,
-                                   void *stream);
+                                   float scale, const int64_t *tree, int tree_words, int max_q,
+                                   int max_kv, uint16_t *out, void *workspace,
+                                   size_t workspace_bytes, void *stream);
 size_t w8a8_kv_tree_attention_workspace_bytes(int page, int heads, int dim, int fmt, int group,
-                                              int64_t T, int seqs, int max_kv);
+                                              int64_t T, int seqs, int max_q, int max_kv);
 
 /* w8a8_kv_write with rotary positions, for the keys and the queries beside them. A head's
  * channels have `pairs` pairs (at most dim / 2): channels p and p + pairs, or 2p and 2p + 1 where

@@ -121,8 +121,8 @@ def load_library():
                                INT, ctypes.c_float, INT, INT, INT, P, P, SZ, P], INT),
         "w8a8_kv_attention_workspace_bytes": ([INT, INT, INT, INT, INT, I64, INT, INT, INT], SZ),
         "w8a8_kv_tree_attention": ([P, I64, I64, P, I64, INT, INT, INT, INT, P, I64, INT, P, P, I64,
-                                    INT, INT, ctypes.c_float, P, INT, INT, P, P, SZ, P], INT),
-        "w8a8_kv_tree_attention_workspace_bytes": ([INT, INT, INT, INT, INT, I64, INT, INT], SZ),
+                                    INT, INT, ctypes.c_float, P, INT, INT, INT, P, P, SZ, P], INT),
+        "w8a8_kv_tree_attention_workspace_bytes": ([INT, INT, INT, INT, INT, I64, INT, INT, INT], SZ),
         "w8a8_kv_append": ([P, I64, INT, INT, INT, INT, P, I64, I64, INT, P, I64, I64, P, I64, I64, P,
                             P, INT, P, P, INT, INT, I64, P, P], INT),
         "w8a8_rms_norm_quantize": ([P, P, P, P, ctypes.c_double, I64, I64, P, P, P], INT),

@@ -43,6 +43,17 @@ __device__ __forceinline__ int seen(const Seq &s, int i, int causal) {
     return max(0, causal ? min(s.kv, s.kv - s.lq + i + 1) : s.kv);
 }
 
+// Tokens that some query up to i sees, and that every query from i on does. In a tree: all, as any
+// node may see any other, and those in front of it.
+template <bool TREE>
+__device__ __forceinline__ int some_seen(const Seq &s, int i, int causal) {
+    return TREE ? max(0, s.kv) : seen(s, i, causal);
+}
+template <bool TREE>
+__device__ __forceinline__ int all_seen(const Seq &s, int i, int causal) {
+    return TREE ? max(0, s.kv - s.lq) : seen(s, i, causal);
+}
+
 __device__ __forceinline__ bool mine(const Split &sp, int rows) {
     return rows >= sp.rows_from && rows <= sp.rows_to;
 }
@@ -98,7 +109,7 @@ __device__ __forceinline__ bf16x8 ones() {
 // head) at 5.4 TB/s, 16 of 8000 with 18 heads of 256 at 5.6; one of 200000 in e2m1, 8 queries a
 // head, at 4.6 (about 370 instructions for 32 tokens of 4.3 KB); 48 sequences of very different
 // lengths at 4.0 (unequal shares, more workgroups that start).
-template <int FMT, int D>
+template <int FMT, int D, bool TREE>
 __global__ void __launch_bounds__(256, D <= 128 ? 3 : 2)
 kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
     constexpr int KU = FMT == KV_FP4 && D % 128 == 0 ? 32 : 16;   // elements of a key unit
@@ -135,7 +146,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 
     for (int rt = blockIdx.y; rt * kSplitRows < rows; rt += gridDim.y) {
         const int some_see =
-            seen(seq, (min(rt * kSplitRows + kSplitRows, rows) - 1) / a.group, a.causal);   // some row
+            some_seen<TREE>(seq, (min(rt * kSplitRows + kSplitRows, rows) - 1) / a.group, a.causal);
         const int share = max(even, ((some_see + sp.splits - 1) / sp.splits + 127) & ~127);
         const int used = (some_see + share - 1) / share;
         if (split >= max(used, 1))
@@ -146,7 +157,8 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
         const int qi = live ? row / a.group : 0;
         const int qh = head * a.group + (live ? row % a.group : 0);
         const int limit = live ? seen(seq, qi, a.causal) : 0;
-        const int all_see = seen(seq, rt * kSplitRows / a.group, a.causal);   // every live row
+        const TreeRow tree(a, seq, qi, TREE && live);
+        const int all_see = all_seen<TREE>(seq, rt * kSplitRows / a.group, a.causal);   // every live row
         u32x4 q[NK][KU / 8];
         {
             const uint16_t *src = a.q + (seq.q0 + qi) * a.q_token + qh * a.q_head;
@@ -163,7 +175,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x4{};
-        float m = start_of(limit);
+        float m = start_of(TREE ? tree.any() : limit > 0);
         f32x4 sums = {};           // in each element: the sum of a row's weights
         uint32_t row_nan = 0;      // blocks of the row's output that a seen NaN value reaches
 
@@ -263,6 +275,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                 }
                 if (part_seen && __any(any_nan)) {
                     // Rare: which rows see a NaN value, and in which blocks of 32 outputs.
+                    const uint32_t visible = TREE ? tree.window(j0) : 0;
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
                         uint64_t marked = __ballot(vs[i] == 256);
@@ -270,7 +283,7 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
                             const int src = __builtin_ctzll(marked);
                             marked &= marked - 1;
                             const int unit = i * 64 + src;
-                            if (j0 + unit / VT < limit)
+                            if (TREE ? visible >> (unit / VT) & 1 : j0 + unit / VT < limit)
                                 row_nan |= 1u << (unit % VT * VU / 32);
                         }
                     }
@@ -280,12 +293,14 @@ kv_attention_split_kernel(KvShape c, KvAttnArgs a, Split sp) {
 
                 if (part_seen) {
                     const int left = limit - j0 - 4 * g;
+                    const uint32_t visible = TREE ? tree.window(j0) >> 4 * g : 0;
                     keep_branch();
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            s[h][e] = 16 * h + e < left ? s[h][e] : -INFINITY;
+                            s[h][e] = (TREE ? visible >> (16 * h + e) & 1 : 16 * h + e < left) ? s[h][e]
+                                                                                               : -INFINITY;
                 }
                 float top = -INFINITY;
 #pragma unroll
@@ -501,7 +516,7 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 #pragma unroll
         for (int f = 0; f < F; ++f)
             o[f] = f32x16{};
-        float m = start_of(limit), l = 0.0f;
+        float m = start_of(limit > 0), l = 0.0f;
         uint32_t row_nan = 0;
 
         for (int ch = split; ch < nch; ch += used) {
@@ -736,9 +751,12 @@ kv_attention_tile_kernel(KvShape c, KvAttnArgs a, Split sp, int tiles) {
 
 // Joins the splits of each row with weights 2^(m_s - max m): LANES lanes hold 4 outputs each of
 // a row (or of 4 LANES of its outputs), WAYS groups of them take the splits in turn.
-template <int D, int LANES, int WAYS>
+// In a tree's call `queries` (or nullptr) is how many the sequences have in all: rows behind them are
+// left as they are.
+template <int D, int LANES, int WAYS, bool TREE>
 __global__ void __launch_bounds__(256)
-kv_attention_join_kernel(const float *part, int splits, int64_t rows, uint16_t *out) {
+kv_attention_join_kernel(const float *part, int splits, int64_t rows, uint16_t *out,
+                         const int32_t *queries, int q_heads) {
     constexpr int PIECES = D / (4 * LANES), PER = LANES * WAYS, JOBS = 256 / PER;
     __shared__ f32x4 red[JOBS][WAYS][LANES];
     __shared__ float red_l[JOBS][WAYS], red_m[JOBS][WAYS];
@@ -748,7 +766,8 @@ kv_attention_join_kernel(const float *part, int splits, int64_t rows, uint16_t *
     const bool live = job < JOBS && row < rows;
     const float *p = part + (live ? row : 0) * (D + 4);
     const int64_t stride = rows * (D + 4);
-    const int used = live ? min((int)p[D + 2], splits) : 0;
+    const bool owned = !TREE || !queries || row < (int64_t)*queries * q_heads;
+    const int used = live && owned ? min((int)p[D + 2], splits) : 0;
     float m = -INFINITY, l = 0.0f;
     f32x4 v = {};
     if (used > 1) {
@@ -801,13 +820,19 @@ kv_attention_join_kernel(const float *part, int splits, int64_t rows, uint16_t *
 }
 
 template <int D, int LANES, int WAYS>
-hipError_t launch_join(const float *part, int splits, int64_t rows, uint16_t *out, hipStream_t s) {
+hipError_t launch_join(const float *part, int splits, int64_t rows, uint16_t *out, bool tree,
+                       const int32_t *queries, int q_heads, hipStream_t s) {
     constexpr int jobs = 256 / (LANES * WAYS), pieces = D / (4 * LANES);
     const int64_t blocks = (rows * pieces + jobs - 1) / jobs;
     if (!launchable(blocks, 256))
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL((kv_attention_join_kernel<D, LANES, WAYS>), dim3((unsigned)blocks), dim3(256), 0, s,
-                       part, splits, rows, out);
+    const dim3 grid((unsigned)blocks), block(256);
+    if (tree)
+        hipLaunchKernelGGL((kv_attention_join_kernel<D, LANES, WAYS, true>), grid, block, 0, s, part, splits,
+                           rows, out, queries, q_heads);
+    else
+        hipLaunchKernelGGL((kv_attention_join_kernel<D, LANES, WAYS, false>), grid, block, 0, s, part, splits,
+                           rows, out, nullptr, 0);
     return hipGetLastError();
 }
 
@@ -913,7 +938,10 @@ hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, h
             if (!launchable(units, 256))
                 return hipErrorInvalidValue;
             const dim3 grid((unsigned)units, (unsigned)((most_rows + kSplitRows - 1) / kSplitRows));
-            hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D>), grid, dim3(256), 0, s, c, a, sp);
+            if (a.tree)
+                hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D, true>), grid, dim3(256), 0, s, c, a, sp);
+            else
+                hipLaunchKernelGGL((kv_attention_split_kernel<FMT, D, false>), grid, dim3(256), 0, s, c, a, sp);
             return hipGetLastError();
         }
         // A workgroup goes on to every tiles-th row tile, so that a loose max_q costs empty
@@ -935,9 +963,11 @@ hipError_t run_plan(const KvShape &c, const KvAttnArgs &a, Plan &p, float *ws, h
     if (e != hipSuccess || p.splits == 1)
         return e;
     // Few splits: a row by D / 4 lanes. Many: 32 outputs of a row by 32 groups of 8 lanes.
+    const int32_t *queries = a.tree && a.q_starts ? a.q_starts + a.seqs : nullptr;
+    const int q_heads = c.heads * a.group;
     return p.splits <= 16 || rows * (D / 4) >= 65536
-               ? launch_join<D, D / 4, 1>(ws, p.splits, rows, a.out, s)
-               : launch_join<D, 8, 32>(ws, p.splits, rows, a.out, s);
+               ? launch_join<D, D / 4, 1>(ws, p.splits, rows, a.out, a.tree, queries, q_heads, s)
+               : launch_join<D, 8, 32>(ws, p.splits, rows, a.out, a.tree, queries, q_heads, s);
 }
 
 }  // namespace

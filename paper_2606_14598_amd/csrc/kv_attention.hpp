@@ -44,10 +44,42 @@ __device__ __forceinline__ Seq sequence(const KvShape &c, const KvAttnArgs &a, i
     return s;
 }
 
+// What a row of a tree sees: the tokens in front of it, and nodes by its bits.
+struct TreeRow {
+    const uint32_t *bits;     // nullptr: no row, sees nothing
+    int words, prefix, kv;    // the tree's first token (below 0: its first nodes are not cached)
+    __device__ __forceinline__ TreeRow(const KvAttnArgs &a, const Seq &s, int qi, bool live)
+        : bits(live ? a.tree + (s.q0 + qi) * a.tree_words : nullptr), words(a.tree_words),
+          prefix(s.kv - s.lq), kv(s.kv) {}
+    __device__ __forceinline__ uint32_t word(int i) const { return i < words ? bits[i] : 0; }
+    // Tokens j .. j + 31, the first in the lowest bit.
+    __device__ __forceinline__ uint32_t window(int j) const {
+        if (!bits || j >= kv)
+            return 0;
+        const int node = j - prefix;
+        uint32_t w;
+        if (node <= -32)
+            w = ~0u;
+        else if (node < 0)
+            w = word(0) << -node | ((1u << -node) - 1);
+        else
+            w = (uint32_t)((word(node / 32) | (uint64_t)word(node / 32 + 1) << 32) >> node % 32);
+        return kv - j < 32 ? w & ((1u << (kv - j)) - 1) : w;
+    }
+    __device__ __forceinline__ bool any() const {
+        uint32_t w = bits && prefix > 0;       // else at most as many tokens as nodes
+        if (!bits)
+            return false;
+        for (int j = 0; w == 0 && j < kv; j += 32)
+            w = window(j);
+        return w != 0;
+    }
+};
+
 // A row's maximum before its first key: minus infinity where it sees none, else the least finite
 // number. A sum of zero then tells a row without keys (zeros) from one all of whose scores are
 // minus infinity, as a query with an infinity has them (NaN, as exp(-inf - -inf) is).
-__device__ __forceinline__ float start_of(int limit) { return limit > 0 ? -__FLT_MAX__ : -INFINITY; }
+__device__ __forceinline__ float start_of(bool sees) { return sees ? -__FLT_MAX__ : -INFINITY; }
 
 __device__ __forceinline__ float inverse(float l, float m) {
     return l == 0.0f ? (m == -INFINITY ? 0.0f : NAN) : 1.0f / l;

@@ -48,38 +48,6 @@ struct TreePlan {
     uint64_t magic;    // n / (page / 16) = n * magic >> 32 for n < 2^22
 };
 
-// What a row of a tree sees: the tokens in front of it, and nodes by its bits.
-struct TreeRow {
-    const uint32_t *bits;     // nullptr: no row, sees nothing
-    int words, prefix, kv;    // the tree's first token (below 0: its first nodes are not cached)
-    __device__ __forceinline__ TreeRow(const KvAttnArgs &a, const Seq &s, int qi, bool live)
-        : bits(live ? a.tree + (s.q0 + qi) * a.tree_words : nullptr), words(a.tree_words),
-          prefix(s.kv - s.lq), kv(s.kv) {}
-    __device__ __forceinline__ uint32_t word(int i) const { return i < words ? bits[i] : 0; }
-    // Tokens j .. j + 31, the first in the lowest bit.
-    __device__ __forceinline__ uint32_t window(int j) const {
-        if (!bits || j >= kv)
-            return 0;
-        const int node = j - prefix;
-        uint32_t w;
-        if (node <= -32)
-            w = ~0u;
-        else if (node < 0)
-            w = word(0) << -node | ((1u << -node) - 1);
-        else
-            w = (uint32_t)((word(node / 32) | (uint64_t)word(node / 32 + 1) << 32) >> node % 32);
-        return kv - j < 32 ? w & ((1u << (kv - j)) - 1) : w;
-    }
-    __device__ __forceinline__ bool any() const {
-        uint32_t w = bits && prefix > 0;       // else at most as many tokens as nodes
-        if (!bits)
-            return false;
-        for (int j = 0; w == 0 && j < kv; j += 32)
-            w = window(j);
-        return w != 0;
-    }
-};
-
 struct Job {
     bool found;
     Note note;
@@ -702,9 +670,19 @@ TreePlan plan_of(const KvShape &c, int64_t T, int seqs, int group, int max_kv) {
 
 size_t notes_bytes(const TreePlan &p) { return (1 + (size_t)p.tiles) * sizeof(Note); }
 
+// Calls whose sequences have few rows go to kv_attention.hip's kernel that reads keys straight into
+// matrix registers, 16 rows a workgroup: up to 16, above 128 channels, where one workgroup of this file's
+// fills a CU, up to 32. us there and here: 42 x 6 rows on 1088 tokens, 18 heads of 256, 99 and 159; 32 x
+// 16 on up to 8192, 8 heads of 128, 55 and 62, with 32 rows 60 and 60, all 8192 long 212 and 135.
+bool few_rows(const KvShape &c, int64_t T, int seqs, int group, int max_q) {
+    return (seqs == 1 ? T : std::min<int64_t>(max_q, T)) * group <= (c.dim <= 128 ? 16 : 32);
+}
+
 }  // namespace
 
-size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_kv) {
+size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
+    if (few_rows(c, T, seqs, group, max_q))
+        return kv_attention_workspace_bytes(c, T, seqs, group, max_q, max_kv);
     const TreePlan p = plan_of(c, T, seqs, group, max_kv);
     return p.target == 0 ? 0 : notes_bytes(p) + (size_t)p.grid * kRows * (c.dim + 4) * 4;
 }
@@ -712,6 +690,8 @@ size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group,
 hipError_t launch_kv_tree(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
     if (a.T * c.heads * a.group > INT32_MAX)
         return hipErrorInvalidValue;
+    if (few_rows(c, a.T, a.seqs, a.group, a.max_q))
+        return launch_kv_attention(c, a, ws, s);
     TreePlan plan = plan_of(c, a.T, a.seqs, a.group, a.max_kv);
     plan.notes = static_cast<Note *>(ws);
     plan.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + notes_bytes(plan));

@@ -117,7 +117,7 @@ w8a8_status attend(const uint16_t *q, int64_t q_token, int64_t q_head, const uin
     a.scale = __builtin_fabsf(scale) * 1.44269504088896341f;
     if (a.scale < 0x1p-126f)
         a.scale = 0x1p-126f;
-    const size_t need = tree ? kv_tree_workspace_bytes(c, T, seqs, group, max_kv)
+    const size_t need = tree ? kv_tree_workspace_bytes(c, T, seqs, group, a.max_q, max_kv)
                              : kv_attention_workspace_bytes(c, T, seqs, group, a.max_q, max_kv);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, kAlign)))
         return W8A8_ERR_WORKSPACE;
@@ -280,11 +280,12 @@ w8a8_status w8a8_kv_attention(const uint16_t *q, int64_t q_token, int64_t q_head
 }
 
 size_t w8a8_kv_tree_attention_workspace_bytes(int page, int heads, int dim, int fmt, int group,
-                                              int64_t T, int seqs, int max_kv) {
+                                              int64_t T, int seqs, int max_q, int max_kv) {
     KvShape c;
-    if (!cache_shape(c, 1, page, heads, dim, fmt) || group < 1 || T < 1 || seqs < 1 || max_kv < 0)
+    if (!cache_shape(c, 1, page, heads, dim, fmt) || group < 1 || T < 1 || seqs < 1 ||
+        max_q < 0 || max_kv < 0)
         return 0;
-    return kv_tree_workspace_bytes(c, T, seqs, group, max_kv);
+    return kv_tree_workspace_bytes(c, T, seqs, group, query_bound(max_q), max_kv);
 }
 
 w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
@@ -292,14 +293,14 @@ w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q
                                    int fmt, const int32_t *table, int64_t table_stride,
                                    int table_pages, const int32_t *kv_lens, const int32_t *q_starts,
                                    int64_t T, int seqs, int group, float scale, const int64_t *tree,
-                                   int tree_words, int max_kv, uint16_t *out, void *workspace,
-                                   size_t workspace_bytes, void *stream) {
+                                   int tree_words, int max_q, int max_kv, uint16_t *out,
+                                   void *workspace, size_t workspace_bytes, void *stream) {
     if (tree_words < 1 || tree_words > W8A8_KV_MAX_TREE_WORDS)
         return W8A8_ERR_ARG;
     if (T > 0 && seqs > 0 && !tree)
         return W8A8_ERR_NULL;
     return attend(q, q_token, q_head, cache, pages, page, heads, dim, fmt, table, table_stride, table_pages,
-                  kv_lens, q_starts, T, seqs, group, scale, 0, tree, tree_words, 0, max_kv, out,
+                  kv_lens, q_starts, T, seqs, group, scale, 0, tree, tree_words, max_q, max_kv, out,
                   workspace, workspace_bytes, stream);
 }
 

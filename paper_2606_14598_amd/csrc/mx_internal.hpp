@@ -80,7 +80,8 @@ size_t kv_attention_workspace_bytes(const KvShape &c, int64_t T, int seqs, int g
                                     int max_kv);
 hipError_t launch_kv_attention(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s);
 
-size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_kv);
+size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_q,
+                               int max_kv);
 hipError_t launch_kv_tree(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s);
 
 }  // namespace w8a8

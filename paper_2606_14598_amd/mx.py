@@ -305,7 +305,7 @@ def kv_tree_attention(q, cache, block_table, kv_lens, tree, *, fmt: str = "fp8",
     tree[q_starts[b] + i, n // 64] is set: itself and its ancestors (tree int64 [T, words], up to
     64 words). A query that sees nothing gives zeros. The weights are rounded to bf16, to two
     terms in sequences of up to 64 rows. q_starts may end before T: rows of q and the output behind the last sequence are neither read nor
-    written. max_kv as in kv_attention; max_q makes no difference here. Everything else is as there."""
+    written. max_q, max_kv as in kv_attention. Everything else is as there."""
     if not isinstance(tree, torch.Tensor) or tree.dtype != torch.int64:
         raise TypeError("tree must be an int64 torch.Tensor")
     return _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, False, tree, max_q, max_kv,
@@ -357,8 +357,9 @@ def _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, causal, tree, 
         nws = _bytes("w8a8_kv_attention_workspace_bytes", page, heads, dim, f, group, T, B, max_q, max_kv)
         name, rule = "w8a8_kv_attention", (int(causal), max_q, max_kv)
     else:
-        nws = _bytes("w8a8_kv_tree_attention_workspace_bytes", page, heads, dim, f, group, T, B, max_kv)
-        name, rule = "w8a8_kv_tree_attention", (_ptr(tree), tree.shape[1], max_kv)
+        nws = _bytes("w8a8_kv_tree_attention_workspace_bytes", page, heads, dim, f, group, T, B, max_q,
+                     max_kv)
+        name, rule = "w8a8_kv_tree_attention", (_ptr(tree), tree.shape[1], max_q, max_kv)
     ws = _workspace(nws, device, workspace)
     _launch(device, name, *at, *rule, _ptr(y), _ptr(ws), 0 if ws is None else ws.nbytes)
     return y

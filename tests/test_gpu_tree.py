@@ -112,7 +112,7 @@ def test_a_chain_is_the_causal_rule(fmt, dim, heads, group, nodes, kvs):
 def test_rows_behind_the_last_sequence():
     """q_starts that end before T: the rest of the output is left as it was, whatever the queries
     there hold; also where the keys are divided."""
-    for nodes, kvs in (([9, 30], [40, 300]), ([20, 70], [3000, 5000])):
+    for nodes, kvs in (([9, 30], [40, 300]), ([20, 70], [3000, 5000]), ([4, 1], [4000, 9000])):
         c = Tree("fp8", 128, 2, 4, 16, nodes, kvs, seed=6)
         want = c.run()
         n = sum(nodes)
@@ -120,7 +120,7 @@ def test_rows_behind_the_last_sequence():
         q[:n] = c.q.cuda()
         c.tree = torch.cat((c.tree, torch.full((50, c.tree.shape[1]), -1, device="cuda")))
         out = torch.full_like(q, 7.0)
-        c.run(q=q, out=out)
+        c.run(q=q, out=out, max_q=max(nodes))
         c.check(out[:n])
         assert (out[n:] == 7).all() and torch.allclose(out[:n].float(), want.float(), rtol=2 ** -6, atol=2 ** -6)
 
@@ -221,7 +221,7 @@ def test_graph_replays_with_other_trees():
     c = Tree("fp8", 128, 2, 4, 16, [20, 20], [700, 40], seed=12)
     q, table, out = c.q.cuda(), c.table.cuda(), None
     width = c.table.shape[1] * 16
-    n = w8a8.load_library().w8a8_kv_tree_attention_workspace_bytes(16, 2, 128, 0, 4, 40, 2, width)
+    n = w8a8.load_library().w8a8_kv_tree_attention_workspace_bytes(16, 2, 128, 0, 4, 40, 2, 20, width)
     work = torch.empty(n, dtype=torch.uint8, device="cuda")
     out = torch.empty_like(q)
 

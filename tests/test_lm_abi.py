@@ -67,23 +67,25 @@ def test_append_refusals(lib):
 
 def test_tree_refusals(lib):
     def call(q=F, cache=F, shape=CACHE, table=F, width=4, lens=F, starts=F, T=6, seqs=3, group=4,
-             scale=0.1, tree=F, words=1, max_kv=64, out=F, ws=F, n=1 << 40):
+             scale=0.1, tree=F, words=1, max_q=4, max_kv=64, out=F, ws=F, n=1 << 40):
         return lib.w8a8_kv_tree_attention(q, 1024, 128, cache, *shape, table, 4, width, lens, starts,
-                                          T, seqs, group, scale, tree, words, max_kv, out, ws, n, None)
+                                          T, seqs, group, scale, tree, words, max_q, max_kv, out, ws,
+                                          n, None)
     for c in BAD_CACHES:
         assert call(shape=c) == ARG
     for bad in (dict(words=0), dict(words=65), dict(group=0), dict(scale=float("nan")), dict(cache=ODD)):
         assert call(**bad) == ARG, bad
     for bad in (dict(tree=None), dict(q=None), dict(out=None), dict(lens=None), dict(table=None)):
         assert call(**bad) == NULL, bad
-    for bad in (dict(T=-1), dict(seqs=0), dict(max_kv=-1), dict(starts=None, seqs=4), dict(width=1 << 30)):
+    for bad in (dict(T=-1), dict(seqs=0), dict(max_q=-1), dict(max_kv=-1), dict(starts=None, seqs=4), dict(width=1 << 30)):
         assert call(**bad) == SHAPE, bad
     assert call(T=0, tree=None) == OK
     # long enough for several parts
-    big = dict(T=64, seqs=1, max_kv=100000, width=7000)
+    big = dict(T=64, seqs=1, max_q=64, max_kv=100000, width=7000)
     size = lib.w8a8_kv_tree_attention_workspace_bytes
-    need = size(16, 2, 128, 0, 4, 64, 1, 100000)
-    assert size(16, 2, 128, 0, 4, 64, 1, 512) == 0 and size(16, 2, 96, 0, 4, 64, 1, 100000) == 0
+    need = size(16, 2, 128, 0, 4, 64, 1, 64, 100000)
+    assert size(16, 2, 128, 0, 4, 64, 1, 64, 512) == 0 and size(16, 2, 96, 0, 4, 64, 1, 64, 100000) == 0
+    assert size(16, 2, 128, 0, 4, 64, 64, 0, 100000) == size(16, 2, 128, 0, 4, 64, 64, 1, 100000) > 0
     assert need > 0
     assert call(**big, n=need - 1) == WORK and call(**big, ws=None) == WORK and call(**big, ws=P(128)) == WORK
 
