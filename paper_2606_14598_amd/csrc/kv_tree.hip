@@ -595,10 +595,17 @@ kv_tree_join_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
     __shared__ f32x4 other_v[GROUPS][LANES];
     __shared__ float other_m[GROUPS], other_l[GROUPS];
     const Note job = plan.notes[1 + blockIdx.x];
-    if ((int)blockIdx.x >= plan.notes[0].used || job.used <= 1 ||
+    if ((int)blockIdx.x >= plan.notes[0].used || job.used <= 1)
+        return;
+    // With lengths that no call may have (sequences that overlap) there can be more pieces than a grid
+    // has, and notes that nobody wrote: nothing outside the buffers is touched for them either.
+    if ((unsigned)job.b >= (unsigned)a.seqs || (unsigned)job.head >= (unsigned)c.heads || job.slot < 0 ||
+        job.stride < 1 || job.used > plan.grid ||
         job.slot + (int64_t)(job.used - 1) * job.stride >= plan.grid)
         return;
     const Seq seq = sequence(c, a, job.b);
+    if ((unsigned)job.tile >= (unsigned)tiles_of(rows_of(a, seq)))
+        return;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, d = 4 * lane;
     const int rows = min(seq.lq * a.group - job.tile * kRows, kRows), q_heads = c.heads * a.group;
     const float *first = plan.part + (int64_t)job.slot * kRows * (D + 4);
@@ -658,9 +665,11 @@ TreePlan plan_of(const KvShape &c, int64_t T, int seqs, int group, int max_kv) {
     const bool divided = max_kv > kWholeTokens && seqs <= kSummed;
     p.target = divided ? (c.dim <= 128 ? 512 : 256) : 0;
     p.least = 128;
-    // pieces: a share less than their number for each row tile, and the target in all
+    // Pieces there can be: a row tile has its cost / share, rounded up, so all have one each and
+    // the call's cost / share together, which with a share of three quarters of cost / target is 4 / 3
+    // of the target (and some for the roundings of these floats).
     p.tiles = (int)std::min<int64_t>(blocks, INT32_MAX / 2);
-    p.grid = (int)std::min<int64_t>(blocks + p.target + p.target / 16, INT32_MAX / 2);
+    p.grid = (int)std::min<int64_t>(blocks + p.target + p.target / 2, INT32_MAX / 2);
     const uint32_t pb = (uint32_t)c.page / 16;
     p.magic = (((uint64_t)1 << 32) + pb - 1) / pb;
     p.notes = nullptr;

@@ -195,6 +195,13 @@ def test_nan_nodes_reach_only_who_sees_them(fmt, nodes, kv, node):
             assert (np.abs(y[ok, h] - want[ok]) <= mag[ok] * 3.5 * 2.0 ** -8).all()
 
 
+@pytest.mark.parametrize("seqs,heads,nodes,kv", [(70, 1, 20, 3000), (60, 1, 18, 2500), (9, 3, 33, 4100)])
+def test_more_pieces_than_run_at_once(seqs, heads, nodes, kv):
+    """Alike sequences whose row tiles make more pieces than the target: all of them have a workgroup."""
+    c = Tree("fp8", 64, heads, 1, 16, [nodes] * seqs, [kv] * seqs, seed=seqs)
+    c.check(c.run())
+
+
 def test_without_starts_strided_queries_and_a_buffer():
     c = Tree("fp8", 128, 2, 4, 16, [7, 7, 7], [20, 7, 333], seed=4)
     want = c.run()
