@@ -8,7 +8,10 @@
 // hang on the order of the sum: codes are determined bit by bit, but for sums that lie within
 // 2^-50 of a rounding border of r.
 //
-// Bound by memory: 2 (4 with a residual) bytes read and 1 or 17/32 (+ 2) written an element.
+// Bound by memory: 2 (4 with a residual) bytes read and 1 or 17/32 (+ 2) written an element. 4608 x
+// 4096 with a residual takes 22.7 us in int8 (5.8 TB/s; a large copy reaches 5.1), 2001 x 1000 in 4 bits
+// 4.1, one token of 4096 channels 2.4, two barriers and 64-bit root included. The sum in 64 bits costs a
+// conversion and a product an element, which the loads hide.
 #include "lm_internal.hpp"
 #include "mx_quant.hpp"
 
@@ -418,7 +421,8 @@ template <int FMT, int TPR, int NV, bool RES>
 hipError_t run_rows(const NormArgs &a, hipStream_t s) {
     constexpr int BS = norm_threads<TPR>(), RPB = BS / TPR;
     const int64_t groups = (a.R + RPB - 1) / RPB;
-    // A grid of at most 2048 threads a CU, whose workgroups get equally many row groups.
+    // A grid of at most 2048 threads a CU, whose workgroups get equally many row groups: weights stay
+    // in registers from one to the next.
     const int64_t most = 256 * 2048 / BS, turns = (groups + most - 1) / most;
     const dim3 grid((unsigned)((groups + turns - 1) / turns)), block(BS);
     const bool whole = a.K % 8 == 0 && aligned(a.x, 16) && aligned(a.weight, 16) &&
