@@ -13,9 +13,9 @@
 // at a time sorted and merged. The first values that a wavefront reads would all be collected: the
 // k-th largest of its lanes' maxima is a bound that k values reach.
 //
-// Bound by reading the logits once: 4096 x 131072 bf16 in 175 us without alternatives (6.1 TB/s; a
-// plain read of as much reaches 7.0), 187 with 5, 214 with 20; 1024 x 131072 float32 in 88. Beside that
-// read stand about 9 vector instructions a value, the exponential counted as four. One row of 131072
+// Bound by reading the logits once: 4096 x 131072 bf16 in 168 us without alternatives (6.4 TB/s; a
+// plain read of as much reaches 7.0), 183 with 5, 200 with 20; 1024 x 131072 float32 in 87. Beside that
+// read stand about 8 vector instructions a value, the exponential counted as four. One row of 131072
 // takes 5.2 us in two launches, 11.2 with 20 alternatives (the networks of the workgroups and of the
 // join, one after the other). us for loads without branches around them (a branch makes the compiler
 // wait for all in flight), the networks in registers and one bar a workgroup, 4096 x 131072 with 5:
@@ -173,6 +173,16 @@ __device__ __forceinline__ void merge_waiting(Best &b, Key *wait, int lane, int 
         set_bar(b, bar);
 }
 
+// The largest of three. fmaxf of values that come out of bit operations costs a second maximum each,
+// which quiets them (4096 x 131072 with 5 alternatives: 187 us, so 183). Without that a signalling NaN
+// hides what stands before it: the result is then another value of the three or a NaN, and the row's
+// results are NaN anyway.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // 16 bytes of a row: the values i .. i + PER - 1, as float32.
 template <bool F32>
 struct Unit {
@@ -209,10 +219,10 @@ struct Unit {
             return __uint_as_float(e & 1 ? raw[e / 2] & 0xFFFF0000u : raw[e / 2] << 16);
     }
     __device__ __forceinline__ float largest() const {
-        float m = (*this)[0];
+        float m = max3((*this)[0], (*this)[1], (*this)[2]);
 #pragma unroll
-        for (int e = 1; e < PER; ++e)
-            m = fmaxf(m, (*this)[e]);
+        for (int e = 3; e < PER; e += 2)
+            m = max3(m, (*this)[e], (*this)[e + 1 < PER ? e + 1 : e]);
         return m;
     }
 };
@@ -318,15 +328,12 @@ logprobs_kernel(LogprobArgs a, int splits, int64_t share, Part *parts, Key *keys
 
     // n units from value `at` of this lane on; those of a whole load all lie before `end`.
     const auto process = [&](const U (&x)[LOADS], int64_t at, bool first) __attribute__((always_inline)) {
-        float tops[LOADS], top = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            tops[u] = x[u].largest();
-            top = fmaxf(top, tops[u]);
-        }
+        static_assert(LOADS == 2);
+        const float tops[LOADS] = {x[0].largest(), x[1].largest()};
+        float top = max3(tops[0], tops[1], tops[1]);
         if (TOP && first) {
             // A bar that a.top values reach: the a.top-th largest of a wavefront's lanes' maxima (of
-            // lanes that have any; a NaN's lane counts by its other values), or the least of the
+            // lanes that have any; a NaN's lane counts by one of its values), or the least of the
             // wavefronts' (a.top / WAVES)-th.
             const uint32_t o = sort64<true>(at < end ? order_of(top) : 0u, lane);
             uint32_t bar = (uint32_t)__builtin_amdgcn_readlane((int)o, a.top - 1);

@@ -137,6 +137,42 @@ def test_rows_without_numbers(T, V):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,V,top", [(2560, 1, 1), (2561, 700, 5), (2563, 5000, 64), (2600, 8192, 0),
+                                     (2562, 515, 20)])
+def test_many_short_rows(dtype, T, V, top):
+    """Enough short rows for one wavefront each, the last workgroup's not all there; some of them masked,
+    without numbers, or with a token outside."""
+    x, t = _logits(T, V, dtype, T + V)
+    if V > 1:
+        x[5::7][torch.rand(len(x[5::7]), V, generator=torch.Generator().manual_seed(1)) < 0.6] = -torch.inf
+        x[5::7, V // 2] = 1.0
+    x[0], x[3, V // 3] = -torch.inf, float("nan")
+    out = w8a8.token_logprobs(x.cuda(), t.cuda(), top=top, temperature=0.8)
+    lp, ent, tl, ti = (o.cpu() for o in out)
+    for r in (0, 3):
+        assert lp[r].isnan() and ent[r].isnan() and tl[r].isnan().all() and ((ti[r] >= 0) & (ti[r] < V)).all()
+    ok = torch.ones(T, dtype=torch.bool)
+    ok[[0, 3]] = False
+    check([o[ok] for o in (lp, ent, tl, ti)], f64(x[ok]), t[ok].numpy(), top, 0.8)
+
+
+@pytest.mark.parametrize("dtype,signalling", [(BF, 0x7F81), (BF, -0x7F), (F32, 0x7F800001)])
+@pytest.mark.parametrize("T,V", [(4, 600), (3, 5000), (3, 40000), (2700, 600)])
+def test_signalling_nans(dtype, signalling, T, V):
+    """Alone, in front of, behind and between the largest values, and everywhere."""
+    x, t = _logits(T, V, dtype, 12)
+    t[:3] = torch.tensor([1, 2, 3])
+    bits = x.view(torch.int16 if dtype == BF else torch.int32)
+    bits[0, 37], bits[1, ::2], bits[2] = signalling, signalling, signalling
+    out = w8a8.token_logprobs(x.cuda(), t.cuda(), top=9)
+    lp, ent, tl, ti = (o.cpu() for o in out)
+    assert lp[:3].isnan().all() and ent[:3].isnan().all() and tl[:3].isnan().all()
+    assert ((ti >= 0) & (ti < V)).all() and all(len(set(r.tolist())) == 9 for r in ti[:3])
+    if T > 3:
+        check([o[3:] for o in (lp, ent, tl, ti)], f64(x[3:]), t[3:].numpy(), 9)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_strides_alignment_and_buffers(dtype):
     """Rows inside padded ones, from any element on; a caller's workspace; another stream."""
     x, t = _logits(5, 20001, dtype, 8)
