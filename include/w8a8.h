@@ -389,10 +389,11 @@ size_t w8a8_kv_attention_workspace_bytes(int page, int heads, int dim, int fmt, 
  * node sees its ancestors and itself; nodes past 64 * tree_words are seen by none, bits past lq
  * are ignored). tree_words is 1 to W8A8_KV_MAX_TREE_WORDS (else W8A8_ERR_ARG). The weights are
  * rounded to two bf16 terms (2^-16) where a sequence's rows lq * group, or the last of them behind
- * a multiple of 128, are up to 64; to one (2^-8) elsewhere. q_starts [seqs + 1] may end before T: rows behind the last
- * sequence are neither read nor written. max_q and max_kv are bounds as there: with few rows
- * (max_q * group) another kernel runs, up to 512 tokens one launch is enough. Everything else is as there. workspace: w8a8_kv_tree_attention_workspace_bytes(...) bytes, 256-byte aligned (NULL
- * allowed when that is 0). */
+ * a multiple of 128, are up to 64; to one (2^-8) elsewhere. q_starts [seqs + 1] may end before T:
+ * rows behind the last sequence are neither read nor written. max_q and max_kv are bounds as there:
+ * with few rows (max_q * group) another kernel runs, up to 512 tokens one launch is enough.
+ * Everything else is as there. workspace: w8a8_kv_tree_attention_workspace_bytes(...) bytes,
+ * 256-byte aligned (NULL allowed when that is 0). */
 #define W8A8_KV_MAX_TREE_WORDS 64
 w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
                                    const uint8_t *cache, int64_t pages, int page, int heads,
@@ -416,8 +417,8 @@ size_t w8a8_kv_tree_attention_workspace_bytes(int page, int heads, int dim, int 
  * positions: [T, axes]; any values whose product with inv_freq is below 2^50. inv_freq: [pairs].
  * Keys are quantized from float32, values as by w8a8_kv_write, into slots [T] (same rules;
  * padding is not written). Queries q [T, q_heads, dim] (strides in elements; q_heads 0: none) are
- * rounded to bf16 into q_out [T, q_heads, dim], contiguous, which must not overlap q, k or v;
- * padding's too. */
+ * rounded to bf16 into q_out [T, q_heads, dim], contiguous, padding's too; q_out must not lie
+ * anywhere between the first and last element of q, of k or of v (W8A8_ERR_ARG). */
 #define W8A8_ROPE_MAX_AXES 4
 w8a8_status w8a8_kv_append(uint8_t *cache, int64_t pages, int page, int heads, int dim, int fmt,
                            const uint16_t *q, int64_t q_token, int64_t q_head, int q_heads,
@@ -434,8 +435,9 @@ w8a8_status w8a8_kv_append(uint8_t *cache, int64_t pages, int page, int heads, i
  *   r = float32(1 / sqrt(sum_k h[k]^2 / K + eps)), the sum and the root in 64 bits;
  *   v[k] = (h[k] * r) * weight[k], float32 (weight NULL: ones),
  * and v as by w8a8_quantize_act or w8a8_mx4_quantize. x, residual, sum: [M,K] bf16; sum may be x
- * or residual itself, and is not written without a residual (NULL). weight: [K] float32, with
- * SmoothQuant's 1/s folded in where the linear is smoothed. eps above 0 (else W8A8_ERR_ARG). K is at
+ * or residual itself (but not part of them: W8A8_ERR_ARG), and is not written without a residual
+ * (NULL). weight: [K] float32, with SmoothQuant's 1/s folded in where the linear is smoothed. eps is
+ * finite and at least 2^-126 (else W8A8_ERR_ARG). K is at
  * most W8A8_MAX_K (int8) or W8A8_MX4_MAX_K (W8A8_ERR_K_OVERFLOW). For non-finite h or weight int8
  * results are unspecified; in 4 bits a block with a non-finite v is NaN (with a NaN in h that is all
  * of its row; an infinity makes r zero). */

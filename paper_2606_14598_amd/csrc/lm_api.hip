@@ -14,6 +14,12 @@ hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s); }
 w8a8_status from_hip(hipError_t e) { return e == hipSuccess ? W8A8_OK : W8A8_ERR_HIP; }
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// Two ranges of n bytes that share some but not all.
+bool partly_same(const void *p, const void *q, int64_t n) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a != b && (a > b ? a - b : b - a) < (uintptr_t)n;
+}
+
 w8a8_status norm(int fmt, const uint16_t *x, const uint16_t *residual, uint16_t *sum,
                  const float *weight, double eps, int64_t R, int64_t K, uint8_t *codes, float *scale,
                  uint8_t *scales, void *stream) {
@@ -21,7 +27,7 @@ w8a8_status norm(int fmt, const uint16_t *x, const uint16_t *residual, uint16_t 
         return W8A8_ERR_SHAPE;
     if (K > (fmt == NORM_INT8 ? W8A8_MAX_K : W8A8_MX4_MAX_K))
         return W8A8_ERR_K_OVERFLOW;
-    if (!(eps > 0.0) || !__builtin_isfinite(eps))
+    if (!(eps >= 0x1p-126) || !__builtin_isfinite(eps))       // below: 1 / sqrt(eps) may be no float32
         return W8A8_ERR_ARG;
     if (R == 0 || (K == 0 && fmt == NORM_MX4))
         return W8A8_OK;
@@ -29,6 +35,8 @@ w8a8_status norm(int fmt, const uint16_t *x, const uint16_t *residual, uint16_t 
         (fmt == NORM_MX4 && !scales))
         return W8A8_ERR_NULL;
     if (fmt == NORM_MX4 && (!aligned(codes, 16) || !aligned(scales, 16)))
+        return W8A8_ERR_ARG;
+    if (residual && (partly_same(sum, x, 2 * R * K) || partly_same(sum, residual, 2 * R * K)))
         return W8A8_ERR_ARG;
     NormArgs a;
     a.x = x;

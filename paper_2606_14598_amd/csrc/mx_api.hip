@@ -66,6 +66,12 @@ w8a8_status check_rows(const KvShape &c, const void *k, const void *v, const int
     return T > 0 && (!k || !v || !slots) ? W8A8_ERR_NULL : W8A8_OK;
 }
 
+// Whether the n bytes from p on reach into T rows of `heads` heads.
+bool overlaps(const void *p, int64_t n, const KvRows &r, int64_t T, int heads, int dim) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(r.p);
+    return a < b + 2 * ((T - 1) * r.token + (heads - 1) * r.head + dim) && b < a + n;
+}
+
 // The bound on a sequence's queries that a launch is laid out for: a loose one, so never 0.
 int query_bound(int max_q) { return max_q > 1 ? max_q : 1; }
 
@@ -343,6 +349,11 @@ w8a8_status w8a8_kv_append(uint8_t *cache, int64_t pages, int page, int heads, i
     a.q = {const_cast<uint16_t *>(q), q_token, q_head};
     a.k = {const_cast<uint16_t *>(k), k_token, k_head};
     a.v = {const_cast<uint16_t *>(v), v_token, v_head};
+    const int64_t out_bytes = 2 * T * q_heads * dim;
+    if (q_heads > 0 && (overlaps(q_out, out_bytes, a.q, T, q_heads, dim) ||
+                        overlaps(q_out, out_bytes, a.k, T, heads, dim) ||
+                        overlaps(q_out, out_bytes, a.v, T, heads, dim)))
+        return W8A8_ERR_ARG;
     a.q_out = q_out;
     a.q_heads = q_heads;
     a.slots = slots;

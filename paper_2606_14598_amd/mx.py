@@ -237,7 +237,7 @@ def kv_append(cache, k, v, slots, positions, inv_freq, *, q=None, fmt: str = "fp
     inv_freq fp32 [pairs]: up to head_dim / 2, channels past 2 pairs stay as they are. A pair is
     channels p and p + pairs, or 2p and 2p + 1 with interleaved. q bf16 [T, q heads, head_dim] (any
     strides of token and head): returned turned, rounded to bf16, contiguous, or in `out`, which may
-    not overlap q; padding's queries too. Returns None without q."""
+    not lie in q, k or v; padding's queries too. Returns None without q."""
     device = cache.device
     _check_heads(k, "k", device)
     _check_heads(v, "v", device)
@@ -304,8 +304,9 @@ def kv_tree_attention(q, cache, block_table, kv_lens, tree, *, fmt: str = "fp8",
     front of the tree, and query i of a sequence sees node n where bit n % 64 of
     tree[q_starts[b] + i, n // 64] is set: itself and its ancestors (tree int64 [T, words], up to
     64 words). A query that sees nothing gives zeros. The weights are rounded to bf16, to two
-    terms in sequences of up to 64 rows. q_starts may end before T: rows of q and the output behind the last sequence are neither read nor
-    written. max_q, max_kv as in kv_attention. Everything else is as there."""
+    terms in sequences of up to 64 rows. q_starts may end before T: rows of q and the output
+    behind the last sequence are neither read nor written. max_q, max_kv as in kv_attention.
+    Everything else is as there."""
     if not isinstance(tree, torch.Tensor) or tree.dtype != torch.int64:
         raise TypeError("tree must be an int64 torch.Tensor")
     return _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, False, tree, max_q, max_kv,

@@ -42,6 +42,34 @@ def test_norm_refusals(lib):
     assert a(None, None, None, None, 1e-6, 4, 0, None, None, None) == NULL   # scales are written
 
 
+def test_norm_refuses_what_its_formula_has_no_result_for(lib):
+    """An eps whose inverse root is past float32 (rows of zeros would be NaN), a sum that overwrites other
+    elements than its own."""
+    for f in (lib.w8a8_rms_norm_quantize, lib.w8a8_rms_norm_mx4_quantize):
+        for eps in (1e-100, 2.0 ** -127):
+            assert f(F, None, None, None, eps, 4, 64, F, F, None) == ARG
+        for x, r, s in ((1024, 8192, 1026), (1024, 8192, 1022), (8192, 1024, 1024 + 2 * 4 * 64 - 2),
+                        (8192, 8192 + 4096, 8192 + 4096 - 2 * 4 * 64 + 2)):
+            assert f(P(x), P(r), P(s), None, 1e-6, 4, 64, P(1 << 20), P(1 << 20), None) == ARG
+
+
+def test_append_refuses_queries_over_its_inputs(lib):
+    """Queries written where queries, keys or values are read: whole, the first or last element, and the
+    gaps between heads."""
+    T, q_heads, heads, dim = 3, 8, 2, 128
+
+    def call(q, k, v, out, q_token=q_heads * dim, q_head=dim):
+        return lib.w8a8_kv_append(F, *CACHE, P(q), q_token, q_head, q_heads, P(k), heads * dim, dim, P(v),
+                                  heads * dim, dim, F, F, 1, None, F, 64, 0, T, P(out), None)
+    size, far = 2 * T * q_heads * dim, (1 << 24, 1 << 25, 1 << 26)
+    for q_token, q_head in ((q_heads * dim, dim), (2 * q_heads * dim, dim), (dim, T * dim)):
+        last = 2 * ((T - 1) * q_token + (q_heads - 1) * q_head + dim - 1)
+        for out in (far[0], far[0] + last, far[0] - size + 2, far[0] + 2 * dim):
+            assert call(*far, out, q_token, q_head) == ARG
+    for at in far[1:]:
+        assert call(*far, at) == ARG and call(*far, at + 2 * (T * heads * dim - 1)) == ARG
+
+
 def test_append_refusals(lib):
     def call(cache=F, shape=CACHE, q=F, q_token=1024, q_head=128, q_heads=8, k=F, k_token=256,
              k_head=128, v=F, v_token=256, v_head=128, slots=F, positions=F, axes=1, sections=None,
