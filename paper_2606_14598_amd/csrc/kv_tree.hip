@@ -45,7 +45,7 @@ struct Note {
 };
 
 struct TreePlan {
-    int target;        // pieces that the keys are divided for, 0: every row tile is one
+    int target;        // pieces that the keys are divided for, 0: every row tile is one (find_tile)
     int least;         // tokens of a piece at least (a multiple of 64)
     int grid;          // pieces there can be
     int tiles;         // row tiles there can be
@@ -70,7 +70,7 @@ __device__ __forceinline__ int tiles_of(int rows) { return (rows + kRows - 1) / 
 
 // Pieces of a row tile of a sequence. share: their cost, in eighths of a token of a full tile.
 __device__ __forceinline__ int used_of(const TreePlan &plan, int kv, int rows, float share) {
-    if (plan.target == 0 || kv <= plan.least)
+    if (kv <= plan.least)
         return 1;
     const float tokens = fmaxf(share * (rows <= kRows / 2 ? 1.0f / 6.0f : 0.125f), (float)plan.least);
     return min((int)ceilf((float)kv * __builtin_amdgcn_rcpf(tokens)), (kv + plan.least - 1) / plan.least);
@@ -118,6 +118,41 @@ __device__ __forceinline__ float share_of(const KvShape &c, const TreePlan &plan
     return even * 0.75f;
 }
 
+// Row tile `index` of a call whose keys stay whole. Tiles are numbered with gaps: those of a sequence
+// from (its first row in the call) / kRows + (its number) on, which lies behind all tiles of those
+// before it. So the sequence is found among the starts, 64 at a time, and not by a sum over all of
+// them: 8192 sequences of up to 16 nodes on up to 512 tokens, 8 heads of 128, 7357 us by sums, 1850 so.
+__device__ __forceinline__ Job find_tile(const KvShape &c, const KvAttnArgs &a, int index) {
+    const int lane = threadIdx.x & 63;
+    const int64_t number = index / c.heads;
+    const auto first_of = [&](int b) {
+        const int64_t q0 = a.q_starts ? min(max((int64_t)a.q_starts[b], (int64_t)0), a.T)
+                                      : a.T / a.seqs * b;
+        return q0 * a.group / kRows + b;
+    };
+    Job job;
+    job.found = false;
+    int b = 0;
+    for (int step = a.seqs, left; step > 1;) {
+        left = min(step, a.seqs - b);              // sequences from b on, one of which it is
+        step = (left + 63) / 64;
+        const bool before = lane * step < left && first_of(b + lane * step) <= number;
+        b += max(__popcll(__ballot(before)) - 1, 0) * step;
+    }
+    job.seq = sequence(c, a, b);
+    const int64_t tile = number - first_of(b);
+    if (tile < 0 || tile >= tiles_of(rows_of(a, job.seq)))
+        return job;
+    job.found = true;
+    job.number = job.split = 0;
+    job.note.b = b;
+    job.note.head = index - (int)number * c.heads;
+    job.note.tile = (int)tile;
+    job.note.used = job.note.stride = 1;
+    job.note.slot = 0;
+    return job;
+}
+
 // Piece number `index` of the call.
 __device__ __forceinline__ Job find_job(const KvShape &c, const KvAttnArgs &a, const TreePlan &plan,
                                         int index) {
@@ -133,15 +168,11 @@ __device__ __forceinline__ Job find_job(const KvShape &c, const KvAttnArgs &a, c
         }
     };
     float share = 0.0f;
-    if (plan.target > 0) {
-        for (int i0 = (a.seqs - 1) / 64 * 64; i0 >= 0; i0 -= 64) {
-            fetch(i0 + lane);
-            share += (float)kv * (float)(tiles_of(rows) * eighths(rows));
-        }
-        share = share_of(c, plan, a.seqs, share, kv, rows);
-    } else {
-        fetch(lane);
+    for (int i0 = (a.seqs - 1) / 64 * 64; i0 >= 0; i0 -= 64) {
+        fetch(i0 + lane);
+        share += (float)kv * (float)(tiles_of(rows) * eighths(rows));
     }
+    share = share_of(c, plan, a.seqs, share, kv, rows);
     Job job;
     job.found = false;
     int pieces = 0, numbers = 0;           // in front of the 64 sequences at hand
@@ -229,7 +260,7 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
         if (threadIdx.x == 0)
             plan.notes[0].used = n;
     }
-    const Job job = find_job(c, a, plan, blockIdx.x);
+    const Job job = plan.target > 0 ? find_job(c, a, plan, blockIdx.x) : find_tile(c, a, blockIdx.x);
     if (!job.found)
         return;
     if (plan.target > 0 && job.split == 0 && threadIdx.x == 0 && job.number < plan.tiles)
@@ -665,21 +696,29 @@ int64_t blocks_of(const KvShape &c, int64_t T, int seqs, int group) {
 
 // Up to here keys stay whole: a second launch costs as much as it saves.
 constexpr int kWholeTokens = 512;
+// And up to here where row tiles alone make four rounds of what runs at once: lengths even out, and parts
+// are written and read for nothing. us divided and whole, 4 queries a head, heads of 128, lengths up to
+// 2000: 512 x 16 nodes, 8 heads 276, 229; 256 x 16 150, 135; 200 x 60 184, 164; with two rounds 128 x 16
+// of up to 8000 187, 248. Longer sequences stay divided: one of them among short ones would run alone.
+constexpr int kFullTokens = 4096;
 
 TreePlan plan_of(const KvShape &c, int64_t T, int seqs, int group, int max_kv) {
     TreePlan p;
     const int64_t blocks = blocks_of(c, T, seqs, group);
-    const bool divided = max_kv > kWholeTokens && seqs <= kSummed;
+    const int at_once = c.dim <= 128 ? 512 : 256;
+    const bool full = blocks > 4 * at_once && max_kv <= kFullTokens;
+    const bool divided = max_kv > kWholeTokens && seqs <= kSummed && !full;
     // What runs at once: two workgroups a CU, one above 128 channels. us with 384, 512 and 768: 32 trees
     // of 60 on 8192 326, 325, 353; 201 nodes on 40001 202, 220, 195 (168 once pieces fit one round).
-    p.target = divided ? (c.dim <= 128 ? 512 : 256) : 0;
+    p.target = divided ? at_once : 0;
     // 13 nodes on 2001 tokens: pieces of 128, 256 at least 13.6, 18.7.
     p.least = 128;
     // Pieces there can be: a row tile has its cost / share, rounded up, so all have one each and
     // the call's cost / share together, which with a share of three quarters of cost / target is 4 / 3
     // of the target (and some for the roundings of these floats).
     p.tiles = (int)std::min<int64_t>(blocks, INT32_MAX / 2);
-    p.grid = (int)std::min<int64_t>(blocks + p.target + p.target / 2, INT32_MAX / 2);
+    const int64_t numbers = c.heads * (T * group / kRows + seqs);          // as find_tile counts
+    p.grid = (int)std::min<int64_t>(divided ? blocks + p.target + p.target / 2 : numbers, INT32_MAX / 2);
     const uint32_t pb = (uint32_t)c.page / 16;
     p.magic = (((uint64_t)1 << 32) + pb - 1) / pb;
     p.notes = nullptr;

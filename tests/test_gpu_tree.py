@@ -109,6 +109,33 @@ def test_a_chain_is_the_causal_rule(fmt, dim, heads, group, nodes, kvs):
         assert torch.allclose(y.float(), Case.run(c, causal=causal).float(), rtol=2 ** -5, atol=2 ** -5)
 
 
+@pytest.mark.parametrize("seqs,most,uniform", [(2, 45, False), (63, 40, False), (64, 33, True), (65, 40, False),
+                                               (700, 40, False), (4097, 20, False), (4100, 17, True)])
+def test_whole_keys_of_many_sequences(seqs, most, uniform):
+    """Row tiles found by the sequences' starts: numbers of sequences around powers of 64, some of them
+    without queries, some of two tiles, with and without starts."""
+    g = random.Random(seqs)
+    nodes = [most if uniform else g.choice((0, 1, g.randint(0, most), most)) for _ in range(seqs)]
+    nodes[0] = max(nodes[0], 1)
+    kvs = [n + g.choice((0, 1, g.randint(0, 60))) for n in nodes]
+    c = Tree("fp8", 64, 1, 4, 16, nodes, kvs, seed=seqs)
+    starts = dict(q_starts=None) if uniform else {}
+    c.check(c.run(**starts, max_q=most, max_kv=112))
+
+
+def test_longer_keys_of_many_row_tiles():
+    """More row tiles than rounds of the card take: keys past one part's length stay whole, up to a bound
+    on the tokens, behind which they are divided."""
+    g = random.Random(2)
+    nodes = [g.randint(0, 9) for _ in range(290)]
+    c = Tree("fp4", 64, 8, 4, 16, nodes, [g.choice((0, 5, 30, 700, 1500)) for _ in nodes], seed=3)
+    need = [w8a8.load_library().w8a8_kv_tree_attention_workspace_bytes(16, 8, 64, 1, 4, sum(nodes), 290, 9, n)
+            for n in (1504, 5000)]
+    assert need[0] == 0 and need[1] > 0
+    for max_kv in (1504, 5000):
+        c.check(c.run(max_q=9, max_kv=max_kv))
+
+
 def test_rows_behind_the_last_sequence():
     """q_starts that end before T: the rest of the output is left as it was, whatever the queries
     there hold; also where the keys are divided."""
