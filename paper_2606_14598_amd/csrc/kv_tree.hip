@@ -14,16 +14,16 @@
 // lengths of a batch differ: the work is divided by what there is. The pieces of a call (a row tile
 // of a head and sequence, and a part of its keys) are numbered one after the other, about as many
 // as the card runs at once, each of about the same cost; a workgroup finds the piece of its own
-// number by a scan over the sequences. Partial results lie in the pieces' own slots of the workspace,
-// and a second launch joins those of each row tile, whose first piece has left a note where they are.
-// So everything follows from the lengths on the device, no row outside the sequences is read or
-// written, and sums have a fixed order.
+// number by a scan over the sequences (where keys stay whole, by a search among their starts). Partial
+// results lie in the pieces' own slots of the workspace, and a second launch joins those of each row
+// tile, whose first piece has left a note where they are. So everything follows from the lengths on the
+// device, no row outside the sequences is read or written, and sums have a fixed order.
 //
 // Bound by instructions where rows are many, as kv_attention.hip's kernel for many rows is: 32 trees of
 // 60 nodes on 8192 tokens each, 8 heads of 128, 4 queries a head, 315 us (800 TFLOP/s, 880 where no row
 // tile is partly filled); by reading the cache, with two workgroups a CU to hide its latency, where they
 // are few: 16 nodes on the same 163 us (3.4 TB/s). 32 trees of up to 60 nodes on up to 8192 tokens, all
-// different: 235 us where a sequence's keys were divided as the causal kernel divides them, 94 to 99 so.
+// different: 235 us where a sequence's keys were divided as the causal kernel divides them, 92 to 99 so.
 #include "kv_attention.hpp"
 
 #include <algorithm>

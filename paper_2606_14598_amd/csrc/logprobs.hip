@@ -15,8 +15,8 @@
 //
 // Bound by reading the logits once: 4096 x 131072 bf16 in 168 us without alternatives (6.4 TB/s; a
 // plain read of as much reaches 7.0), 183 with 5, 200 with 20; 1024 x 131072 float32 in 87. Beside that
-// read stand about 8 vector instructions a value, the exponential counted as four. One row of 131072
-// takes 5.2 us in two launches, 11.2 with 20 alternatives (the networks of the workgroups and of the
+// read stand about 10 vector instructions a value, the exponential counted as four. One row of 131072
+// takes 5.1 us in two launches, 11.0 with 20 alternatives (the networks of the workgroups and of the
 // join, one after the other). us for loads without branches around them (a branch makes the compiler
 // wait for all in flight), the networks in registers and one bar a workgroup, 4096 x 131072 with 5:
 // 285 before, 211; streaming loads and one fused operation a value less: 195.
