@@ -14,10 +14,11 @@
 // lengths of a batch differ: the work is divided by what there is. The pieces of a call (a row tile
 // of a head and sequence, and a part of its keys) are numbered one after the other, about as many
 // as the card runs at once, each of about the same cost; a workgroup finds the piece of its own
-// number by a scan over the sequences (where keys stay whole, by a search among their starts). Partial
-// results lie in the pieces' own slots of the workspace, and a second launch joins those of each row
-// tile, whose first piece has left a note where they are. So everything follows from the lengths on the
-// device, no row outside the sequences is read or written, and sums have a fixed order.
+// number by a scan over the sequences (where keys stay whole, by a search among their starts). Pieces of
+// row tiles that are divided have a slot each in the workspace for their partial results, and a second
+// launch joins those of each such tile, whose first piece has left a note where they are. So everything
+// follows from the lengths on the device, no row outside the sequences is read or written, and sums have
+// a fixed order.
 //
 // Bound by instructions where rows are many, as kv_attention.hip's kernel for many rows is: 32 trees of
 // 60 nodes on 8192 tokens each, 8 heads of 128, 4 queries a head, 315 us (800 TFLOP/s, 880 where no row
@@ -36,10 +37,10 @@ constexpr int kMostTiles = 1 << 20;            // counted of a sequence: far mor
 // Sequences over whose tokens a wavefront sums, 64 at a time; with more of them keys stay whole.
 constexpr int kSummed = 512;
 
-// Where the pieces of a row tile are.
+// Where the pieces of a divided row tile are.
 struct Note {
     int b, head, tile;
-    int used;          // pieces; of the first note: the row tiles of the call
+    int used;          // pieces; of the first note: the divided row tiles of the call
     int slot, stride;  // of the tile's first piece, and from one to the next
     int pad[2];
 };
@@ -48,16 +49,16 @@ struct TreePlan {
     int target;        // pieces that the keys are divided for, 0: every row tile is one (find_tile)
     int least;         // tokens of a piece at least (a multiple of 64)
     int grid;          // pieces there can be
-    int tiles;         // row tiles there can be
-    struct Note *notes;   // [1 + tiles]: the number of row tiles, then each of them
-    float *part;       // [grid][kRows][dim + 4]: O, m, l of a piece
+    int tiles, slots;  // divided row tiles there can be, and their pieces
+    struct Note *notes;   // [1 + tiles]: the number of divided row tiles, then each of them
+    float *part;       // [slots][kRows][dim + 4]: O, m, l of a piece
     uint64_t magic;    // n / (page / 16) = n * magic >> 32 for n < 2^22
 };
 
 struct Job {
     bool found;
     Note note;
-    int number, split; // of its row tile in the call, and of the piece in that
+    int number, split; // of its row tile among the divided ones, and of the piece in that
     Seq seq;
 };
 
@@ -153,9 +154,9 @@ __device__ __forceinline__ Job find_tile(const KvShape &c, const KvAttnArgs &a, 
     return job;
 }
 
-// Piece number `index` of the call.
+// Piece number `index` of the call. For piece 0, `divided` becomes the number of divided row tiles.
 __device__ __forceinline__ Job find_job(const KvShape &c, const KvAttnArgs &a, const TreePlan &plan,
-                                        int index) {
+                                        int index, int &divided) {
     const int lane = threadIdx.x & 63;
     // the first 64 sequences stay in registers
     int kv = 0, rows = 0;
@@ -175,7 +176,7 @@ __device__ __forceinline__ Job find_job(const KvShape &c, const KvAttnArgs &a, c
     share = share_of(c, plan, a.seqs, share, kv, rows);
     Job job;
     job.found = false;
-    int pieces = 0, numbers = 0;           // in front of the 64 sequences at hand
+    int pieces = 0, slots = 0, numbers = 0;          // in front of the 64 sequences at hand
     for (int i0 = 0; i0 < a.seqs; i0 += 64) {
         if (i0 > 0)
             fetch(i0 + lane);
@@ -184,9 +185,11 @@ __device__ __forceinline__ Job find_job(const KvShape &c, const KvAttnArgs &a, c
         const int most = plan.grid + 1;
         const int own_tiles = (int)min((int64_t)c.heads * tiles, (int64_t)most);
         const int own = (int)min((int64_t)own_tiles * used, (int64_t)most);
-        const int sum = lanes_scan(own), sum_tiles = lanes_scan(own_tiles);
+        // what is not divided has no slots and no note
+        const int cut = used > 1 ? own : 0, cut_tiles = used > 1 ? own_tiles : 0;
+        const int sum = lanes_scan(own), sum_cut = lanes_scan(cut), sum_tiles = lanes_scan(cut_tiles);
         const uint64_t past = __ballot(pieces + sum > index);
-        if (past) {
+        if (past && !job.found) {
             const int at = __builtin_ctzll(past);
             const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
             const int first = pieces + of(sum - own);
@@ -200,28 +203,18 @@ __device__ __forceinline__ Job find_job(const KvShape &c, const KvAttnArgs &a, c
             // heads fastest: the row tiles of a head go to one XCD where heads come in eights
             job.note.tile = in / (uint32_t)c.heads;
             job.note.head = in - job.note.tile * c.heads;
-            job.note.slot = first + in;
-            job.number = numbers + of(sum_tiles - own_tiles) + in;
+            job.note.slot = slots + of(sum_cut - cut) + in;
+            job.number = numbers + of(sum_tiles - cut_tiles) + in;
             job.seq = sequence(c, a, job.note.b);
-            return job;
+            if (index > 0)
+                return job;
         }
         pieces = min(pieces + __builtin_amdgcn_readlane(sum, 63), most);
+        slots = min(slots + __builtin_amdgcn_readlane(sum_cut, 63), most);
         numbers = min(numbers + __builtin_amdgcn_readlane(sum_tiles, 63), most);
     }
+    divided = numbers;
     return job;
-}
-
-// All row tiles of the call: what find_job counts, to its end.
-__device__ __forceinline__ int count_tiles(const KvShape &c, const KvAttnArgs &a, const TreePlan &plan) {
-    int n = 0;
-    for (int i0 = 0; i0 < a.seqs; i0 += 64) {
-        int tiles = 0;
-        if (i0 + (int)(threadIdx.x & 63) < a.seqs)
-            tiles = tiles_of(rows_of(a, sequence(c, a, i0 + (threadIdx.x & 63))));
-        tiles = (int)min((int64_t)c.heads * tiles, (int64_t)plan.tiles);
-        n = min(n + __builtin_amdgcn_readlane(lanes_scan(tiles), 63), plan.tiles);
-    }
-    return n;
 }
 
 // The other half's value beside this one's: lanes l and l ^ 32 hold the same row.
@@ -255,16 +248,19 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
     __shared__ uint32_t other_nan[2][64];
     static_assert(sizeof(keys) >= 2 * 64 * (D / 2) * sizeof(float), "O of two wavefronts");
 
-    if (blockIdx.x == 0 && plan.target > 0) {
-        const int n = count_tiles(c, a, plan);
-        if (threadIdx.x == 0)
-            plan.notes[0].used = n;
-    }
-    const Job job = plan.target > 0 ? find_job(c, a, plan, blockIdx.x) : find_tile(c, a, blockIdx.x);
+    int divided = 0;
+    const Job job = plan.target > 0 ? find_job(c, a, plan, blockIdx.x, divided) : find_tile(c, a, blockIdx.x);
+    if (plan.target > 0 && blockIdx.x == 0 && threadIdx.x == 0)
+        plan.notes[0].used = min(divided, plan.tiles);
     if (!job.found)
         return;
-    if (plan.target > 0 && job.split == 0 && threadIdx.x == 0 && job.number < plan.tiles)
-        plan.notes[1 + job.number] = job.note;
+    const int64_t slot = job.note.slot + (int64_t)job.split * job.note.stride;
+    if (job.note.used > 1) {
+        if (slot >= plan.slots)        // with lengths that no call may have (sequences that overlap)
+            return;
+        if (job.split == 0 && threadIdx.x == 0 && job.number < plan.tiles)
+            plan.notes[1 + job.number] = job.note;
+    }
     const Seq seq = job.seq;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -575,7 +571,6 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
             return;
         const int64_t out_row = (seq.q0 + qi) * q_heads + qh;
         const float inv = inverse(l, m);
-        const int64_t slot = job.note.slot + (int64_t)job.split * job.note.stride;
         float *const part = plan.part + (slot * kRows + row - job.note.tile * kRows) * (D + 4);
 #pragma unroll
         for (int f = 0; f < F; ++f) {
@@ -637,8 +632,8 @@ kv_tree_join_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
     // With lengths that no call may have (sequences that overlap) there can be more pieces than a grid
     // has, and notes that nobody wrote: nothing outside the buffers is touched for them either.
     if ((unsigned)job.b >= (unsigned)a.seqs || (unsigned)job.head >= (unsigned)c.heads || job.slot < 0 ||
-        job.stride < 1 || job.used > plan.grid ||
-        job.slot + (int64_t)(job.used - 1) * job.stride >= plan.grid)
+        job.stride < 1 || job.used > plan.slots ||
+        job.slot + (int64_t)(job.used - 1) * job.stride >= plan.slots)
         return;
     const Seq seq = sequence(c, a, job.b);
     if ((unsigned)job.tile >= (unsigned)tiles_of(rows_of(a, seq)))
@@ -716,9 +711,14 @@ TreePlan plan_of(const KvShape &c, int64_t T, int seqs, int group, int max_kv) {
     // Pieces there can be: a row tile has its cost / share, rounded up, so all have one each and
     // the call's cost / share together, which with a share of three quarters of cost / target is 4 / 3
     // of the target (and some for the roundings of these floats).
-    p.tiles = (int)std::min<int64_t>(blocks, INT32_MAX / 2);
     const int64_t numbers = c.heads * (T * group / kRows + seqs);          // as find_tile counts
     p.grid = (int)std::min<int64_t>(divided ? blocks + p.target + p.target / 2 : numbers, INT32_MAX / 2);
+    // A divided row tile has a cost of more than one share (x shares make ceil(x) pieces), so there are
+    // at most 4 / 3 of the target of them, and as ceil(x) < 2 x above 1, 8 / 3 of it pieces: both rounded up,
+    // which is more than the floats are off. So the workspace does not grow with the call: 92 MB at 128
+    // channels. With a slot a piece of every row tile 512 trees of 60 nodes took 848 MB.
+    p.tiles = (int)std::min<int64_t>(blocks, (4 * p.target + 2) / 3);
+    p.slots = std::min(p.grid, (8 * p.target + 2) / 3);
     const uint32_t pb = (uint32_t)c.page / 16;
     p.magic = (((uint64_t)1 << 32) + pb - 1) / pb;
     p.notes = nullptr;
@@ -742,7 +742,7 @@ size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group,
     if (few_rows(c, T, seqs, group, max_q))
         return kv_attention_workspace_bytes(c, T, seqs, group, max_q, max_kv);
     const TreePlan p = plan_of(c, T, seqs, group, max_kv);
-    return p.target == 0 ? 0 : notes_bytes(p) + (size_t)p.grid * kRows * (c.dim + 4) * 4;
+    return p.target == 0 ? 0 : notes_bytes(p) + (size_t)p.slots * kRows * (c.dim + 4) * 4;
 }
 
 hipError_t launch_kv_tree(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
@@ -753,17 +753,16 @@ hipError_t launch_kv_tree(const KvShape &c, const KvAttnArgs &a, void *ws, hipSt
     TreePlan plan = plan_of(c, a.T, a.seqs, a.group, a.max_kv);
     plan.notes = static_cast<Note *>(ws);
     plan.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + notes_bytes(plan));
-    const int64_t blocks = blocks_of(c, a.T, a.seqs, a.group);
-    if (!launchable(plan.grid, 256) || !launchable(blocks, 256))
+    if (!launchable(plan.grid, 256))
         return hipErrorInvalidValue;
     // The join's workgroups a row tile: a row a group of lanes, or, with few tiles, a row each.
-    const int64_t join_parts = std::max<int64_t>(16, std::min<int64_t>(128, 8192 / blocks));
+    const int join_parts = std::max(16, std::min(128, 8192 / std::max(plan.tiles, 1)));
     const auto run = [&](auto dim, auto format) {
         constexpr int F = decltype(format)::value, D = decltype(dim)::value;
         hipLaunchKernelGGL((kv_tree_kernel<F, D>), dim3((unsigned)plan.grid), dim3(256), 0, s, c, a, plan);
         if (plan.target > 0 && hipPeekAtLastError() == hipSuccess)
-            hipLaunchKernelGGL((kv_tree_join_kernel<D>), dim3((unsigned)blocks, (unsigned)join_parts), dim3(256),
-                               0, s, c, a, plan);
+            hipLaunchKernelGGL((kv_tree_join_kernel<D>), dim3((unsigned)plan.tiles, (unsigned)join_parts),
+                               dim3(256), 0, s, c, a, plan);
         return hipGetLastError();
     };
     const auto go = [&](auto dim) {

@@ -182,3 +182,18 @@ def test_references_on_worked_cases():
     lp, h, tl, ti = logprobs(np.array([[0.0, np.log(3.0), -np.inf]]), np.array([0]), 2, 1.0)
     assert np.isclose(lp[0], np.log(0.25)) and ti.tolist() == [[1, 0]] and np.isclose(tl[0, 0], np.log(0.75))
     assert np.isclose(h[0], -(0.25 * np.log(0.25) + 0.75 * np.log(0.75)))
+
+
+def test_tree_workspace_does_not_grow_with_the_call(lib):
+    """Partial results of 8 / 3 of the workgroups that run at once (512 of two a CU, 256 above 128
+    channels), 128 rows of dim + 4 float32 each, and notes of 32 bytes: whatever the queries and sequences.
+    (Up to 32 rows a sequence another kernel may run, which may need none.)"""
+    size = lib.w8a8_kv_tree_attention_workspace_bytes
+    for dim, at_once in ((64, 512), (128, 512), (192, 256), (256, 256)):
+        most = (8 * at_once / 3 + 1) * 128 * (dim + 4) * 4 + (4 * at_once / 3 + 2) * 32
+        for seqs in (1, 3, 64, 512):
+            for nodes in (13, 60, 300, 4000):
+                for max_kv in (4097, 32768, 1 << 24):
+                    for heads, group in ((8, 4), (1, 64), (128, 1)):
+                        n = size(64, heads, dim, 0, group, seqs * nodes, seqs, nodes, max_kv)
+                        assert n <= most and (n > 0 or nodes * group <= 32), (dim, seqs, nodes, max_kv, heads, group, n)
