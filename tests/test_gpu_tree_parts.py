@@ -1,11 +1,16 @@
-"""Tree attention whose keys are divided among workgroups: the parts' place in the workspace."""
+"""Tree attention whose keys are divided among workgroups: the parts' place in the workspace, and
+keys that stay whole over several chunks of page places (4096 tokens), at every number of channels."""
 import random
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2606_14598_amd as w8a8
 from _helpers import say
+from _lm_ref import tree_visible
+from _mx_ref import f64
+from test_gpu_kv import _kv
 from test_gpu_tree import Tree
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +48,49 @@ def test_most_parts_and_a_workspace_in_turn():
         c = cases[i]
         c.check(c.run(max_q=max(c.qs), max_kv=max(c.kvs), workspace=work[:n]))
         assert (work[n:] == 0x7F).all()
+
+
+LONG = [
+    # heads, group, nodes, tokens: a row tile of 128 rows beside one of up to 64, and in the second some
+    # sequences without either
+    (1, 1, [180], [9001]),
+    (1, 2, [40, 3, 70], [9100, 4097, 8200]),
+]
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_long_keys_at_every_width(fmt, dim, case):
+    """Keys divided into more parts than one group of lanes joins, and whole, which is three chunks."""
+    heads, group, nodes, kvs = LONG[case]
+    say(f"long {fmt} {dim} {LONG[case]}")
+    c = Tree(fmt, dim, heads, group, 48, nodes, kvs, seed=dim + case)
+    for max_kv in (max(kvs), 512):
+        assert (_size(c, sum(nodes), len(nodes), max(nodes), max_kv) > 0) == (max_kv > 512)
+        y = c.run(max_q=max(nodes), max_kv=max_kv)
+        c.check(y)
+        assert torch.equal(y, c.run(max_q=max(nodes), max_kv=max_kv))
+
+
+@pytest.mark.parametrize("dim", [128, 192, 256])
+@pytest.mark.parametrize("at", [20, 5000, 8500, 8900, -130])
+def test_nan_in_long_keys(dim, at):
+    """A NaN key and value in the first, second and third chunk, which every row sees, and in a node (the tree
+    begins at 8861): in those who see it, the value's block alone."""
+    nodes, kv = 140, 9001
+    j = at % kv
+    for part in (0, 1):
+        c = Tree("fp8", dim, 1, 1, 16, [nodes], [kv], seed=dim)
+        new = _kv(kv, 1, dim, 8)
+        new[j, part, 0, 40] = float("nan")
+        pages = c.table[0].tolist()
+        c.write(new, [pages[i // 16] * 16 + i % 16 for i in range(kv)])
+        see = tree_visible(c.bits, nodes, kv)
+        bad = np.zeros((nodes, 1, dim), bool)
+        bad[see[:, j]] = True
+        if part == 1:
+            bad[:, :, :32], bad[:, :, 64:] = False, False
+        assert see[:, j].any() and see[:, j].all() == (j < kv - nodes)
+        for max_kv in (kv, 512):
+            assert np.array_equal(np.isnan(f64(c.run(max_kv=max_kv))), bad)
