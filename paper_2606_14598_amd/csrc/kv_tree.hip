@@ -217,12 +217,6 @@ __device__ __forceinline__ Job find_job(const KvShape &c, const KvAttnArgs &a, c
     return job;
 }
 
-// The other half's value beside this one's: lanes l and l ^ 32 hold the same row.
-__device__ __forceinline__ u32x2 halves_of(float v) {
-    return __builtin_bit_cast(
-        u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
-}
-
 // A piece: 64 tokens at a time are decoded once into LDS for all four wavefronts, between the
 // products of the 64 before. A wavefront has 32 rows and all 64 tokens of each step, or, in tiles
 // of up to 64 rows, 32 rows and 32 of the tokens; then two wavefronts' results are joined in LDS.
@@ -447,7 +441,7 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         top = fmaxf(top, s[t][i]);
-                const u32x2 tops = halves_of(top);
+                const u32x2 tops = both_halves(top);
                 top = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])) * a.scale, m);
                 if (__any(top > m + kSlack)) {
                     keep_branch();
@@ -532,7 +526,7 @@ kv_tree_kernel(KvShape c, KvAttnArgs a, TreePlan plan) {
             }
         }
 
-        const u32x2 ls = halves_of(l);
+        const u32x2 ls = both_halves(l);
         l = __uint_as_float(ls[0]) + __uint_as_float(ls[1]);
         if constexpr (TG > 1) {
             // The other tokens' m, l and O of the same rows, lane by lane.
