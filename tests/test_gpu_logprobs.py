@@ -247,3 +247,11 @@ def test_graph_replays(T, V):
         torch.cuda.synchronize()
         got = [o.clone() for o in out]
         assert all(torch.equal(a, b) for a, b in zip(got, w8a8.token_logprobs(x, t, top=5)))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,V,top", [(2560, 12001, 5), (2561, 16384, 20), (2560, 16385, 5), (2559, 16384, 3)])
+def test_longest_short_rows(dtype, T, V, top):
+    """Rows too long to stay whole where they are few, up to the longest that a wavefront takes, and just
+    past that rule in length and number."""
+    test_many_short_rows(dtype, T, V, top)
