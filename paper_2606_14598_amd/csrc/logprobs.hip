@@ -29,8 +29,12 @@ namespace w8a8 {
 namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * 64;
-// Log2 of how far a lane's maximum may rise before its sums are rescaled: s stays below 2^20 V.
-constexpr float kSlack = 20.0f;
+// Log2 of how far a lane's maximum may rise before its sums are rescaled. What it lags behind stands in
+// log2 s and in t / s, whose difference is the entropy, and every weight added to t beside a larger one
+// rounds at its size: up to 20 the entropy of 3000 x 16000 sharpened logits was 4 10^-6 off, in the
+// mean, up to 4 it is 3 10^-7, as by float32 sums relative to the row's maximum. us up to 20, 4 and 0:
+// 4096 x 131072 with 5 alternatives 178, 180, 182, 2500 x 30000 41.3, 41.8, 42.0.
+constexpr float kSlack = 4.0f;
 // Up to 2^24 the rounding of m is a distance of 1 at most, which s and log p have alike.
 constexpr float kFloor = -0x1p24f, kCeiling = 0x1p24f;
 constexpr double kLn2 = 0.693147180559945309;

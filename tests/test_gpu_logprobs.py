@@ -255,3 +255,23 @@ def test_longest_short_rows(dtype, T, V, top):
     """Rows too long to stay whole where they are few, up to the longest that a wavefront takes, and just
     past that rule in length and number."""
     test_many_short_rows(dtype, T, V, top)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,V", [(1100, 16384), (2600, 16384), (2, 70000)])
+def test_entropy_behind_a_late_peak(dtype, T, V):
+    """Whole logits in powers of two (the temperature is log2 e): 0 first, then one of 19 in each few, then
+    -1. Relative to about the largest of them every weight is a power of two and the sums of a lane have at
+    most 24 bits, so they are exact; relative to what a lane saw first, the rest is lost beside 19 2^19. With
+    log2 s below 16: its ulp 2^-20; up to 20 joins of s and of t (below s), 2^-23 each, 2^-19 together; the
+    quotient's and the difference's roundings, 2^-21: in all 2^-18, times ln 2. (A token's logits are
+    exact, and an exponent of up to 20 is off by 2^-25 of it where the temperature is no float32.)"""
+    temperature = float(np.float32(1.44269504088896341))
+    x = torch.full((T, V), -1.0)
+    x[:, :4096] = 0.0
+    x[:, 4096:6144:8] = 19.0
+    t = torch.arange(T) % V
+    out = w8a8.token_logprobs(x.to(dtype).cuda(), t.cuda(), top=3, temperature=temperature)
+    check(out, f64(x), t.numpy(), 3, temperature)
+    want = logprobs(f64(x[:1]), t[:1].numpy(), 3, temperature)[1][0]
+    assert np.abs(f64(out[1]) - want).max() <= 2.0 ** -18 * np.log(2), (f64(out[1])[0], want)
