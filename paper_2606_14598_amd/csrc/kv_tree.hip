@@ -726,14 +726,22 @@ size_t notes_bytes(const TreePlan &p) { return (1 + (size_t)p.tiles) * sizeof(No
 // matrix registers, 16 rows a workgroup: up to 16, above 128 channels, where one workgroup of this file's
 // fills a CU, up to 32. us there and here: 42 x 6 rows on 1088 tokens, 18 heads of 256, 99 and 159; 32 x
 // 16 on up to 8192, 8 heads of 128, 55 and 62, with 32 rows 60 and 60, all 8192 long 212 and 135.
-bool few_rows(const KvShape &c, int64_t T, int seqs, int group, int max_q) {
-    return (seqs == 1 ? T : std::min<int64_t>(max_q, T)) * group <= (c.dim <= 128 ? 16 : 32);
+//
+// That kernel has a part for every row of the call in each of its splits, 68 MB at most where T is what the
+// sequences have, but without end where the call is laid out for more: 4 sequences of 4 nodes on 131072
+// tokens in 8192 rows 17.7 GB. Those go to this file's: in 16 rows (there) 204 us, in 1024 (here) 246, on
+// 8192 tokens 30 and 30, with heads of 256 43 and 54.
+constexpr size_t kFewBytes = size_t(1) << 27;
+
+bool few_rows(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
+    return (seqs == 1 ? T : std::min<int64_t>(max_q, T)) * group <= (c.dim <= 128 ? 16 : 32) &&
+           kv_attention_workspace_bytes(c, T, seqs, group, max_q, max_kv) <= kFewBytes;
 }
 
 }  // namespace
 
 size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group, int max_q, int max_kv) {
-    if (few_rows(c, T, seqs, group, max_q))
+    if (few_rows(c, T, seqs, group, max_q, max_kv))
         return kv_attention_workspace_bytes(c, T, seqs, group, max_q, max_kv);
     const TreePlan p = plan_of(c, T, seqs, group, max_kv);
     return p.target == 0 ? 0 : notes_bytes(p) + (size_t)p.slots * kRows * (c.dim + 4) * 4;
@@ -742,7 +750,7 @@ size_t kv_tree_workspace_bytes(const KvShape &c, int64_t T, int seqs, int group,
 hipError_t launch_kv_tree(const KvShape &c, const KvAttnArgs &a, void *ws, hipStream_t s) {
     if (a.T * c.heads * a.group > INT32_MAX)
         return hipErrorInvalidValue;
-    if (few_rows(c, a.T, a.seqs, a.group, a.max_q))
+    if (few_rows(c, a.T, a.seqs, a.group, a.max_q, a.max_kv))
         return launch_kv_attention(c, a, ws, s);
     TreePlan plan = plan_of(c, a.T, a.seqs, a.group, a.max_kv);
     plan.notes = static_cast<Note *>(ws);

@@ -94,3 +94,21 @@ def test_nan_in_long_keys(dim, at):
         assert see[:, j].any() and see[:, j].all() == (j < kv - nodes)
         for max_kv in (kv, 512):
             assert np.array_equal(np.isnan(f64(c.run(max_kv=max_kv))), bad)
+
+
+@pytest.mark.parametrize("dim,T", [(128, 9), (128, 500), (128, 9000), (256, 5000)])
+def test_few_rows_in_a_call_laid_out_for_many(dim, T):
+    """Three sequences of up to 4 nodes in T rows: those behind them are left as they were, whichever
+    kernel runs."""
+    c = Tree("fp8", dim, 2, 4, 16, [4, 1, 4], [5000, 1700, 3], seed=5)
+    width = c.table.shape[1] * 16
+    assert 0 < _size(c, T, 3, 4, width) <= 1 << 27
+    q = torch.full((T, 8, dim), float("nan"), dtype=torch.bfloat16, device="cuda")
+    q[:9] = c.q.cuda()
+    c.tree = torch.cat((c.tree, torch.full((T - 9, 1), -1, device="cuda")))
+    out = torch.full_like(q, 7.0)
+    for bounds in ({"max_q": 4}, {"max_q": 4, "max_kv": 512}, {"max_q": 1}, {}):
+        out[:9] = 7.0
+        c.run(q=q, out=out, **bounds)
+        c.check(out[:9])
+        assert (out[9:] == 7).all()

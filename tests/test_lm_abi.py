@@ -197,3 +197,15 @@ def test_tree_workspace_does_not_grow_with_the_call(lib):
                     for heads, group in ((8, 4), (1, 64), (128, 1)):
                         n = size(64, heads, dim, 0, group, seqs * nodes, seqs, nodes, max_kv)
                         assert n <= most and (n > 0 or nodes * group <= 32), (dim, seqs, nodes, max_kv, heads, group, n)
+
+
+def test_tree_workspace_of_few_rows_does_not_grow_with_padding(lib):
+    """Calls laid out for more queries than their sequences have (q_starts may end before T), and a max_q
+    below what there is: up to 2^27 bytes."""
+    size = lib.w8a8_kv_tree_attention_workspace_bytes
+    for dim in (64, 128, 192, 256):
+        for heads, group in ((8, 4), (1, 1), (18, 1), (128, 1)):
+            for T in (16, 1024, 8192, 100000):
+                for seqs, max_q in ((1, 4), (2, 1), (4, 4), (64, 2), (600, 1)):
+                    for max_kv in (513, 8192, 131072, 1 << 24):
+                        assert size(64, heads, dim, 0, group, T, seqs, max_q, max_kv) <= 1 << 27
