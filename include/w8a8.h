@@ -389,11 +389,15 @@ size_t w8a8_kv_attention_workspace_bytes(int page, int heads, int dim, int fmt, 
  * node sees its ancestors and itself; nodes past 64 * tree_words are seen by none, bits past lq
  * are ignored). tree_words is 1 to W8A8_KV_MAX_TREE_WORDS (else W8A8_ERR_ARG). The weights are
  * rounded to two bf16 terms (2^-16) where a sequence's rows lq * group, or the last of them behind
- * a multiple of 128, are up to 64; to one (2^-8) elsewhere. q_starts [seqs + 1] may end before T:
- * rows behind the last sequence are neither read nor written. max_q and max_kv are bounds as there:
- * with few rows (max_q * group) another kernel runs, up to 512 tokens one launch is enough.
- * Everything else is as there. workspace: w8a8_kv_tree_attention_workspace_bytes(...) bytes,
- * 256-byte aligned (NULL allowed when that is 0). */
+ * a multiple of 128, are up to 64; to one (2^-8) elsewhere. Keys are divided by the lengths of all
+ * sequences of a call, and a weight is rounded relative to the largest of its part: an output may
+ * differ by such roundings with the other sequences of its call. Up to 512 sequences keys are divided;
+ * with more of them a long sequence among short ones runs by itself, one workgroup a head and 128
+ * rows (8 nodes on 100000 tokens beside 512 others 1.9 ms, beside 511 0.3). q_starts [seqs + 1] may
+ * end before T: rows behind the last sequence are neither read nor written. max_q and max_kv are
+ * bounds as there: with few rows (max_q * group) another kernel runs, up to 512 tokens one launch is
+ * enough. Everything else is as there. workspace: w8a8_kv_tree_attention_workspace_bytes(...) bytes
+ * (at most 2^27, however many queries and sequences), 256-byte aligned (NULL allowed when that is 0). */
 #define W8A8_KV_MAX_TREE_WORDS 64
 w8a8_status w8a8_kv_tree_attention(const uint16_t *q, int64_t q_token, int64_t q_head,
                                    const uint8_t *cache, int64_t pages, int page, int heads,
@@ -438,7 +442,7 @@ w8a8_status w8a8_kv_append(uint8_t *cache, int64_t pages, int page, int heads, i
  * or residual itself (but not part of them: W8A8_ERR_ARG), and is not written without a residual
  * (NULL). weight: [K] float32, with SmoothQuant's 1/s folded in where the linear is smoothed. eps is
  * finite and at least 2^-126 (else W8A8_ERR_ARG). K is at
- * most W8A8_MAX_K (int8) or W8A8_MX4_MAX_K (W8A8_ERR_K_OVERFLOW). For non-finite h or weight int8
+ * most W8A8_MAX_K (int8) or W8A8_MX4_MAX_K (W8A8_ERR_K_OVERFLOW). For non-finite h, weight or v int8
  * results are unspecified; in 4 bits a block with a non-finite v is NaN (with a NaN in h that is all
  * of its row; an infinity makes r zero). */
 w8a8_status w8a8_rms_norm_quantize(const uint16_t *x, const uint16_t *residual, uint16_t *sum,

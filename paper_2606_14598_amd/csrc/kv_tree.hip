@@ -8,7 +8,10 @@
 // are rounded for the second product: to two bf16 terms (2^-16 of each at most) in row tiles of up to
 // 64 rows, to one (2^-8) in others, whose products bind. There l sums the rounded weights: what a
 // weight's rounding by d does to an output is then d (v - o) / l and not d v / l, less where a few
-// weights are most of the sum.
+// weights are most of the sum. Two terms everywhere take 414 us where one takes 324 (32 trees of 60 nodes on
+// 8192 tokens, 8 heads of 128, 4 queries a head), 220 where it takes 173 (201 nodes on 40001). Rounding is
+// relative to a piece's running maximum (the largest weight, 1, stays as it is), so one term's hangs on
+// where the pieces end: on all lengths of a call.
 //
 // A step of a sequence has some tens of nodes, so a row tile of 128 rows is seldom full, and the
 // lengths of a batch differ: the work is divided by what there is. The pieces of a call (a row tile
@@ -20,11 +23,12 @@
 // follows from the lengths on the device, no row outside the sequences is read or written, and sums have
 // a fixed order.
 //
-// Bound by instructions where rows are many, as kv_attention.hip's kernel for many rows is: 32 trees of
-// 60 nodes on 8192 tokens each, 8 heads of 128, 4 queries a head, 315 us (800 TFLOP/s, 880 where no row
-// tile is partly filled); by reading the cache, with two workgroups a CU to hide its latency, where they
-// are few: 16 nodes on the same 163 us (3.4 TB/s). 32 trees of up to 60 nodes on up to 8192 tokens, all
-// different: 235 us where a sequence's keys were divided as the causal kernel divides them, 92 to 99 so.
+// 32 trees of 60 nodes on 8192 tokens each, 8 heads of 128, 4 queries a head, take 315 us (800 TFLOP/s, 880
+// where no row tile is partly filled), 16 nodes on the same 167 (3.3 TB/s). No unit binds alone: of the
+// SIMDs' cycles 47% are matrix and 43% vector instructions (16 nodes: 35% and 43%), which the two
+// wavefronts of each overlap only in part, and 12% of the CUs' cycles are conflicts in LDS. 32 trees of up to
+// 60 nodes on up to 8192 tokens, all different: 235 us where a sequence's keys were divided as the causal
+// kernel divides them, 91 to 99 so.
 #include "kv_attention.hpp"
 
 #include <algorithm>
@@ -34,7 +38,9 @@ namespace {
 
 constexpr int kRows = 128, kTokens = 64;       // of a row tile, and staged at a time
 constexpr int kMostTiles = 1 << 20;            // counted of a sequence: far more than run at once
-// Sequences over whose tokens a wavefront sums, 64 at a time; with more of them keys stay whole.
+// Sequences over whose tokens a wavefront sums, 64 at a time; with more of them keys stay whole, however
+// long: a sequence of 100000 tokens among ones of 500, 8 nodes each, 8 heads of 128, 4 queries a head: 290 us
+// with 512 sequences, 1919 with 513, 1942 with 1024 (355 without the long one).
 constexpr int kSummed = 512;
 
 // Where the pieces of a divided row tile are.

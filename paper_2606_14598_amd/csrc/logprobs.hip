@@ -13,8 +13,8 @@
 // at a time sorted and merged. The first values that a wavefront reads would all be collected: the
 // k-th largest of its lanes' maxima is a bound that k values reach.
 //
-// Bound by reading the logits once: 4096 x 131072 bf16 in 168 us without alternatives (6.4 TB/s; a
-// plain read of as much reaches 7.0), 183 with 5, 200 with 20; 1024 x 131072 float32 in 87. Beside that
+// Bound by reading the logits once: 4096 x 131072 bf16 in 161 us without alternatives (6.7 TB/s; a
+// plain read of as much reaches 6.8 to 7.0), 180 with 5, 199 with 20; 1024 x 131072 float32 in 82. Beside that
 // read stand about 10 vector instructions a value, the exponential counted as four. One row of 131072
 // takes 5.1 us in two launches, 11.0 with 20 alternatives (the networks of the workgroups and of the
 // join, one after the other). us for loads without branches around them (a branch makes the compiler

@@ -304,9 +304,11 @@ def kv_tree_attention(q, cache, block_table, kv_lens, tree, *, fmt: str = "fp8",
     front of the tree, and query i of a sequence sees node n where bit n % 64 of
     tree[q_starts[b] + i, n // 64] is set: itself and its ancestors (tree int64 [T, words], up to
     64 words). A query that sees nothing gives zeros. The weights are rounded to bf16, to two
-    terms in sequences of up to 64 rows. q_starts may end before T: rows of q and the output
-    behind the last sequence are neither read nor written. max_q, max_kv as in kv_attention.
-    Everything else is as there."""
+    terms in sequences of up to 64 rows; one term's rounding may differ with the other sequences
+    of the call, by whose lengths keys are divided (up to 512 sequences; with more a long one among
+    short ones is slow). q_starts may end before T: rows of q and the output behind the last
+    sequence are neither read nor written. max_q, max_kv as in kv_attention. Everything else is as
+    there."""
     if not isinstance(tree, torch.Tensor) or tree.dtype != torch.int64:
         raise TypeError("tree must be an int64 torch.Tensor")
     return _attend(q, cache, block_table, kv_lens, fmt, q_starts, scale, False, tree, max_q, max_kv,
