@@ -10,8 +10,8 @@
 //
 // Bound by memory: 2 (4 with a residual) bytes read and 1 or 17/32 (+ 2) written an element. 4608 x
 // 4096 with a residual takes 22.7 us in int8 (5.8 TB/s; a large copy reaches 5.1), 22.9 in 4 bits (5.4),
-// 4608 x 16384 101 and 97, 2001 x 1000 in 4 bits 4.1, one token of 4096 channels 2.4, two barriers and 64-bit root included. The sum in 64 bits costs a
-// conversion and a product an element, which the loads hide.
+// 4608 x 16384 101 and 97, 2001 x 1000 in 4 bits 4.1, one token of 4096 channels 2.4, two barriers and
+// 64-bit root included. The sum in 64 bits costs a conversion and a product an element, which the loads hide.
 #include "lm_internal.hpp"
 #include "mx_quant.hpp"
 
